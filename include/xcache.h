@@ -371,6 +371,166 @@ xc_status xc_mfma_rate(int32_t shape, int32_t random_operands, void* stream, dou
  * XC_ERR_HIP. */
 xc_status xc_lds_dma_rate(int32_t row_bytes, void* stream, double* tbytes_per_s);
 
+/* ---- Branching rollouts -------------------------------------------------
+ *
+ * Many candidate futures that branch from one history (the chunks already
+ * generated), held in a paged key/value cache: sequences share pages, a fork
+ * copies nothing, and attention reads the history that a batch shares once
+ * for all of its branches.
+ *
+ * A pool manages page buffers that the caller owns and a page table per
+ * sequence; token i of a sequence lies at place first + i of its pages.  A
+ * batch is a set of sequences with the number of each one's last tokens that
+ * are the batch's rows (packed in the order of the sequences); it serves any
+ * number of calls, one per block and pass of a model.  The usual order:
+ *   xc_seq_extend     room for the new tokens of every branch
+ *   xc_batch_set      these tokens as rows
+ *   per block:        xc_qk_norm_rope, xc_branch_attention
+ *
+ * The conventions above hold, with the pool's stream and device (those of
+ * xc_pool_init; another current device is restored before return).  Further:
+ *   - XC_ERR_OOM also reports too few free pages or sequence numbers; the
+ *     call has then changed nothing.
+ *   - The lowest free page and sequence number are always taken first.
+ *   - Calls that change tables (xc_seq_extend, xc_seq_import, xc_pool_compact,
+ *     xc_batch_set) return XC_ERR_STATE while the stream is being captured.
+ *     xc_qk_norm_rope and xc_branch_attention may be captured; such a graph
+ *     holds the batch's tables and pieces: it is replayed while its batch is
+ *     alive and neither the batch nor its sequences' tables have changed, one
+ *     replay or call of one batch at a time.  Two batches share nothing but
+ *     the pool.
+ *   - A pool and its batches are used by one thread at a time; a batch may
+ *     outlive xc_pool_destroy. */
+
+/* Page buffers: keys and values each [n_blocks][n_pages][kv_heads]
+ * [page_tokens][head_dim] of the dtype, one page number for all blocks. */
+typedef struct xc_pool_config {
+  int32_t n_blocks;     /* transformer blocks, up to 4096                     */
+  int32_t q_heads;      /* query heads, a multiple of kv_heads, up to 1024    */
+  int32_t kv_heads;     /* key and value heads                                */
+  int32_t head_dim;     /* 64 or 128, XC_F32 also 32                          */
+  int32_t dtype;        /* XC_F32 or XC_BF16                                  */
+  int32_t page_tokens;  /* 16, 32, 64, 128 or 256                             */
+  int32_t n_pages;      /* n_pages * page_tokens <= 2^30                      */
+  int32_t max_seqs;     /* sequences alive at a time, up to 2^20              */
+} xc_pool_config;
+
+typedef struct xc_pool xc_pool;
+typedef struct xc_batch xc_batch;
+
+/* A pool over the caller's page buffers (device, 16-byte aligned, not
+ * overlapping; their contents are left as they are), which stay alive until
+ * the pool and its batches are gone.  Query heads per key head: up to 256
+ * (XC_F32: 128).
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED (a size this build does not
+ * implement), XC_ERR_OOM, XC_ERR_HIP. */
+xc_status xc_pool_init(const xc_pool_config* config, void* keys, void* values, void* hip_stream, xc_pool** out);
+
+/* Releases the pool (NULL is a no-op; nothing is synchronised). */
+xc_status xc_pool_destroy(xc_pool* pool);
+
+/* Pages that some sequence holds, pages that none holds, sequences alive
+ * (each pointer may be NULL). */
+xc_status xc_pool_info(xc_pool* pool, int32_t* live_pages, int32_t* free_pages, int32_t* live_seqs);
+
+/* A sequence without tokens.  Errors: XC_ERR_INVALID_ARG, XC_ERR_OOM. */
+xc_status xc_seq_new(xc_pool* pool, int32_t* seq);
+
+/* n sequences with the tokens of src, sharing its pages.  Nothing is copied.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_OOM. */
+xc_status xc_seq_fork(xc_pool* pool, int32_t src, int32_t n, int32_t* seqs);
+
+/* Makes room for tokens[i] >= 0 more tokens in seqs[i] (distinct).  Where the
+ * last page of a sequence is partly filled and shared, the sequence gets a
+ * page of its own and the filled rows are copied (all blocks, keys and
+ * values, one launch for all sequences); the new tokens' rows are left as
+ * they are until something writes them.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_OOM (all or nothing), XC_ERR_STATE,
+ * XC_ERR_HIP (sticky). */
+xc_status xc_seq_extend(xc_pool* pool, int32_t n, const int32_t* seqs, const int32_t* tokens);
+
+/* Drops the first `front` tokens (a rolling window) and the last `back`;
+ * pages without a token left are released.
+ * Errors: XC_ERR_INVALID_ARG (more than there are). */
+xc_status xc_seq_trim(xc_pool* pool, int32_t seq, int32_t front, int32_t back);
+
+/* Ends n (distinct) sequences and releases their pages. */
+xc_status xc_seq_free(xc_pool* pool, int32_t n, const int32_t* seqs);
+
+/* Appends the clean past chunks that the handle's current generation sees
+ * (min(n, kv_window - 1) chunks of L tokens, oldest first; every block) to a
+ * sequence: a rollout's history becomes one that many branches share.  The
+ * handle has the pool's dtype, n_blocks, n_heads == kv_heads and head_dim, and
+ * is bound to the same stream and device.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_OOM, XC_ERR_STATE, XC_ERR_HIP (sticky). */
+xc_status xc_seq_import(xc_pool* pool, int32_t seq, xc_handle* h);
+
+/* The table of a sequence: the place of its first token, its tokens, up to cap
+ * page numbers and their full number (each pointer may be NULL). */
+xc_status xc_seq_pages(xc_pool* pool, int32_t seq, int32_t* first, int32_t* tokens, int32_t* pages, size_t cap,
+                       size_t* n_pages);
+
+/* Moves live pages (whole ones, every block) so that they are the pages
+ * 0 .. live - 1: those past that go, in ascending order, to the free ones
+ * below it.  Tables follow; batches of moved sequences are set anew before
+ * their next call.  *moved (may be NULL): pages moved.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE, XC_ERR_HIP (sticky). */
+xc_status xc_pool_compact(xc_pool* pool, int32_t* moved);
+
+/* A batch without rows. */
+xc_status xc_batch_init(xc_pool* pool, xc_batch** out);
+
+/* Releases a batch after its work (NULL is a no-op; synchronises the pool's
+ * stream). */
+xc_status xc_batch_destroy(xc_batch* batch);
+
+/* The rows of the batch: the last new_tokens[i] (0 to all) tokens of seqs[i]
+ * (distinct), packed in this order, at most 2^24 rows.  Uploads the tables
+ * and plans the attention; may allocate.  Valid until the table of one of
+ * the sequences changes (extend, trim, free, compact, import; a fork of it
+ * changes nothing): the calls below then return XC_ERR_STATE.  After
+ * XC_ERR_OOM or XC_ERR_HIP the batch has no rows.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED, XC_ERR_OOM, XC_ERR_STATE,
+ * XC_ERR_HIP (sticky). */
+xc_status xc_batch_set(xc_batch* batch, int32_t n, const int32_t* seqs, const int32_t* new_tokens);
+
+/* Norms and rotation of the batch's queries and keys in one pass: per head
+ * RMSNorm (eps 1e-6) times its gain, then the rotary embedding; queries go to
+ * q_out, keys and values (as they are) to the rows of their tokens in the
+ * pages of one block.  May be repeated for the same tokens (denoising
+ * passes).
+ *   qkv        : device [rows][ld], q heads, then k heads, then v heads of
+ *                head_dim columns each, in the pool's dtype.
+ *   gq, gk     : device float32 [head_dim].
+ *   positions  : device int32 [rows][n_axes]; NULL: no rotation.
+ *   n_axes     : 1, or 3 (frame, row, column; the axis split of
+ *                xc_model_config's rope).
+ *   theta      : rotary base > 1.
+ *   q_out      : device [rows][q_ld], columns as the q part of qkv.
+ * ld and q_ld in elements, rows 16-byte aligned; qkv and q_out do not
+ * overlap (a batch without rows reads neither, they may be NULL).  Arithmetic in float32 with one rounding, angles in 64 bits.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (the batch is not set or out of
+ * date, or a page to be written is shared with another sequence), XC_ERR_HIP
+ * (sticky). */
+xc_status xc_qk_norm_rope(xc_batch* batch, int32_t block, const void* qkv, int64_t ld, const float* gq, const float* gk,
+                          const int32_t* positions, int32_t n_axes, double theta, void* q_out, int64_t q_ld);
+
+/* Attention of the batch's rows: softmax(scale q k^T) v over all tokens of the
+ * row's sequence in one block (no mask, as in the model), key head h serving
+ * query heads h * q_heads / kv_heads and on.  Whole pages that all sequences
+ * with rows have in common are read once for the batch where that pays.
+ *   q      : device [rows][q_ld], out: device [rows][out_ld], both q_heads *
+ *            head_dim columns in the pool's dtype, rows 16-byte aligned, not
+ *            overlapping; NULL where the batch has no rows.
+ *   scale  : positive (a normal number); 0 takes 1 / sqrt(head_dim).
+ * Scores, softmax statistics and sums are float32; bf16 pools round the
+ * probabilities to bf16 for the product with v.  The same call gives the same
+ * bits.  Keys and values outside the sequences are not read.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set or out of date),
+ * XC_ERR_HIP (sticky). */
+xc_status xc_branch_attention(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, void* out,
+                              int64_t out_ld);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,10 @@ SOURCES = [
     "xc_gemm.hip",
     "xc_attention.hip",
     "xc_diag.hip",
+    "xc_pages.hip",
+    "xc_branch.hip",
     "xc_capi.cpp",
+    "xc_pool.cpp",
 ]
 
 ARCH = "gfx950"

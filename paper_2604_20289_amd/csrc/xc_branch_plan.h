@@ -1,0 +1,166 @@
+// How the attention of branching sequences is cut into workgroups: host
+// arithmetic without HIP.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+#include <vector>
+
+namespace xc {
+
+// A workgroup's share of the attention: the query rows of `tokens` batch rows
+// (each with the query heads of one key head) over the keys at places [lo, hi)
+// of one sequence's pages.
+struct AttnUnit {
+  int tok0, tokens;  // batch rows
+  int table;         // the sequence's page table begins at tables[table]
+  int lo, hi;
+  int slot;          // piece the result goes to; -1: it is the whole result
+};
+
+struct PlanSeq {
+  int rows;           // batch rows (its last tokens)
+  int first, tokens;  // keys: places [first, first + tokens) of its pages
+  int table;
+};
+
+struct PlanShape {
+  int tile_rows;  // query rows of a workgroup
+  int group;      // query heads per key head
+  int kv_heads;
+  int D;
+  int elem;       // bytes per element
+  int cus;
+};
+
+struct OwnSlots {
+  int first, n;
+};
+
+struct AttnPlan {
+  std::vector<AttnUnit> units;
+  std::vector<OwnSlots> own;  // per sequence: the slots of its own pieces
+  int shared_slots = 0;       // slots 0 .. shared_slots - 1: pieces of the shared history, of every row
+  int n_slots = 0;            // 0: no row has pieces
+};
+
+constexpr int kPlanMaxSlots = 96;
+constexpr long long kPlanMaxPieceBytes = 1ll << 30;
+
+namespace plan_detail {
+
+inline long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
+
+// keys [lo, hi) in tiles of 64 places from lo rounded down to 16 (a group of
+// 16 places lies in one page)
+inline int tiles_of(int lo, int hi) { return hi > lo ? (int)cdiv(hi - (lo & ~15), 64) : 0; }
+
+// place where piece i of n begins: whole tiles, as even as they go
+inline int cut(int lo, int hi, int n, int i) {
+  if (i == 0) return lo;
+  if (i == n) return hi;
+  return (lo & ~15) + 64 * (int)((long long)tiles_of(lo, hi) * i / n);
+}
+
+// Microseconds of one 64-key tile in a workgroup of `rows` query rows, and of
+// what a workgroup does besides its tiles.
+inline double tile_us(const PlanShape& s, int rows) {
+  const double full = s.elem == 2 ? 2.0 * s.D / 128 : 9.0 * s.D / 128;
+  const double least = s.elem == 2 ? 0.9 : 2.2 * s.D / 128;
+  return std::max(least, full * rows / s.tile_rows);
+}
+constexpr double kUnitUs = 4.0, kMergeUs = 5.0, kBytesPerUs = 4.6e6;
+
+struct Work {
+  double sum = 0, longest = 0;
+  void add(long long units, double us) {
+    if (units <= 0) return;
+    sum += units * us;
+    longest = std::max(longest, us);
+  }
+  double us(int cus) const { return std::max(sum / cus, longest); }
+};
+
+}  // namespace plan_detail
+
+// shared_end: the place up to which every sequence's pages are the same ones
+// (whole pages; 0: nothing shared).
+//
+// Two ways.  Together: the rows of all sequences are packed into workgroups
+// that read the shared history once, the rest is read per sequence, and the
+// pieces are merged: few rows per sequence.  Apart: each sequence's rows run
+// over its history and its own keys in one go: a sequence whose rows fill
+// workgroups by themselves gains nothing by packing.  Either way a long run of
+// keys is cut into pieces of about `c` tiles, so that few rows still fill the
+// chip.  The cheaper of all by the times above is taken.
+inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end, const PlanShape& sh) {
+  using namespace plan_detail;
+  const int per = std::max(1, sh.tile_rows / sh.group);  // batch rows per workgroup
+  long long rows = 0;
+  for (const PlanSeq& q : seqs) rows += q.rows;
+  AttnPlan best;
+  best.own.assign(seqs.size(), {0, 0});
+  if (rows == 0) return best;
+  const PlanSeq* head = nullptr;  // any sequence with rows: the shared places are in all of them
+  for (const PlanSeq& q : seqs)
+    if (q.rows > 0 && head == nullptr) head = &q;
+  const double piece_bytes = (double)rows * sh.kv_heads * sh.group * (sh.D * 4 + 8);
+
+  auto slots_of = [](int tiles, int c) { return tiles ? (int)cdiv(tiles, c) : 0; };
+  double best_us = 0;
+  bool have = false, best_packed = false;
+  int best_c = 0;
+  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128, 192, 256, 512, 1024, 1 << 26};
+  for (int packed = 0; packed < (shared_end > 0 && seqs.size() > 1 ? 2 : 1); ++packed)
+    for (int c : kCuts) {
+      Work w;
+      int shared = 0, most = 0;
+      double read = 0;
+      auto add = [&](long long r, int lo, int hi) {
+        const int tiles = tiles_of(lo, hi), s = slots_of(tiles, c);
+        if (s == 0) return 0;
+        const long long full = r / per, rest = r % per;
+        const double len = (double)tiles / s;
+        w.add(full * s * sh.kv_heads, kUnitUs + len * tile_us(sh, per * sh.group));
+        if (rest) w.add((long long)s * sh.kv_heads, kUnitUs + len * tile_us(sh, (int)rest * sh.group));
+        read += 2.0 * (hi - lo) * sh.D * sh.elem * sh.kv_heads;
+        return s;
+      };
+      if (packed) shared = add(rows, head->first, shared_end);
+      bool direct = !packed;
+      for (const PlanSeq& q : seqs) {
+        if (q.rows == 0) continue;
+        const int s = add(q.rows, packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens);
+        most = std::max(most, s);
+        if (s > 1) direct = false;
+      }
+      const int slots = direct ? 0 : shared + most;
+      if (slots > kPlanMaxSlots || (slots > 2 && slots * piece_bytes > (double)kPlanMaxPieceBytes)) continue;
+      const double us = std::max(w.us(sh.cus), read / kBytesPerUs) +
+                        (slots ? kMergeUs + 2 * slots * piece_bytes / kBytesPerUs : 0);
+      if (!have || us < best_us) have = true, best_us = us, best_packed = packed != 0, best_c = c;
+    }
+
+  auto emit = [&](const PlanSeq& q, int tok0, long long r, int lo, int hi, int slot0, bool direct) {
+    const int n = slots_of(tiles_of(lo, hi), best_c);
+    for (int i = 0; i < n; ++i)
+      for (long long t = 0; t < r; t += per)
+        best.units.push_back({tok0 + (int)t, (int)std::min<long long>(per, r - t), q.table, cut(lo, hi, n, i),
+                              cut(lo, hi, n, i + 1), direct && n == 1 ? -1 : slot0 + i});
+    return n;
+  };
+  if (best_packed) best.shared_slots = best.n_slots = emit(*head, 0, rows, head->first, shared_end, 0, false);
+  int tok0 = 0;
+  for (size_t i = 0; i < seqs.size(); ++i) {
+    const PlanSeq& q = seqs[i];
+    if (q.rows == 0) continue;
+    const int n = emit(q, tok0, q.rows, best_packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens,
+                       best.shared_slots, !best_packed);
+    best.own[i] = {best.shared_slots, !best_packed && n == 1 ? 0 : n};
+    if (best_packed || n > 1) best.n_slots = std::max(best.n_slots, best.shared_slots + n);
+    tok0 += q.rows;
+  }
+  return best;
+}
+
+}  // namespace xc

@@ -39,6 +39,7 @@
 #include <vector>
 
 #include "xc_internal.h"
+#include "xc_pool.h"
 #include "xc_rules.h"
 #include "xcache.h"
 
@@ -1096,6 +1097,25 @@ xc_status forward_pass(xc_handle* h, int32_t step, float timestep, const float* 
 }
 
 }  // namespace
+
+HandleWindow xc::handle_window(const xc_handle* h) {
+  HandleWindow w;
+  w.st = h->st;
+  w.device = h->device;
+  w.dtype = h->dtype;
+  w.n_blocks = h->B;
+  w.heads = h->H;
+  w.D = h->D;
+  w.tokens = (int)h->L;
+  w.Lcap = h->Lcap;
+  w.keys = h->kc;
+  w.values = h->vt;
+  w.sticky = h->sticky;
+  // the clean past chunks that the current generation sees
+  w.chunks = (int)std::min<long long>(h->n, h->Wkv - 1);
+  for (int i = w.chunks; i > 0; --i) w.slots.push_back((int)((h->n - i) % h->Wkv));
+  return w;
+}
 
 extern "C" {
 

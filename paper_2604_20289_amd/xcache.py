@@ -37,7 +37,10 @@ KERNEL_NAMES = ["attention", "gemm_qkv", "gemm_oproj", "gemm_up", "gemm_down", "
 EXPORTED = ["xc_status_string", "xc_init", "xc_forward_chunk", "xc_forward_chunk_noalloc", "xc_kv_update",
             "xc_set_condition", "xc_read_cache", "xc_stats",
             "xc_reset", "xc_destroy", "xc_axpby", "xc_fingerprint_rows", "xc_profile", "xc_kernel_times",
-            "xc_mfma_rate", "xc_lds_dma_rate"]
+            "xc_mfma_rate", "xc_lds_dma_rate",
+            "xc_pool_init", "xc_pool_destroy", "xc_pool_info", "xc_pool_compact", "xc_seq_new", "xc_seq_fork",
+            "xc_seq_extend", "xc_seq_trim", "xc_seq_free", "xc_seq_import", "xc_seq_pages", "xc_batch_init",
+            "xc_batch_destroy", "xc_batch_set", "xc_qk_norm_rope", "xc_branch_attention"]
 
 
 class ViewGroupC(ctypes.Structure):
@@ -70,6 +73,11 @@ class StatsC(ctypes.Structure):
                 ("kv_block_evals", ctypes.c_int64), ("last_step", ctypes.c_int32)]
 
 
+class PoolConfigC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_blocks", "q_heads", "kv_heads", "head_dim", "dtype", "page_tokens",
+                                              "n_pages", "max_seqs")]
+
+
 class XCacheError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -90,6 +98,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                            "(there is no non-HIP fallback)")
     lib = ctypes.CDLL(p)
     vp, i32, u32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_float, ctypes.c_size_t
+    i64 = ctypes.c_int64
     P = ctypes.POINTER
     sig = {
         "xc_status_string": (ctypes.c_char_p, [i32]),
@@ -108,6 +117,22 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "xc_kernel_times": (i32, [vp, i32, P(ctypes.c_int64), P(ctypes.c_double), i32]),
         "xc_mfma_rate": (i32, [i32, i32, vp, P(ctypes.c_double)]),
         "xc_lds_dma_rate": (i32, [i32, vp, P(ctypes.c_double)]),
+        "xc_pool_init": (i32, [P(PoolConfigC), vp, vp, vp, P(vp)]),
+        "xc_pool_destroy": (i32, [vp]),
+        "xc_pool_info": (i32, [vp, P(i32), P(i32), P(i32)]),
+        "xc_pool_compact": (i32, [vp, P(i32)]),
+        "xc_seq_new": (i32, [vp, P(i32)]),
+        "xc_seq_fork": (i32, [vp, i32, i32, vp]),
+        "xc_seq_extend": (i32, [vp, i32, vp, vp]),
+        "xc_seq_trim": (i32, [vp, i32, i32, i32]),
+        "xc_seq_free": (i32, [vp, i32, vp]),
+        "xc_seq_import": (i32, [vp, i32, vp]),
+        "xc_seq_pages": (i32, [vp, i32, P(i32), P(i32), vp, sz, P(sz)]),
+        "xc_batch_init": (i32, [vp, P(vp)]),
+        "xc_batch_destroy": (i32, [vp]),
+        "xc_batch_set": (i32, [vp, i32, vp, vp]),
+        "xc_qk_norm_rope": (i32, [vp, i32, vp, i64, vp, vp, vp, i32, ctypes.c_double, vp, i64]),
+        "xc_branch_attention": (i32, [vp, i32, vp, i64, f32, vp, i64]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -273,6 +298,237 @@ def xc_lds_dma_rate(row_bytes: int, stream: Optional[int] = None) -> float:
     t = ctypes.c_double()
     _check(load_library().xc_lds_dma_rate(row_bytes, stream or None, ctypes.byref(t)), "xc_lds_dma_rate")
     return t.value
+
+
+def xc_pool_init(config: PoolConfigC, keys, values, stream: int = 0) -> int:
+    h = ctypes.c_void_p()
+    _check(load_library().xc_pool_init(ctypes.byref(config), _ptr(keys), _ptr(values), stream or None,
+                                       ctypes.byref(h)), "xc_pool_init")
+    return h.value
+
+
+def xc_pool_destroy(pool: int):
+    _check(load_library().xc_pool_destroy(pool), "xc_pool_destroy")
+
+
+def xc_pool_info(pool: int) -> dict:
+    v = [ctypes.c_int32() for _ in range(3)]
+    _check(load_library().xc_pool_info(pool, *map(ctypes.byref, v)), "xc_pool_info")
+    return dict(zip(("live_pages", "free_pages", "live_seqs"), (x.value for x in v)))
+
+
+def xc_pool_compact(pool: int) -> int:
+    moved = ctypes.c_int32()
+    _check(load_library().xc_pool_compact(pool, ctypes.byref(moved)), "xc_pool_compact")
+    return moved.value
+
+
+def _ints(x) -> ctypes.Array:
+    return (ctypes.c_int32 * len(x))(*x)
+
+
+def xc_seq_new(pool: int) -> int:
+    seq = ctypes.c_int32()
+    _check(load_library().xc_seq_new(pool, ctypes.byref(seq)), "xc_seq_new")
+    return seq.value
+
+
+def xc_seq_fork(pool: int, src: int, n: int) -> list:
+    out = (ctypes.c_int32 * max(n, 0))()
+    _check(load_library().xc_seq_fork(pool, src, n, out), "xc_seq_fork")
+    return list(out)
+
+
+def xc_seq_extend(pool: int, seqs: Sequence[int], tokens: Sequence[int]):
+    if len(seqs) != len(tokens):
+        raise ValueError("one token count per sequence")
+    _check(load_library().xc_seq_extend(pool, len(seqs), _ints(seqs), _ints(tokens)), "xc_seq_extend")
+
+
+def xc_seq_trim(pool: int, seq: int, front: int, back: int):
+    _check(load_library().xc_seq_trim(pool, seq, front, back), "xc_seq_trim")
+
+
+def xc_seq_free(pool: int, seqs: Sequence[int]):
+    _check(load_library().xc_seq_free(pool, len(seqs), _ints(seqs)), "xc_seq_free")
+
+
+def xc_seq_import(pool: int, seq: int, h: int):
+    _check(load_library().xc_seq_import(pool, seq, h), "xc_seq_import")
+
+
+def xc_seq_pages(pool: int, seq: int):
+    """(place of the first token, tokens, page numbers) of a sequence."""
+    first, tokens, n = ctypes.c_int32(), ctypes.c_int32(), ctypes.c_size_t()
+    lib = load_library()
+    _check(lib.xc_seq_pages(pool, seq, None, None, None, 0, ctypes.byref(n)), "xc_seq_pages")
+    pages = np.empty(n.value, np.int32)
+    _check(lib.xc_seq_pages(pool, seq, ctypes.byref(first), ctypes.byref(tokens), pages.ctypes.data, n.value,
+                            ctypes.byref(n)), "xc_seq_pages")
+    return first.value, tokens.value, pages
+
+
+def xc_batch_init(pool: int) -> int:
+    b = ctypes.c_void_p()
+    _check(load_library().xc_batch_init(pool, ctypes.byref(b)), "xc_batch_init")
+    return b.value
+
+
+def xc_batch_destroy(batch: int):
+    _check(load_library().xc_batch_destroy(batch), "xc_batch_destroy")
+
+
+def xc_batch_set(batch: int, seqs: Sequence[int], new_tokens: Sequence[int]):
+    if len(seqs) != len(new_tokens):
+        raise ValueError("one token count per sequence")
+    _check(load_library().xc_batch_set(batch, len(seqs), _ints(seqs), _ints(new_tokens)), "xc_batch_set")
+
+
+def xc_qk_norm_rope(batch: int, block: int, qkv, ld: int, gq, gk, positions, n_axes: int, theta: float, q_out,
+                    q_ld: int):
+    _check(load_library().xc_qk_norm_rope(batch, block, _ptr(qkv), ld, _ptr(gq), _ptr(gk), _ptr(positions), n_axes,
+                                          theta, _ptr(q_out), q_ld), "xc_qk_norm_rope")
+
+
+def xc_branch_attention(batch: int, block: int, q, q_ld: int, scale: float, out, out_ld: int):
+    _check(load_library().xc_branch_attention(batch, block, _ptr(q), q_ld, scale, _ptr(out), out_ld),
+           "xc_branch_attention")
+
+
+def _tensor_dtype(t) -> int:
+    """XC_F32 or XC_BF16 of a tensor."""
+    name = str(t.dtype)
+    if not name.endswith((".float32", ".bfloat16")):
+        raise ValueError(f"{name} is neither float32 nor bfloat16")
+    return XC_F32 if name.endswith("float32") else XC_BF16
+
+
+def _rows(t, what: str, rows: int, width: int, dtype, device) -> int:
+    """The row stride, in elements, of [rows, width] or [rows, heads, head_dim] with dense rows."""
+    if t.dim() not in (2, 3) or t.shape[0] != rows or t.numel() != rows * width:
+        raise ValueError(f"{what} must hold {rows} rows of {width}, not {tuple(t.shape)}")
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{what} must be {dtype} on {device}")
+    if rows and (t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise ValueError(f"{what} must have dense rows")
+    return t.stride(0) if rows > 1 else width
+
+
+class Pool:
+    """Page tables of branching sequences over the page buffers ``keys`` and
+    ``values`` (contiguous device tensors [blocks, pages, kv_heads, page
+    tokens, head_dim], float32 or bfloat16); see xc_pool_init."""
+
+    def __init__(self, keys, values, q_heads: int, max_seqs: int = 64, stream: int = 0):
+        self.p = 0
+        if keys.dim() != 5 or keys.shape != values.shape or keys.dtype != values.dtype or \
+                keys.device != values.device or not keys.is_contiguous() or not values.is_contiguous():
+            raise ValueError("keys and values must be contiguous and alike: "
+                             "[blocks, pages, kv_heads, page tokens, head_dim]")
+        if keys.device.type != "cuda":
+            raise ValueError("keys and values must be on a GPU")
+        c = PoolConfigC()
+        c.n_blocks, c.n_pages, c.kv_heads, c.page_tokens, c.head_dim = keys.shape
+        c.q_heads, c.dtype, c.max_seqs = q_heads, _tensor_dtype(keys), max_seqs
+        self.keys, self.values, self.config = keys, values, c
+        self.p = xc_pool_init(c, keys, values, stream)
+
+    def new(self) -> int:
+        return xc_seq_new(self.p)
+
+    def fork(self, seq: int, n: int) -> list:
+        return xc_seq_fork(self.p, seq, n)
+
+    def extend(self, seqs, tokens):
+        xc_seq_extend(self.p, seqs, tokens)
+
+    def trim(self, seq: int, front: int = 0, back: int = 0):
+        xc_seq_trim(self.p, seq, front, back)
+
+    def free(self, seqs):
+        xc_seq_free(self.p, seqs)
+
+    def compact(self) -> int:
+        return xc_pool_compact(self.p)
+
+    def pages(self, seq: int):
+        return xc_seq_pages(self.p, seq)
+
+    def import_window(self, seq: int, xcache: "XCache"):
+        """Append the past chunks of a rollout's window (xc_seq_import)."""
+        xc_seq_import(self.p, seq, xcache.h)
+
+    def info(self) -> dict:
+        return xc_pool_info(self.p)
+
+    def close(self):
+        if self.p:
+            xc_pool_destroy(self.p)
+            self.p = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Batch:
+    """Rows of a pool's sequences: their norms and rotation, their attention
+    (see xc_batch_set, xc_qk_norm_rope, xc_branch_attention)."""
+
+    def __init__(self, pool: Pool):
+        self.b = 0
+        self.pool, self.rows = pool, 0  # the buffers live as long as the batch
+        c = pool.config
+        self._q_width = c.q_heads * c.head_dim
+        self._width = self._q_width + 2 * c.kv_heads * c.head_dim
+        self._head_dim = c.head_dim
+        self._dtype, self._device = pool.keys.dtype, pool.keys.device
+        self.b = xc_batch_init(pool.p)
+
+    def set(self, seqs, new_tokens):
+        try:
+            xc_batch_set(self.b, seqs, new_tokens)
+        except XCacheError as e:
+            if e.status in (XC_ERR_OOM, XC_ERR_HIP):  # the batch has no rows then
+                self.rows = 0
+            raise
+        self.rows = sum(new_tokens)
+
+    def qk_norm_rope(self, block: int, qkv, gq, gk, positions, theta: float, q_out):
+        """``qkv`` [rows, (q_heads + 2 kv_heads) head_dim], ``q_out`` [rows, q_heads (x) head_dim],
+        ``positions`` int32 [rows, 1 or 3] or None, gains float32 [head_dim]."""
+        ld = _rows(qkv, "qkv", self.rows, self._width, self._dtype, self._device)
+        q_ld = _rows(q_out, "q_out", self.rows, self._q_width, self._dtype, self._device)
+        for g in (gq, gk):
+            if str(g.dtype) != "torch.float32" or g.device != self._device or g.numel() != self._head_dim or \
+                    not g.is_contiguous():
+                raise ValueError(f"gains must be float32 [{self._head_dim}] on {self._device}")
+        axes = 1
+        if positions is not None:
+            if str(positions.dtype) != "torch.int32" or positions.device != self._device or positions.dim() != 2 or \
+                    positions.shape[0] != self.rows or not positions.is_contiguous():
+                raise ValueError(f"positions must be int32 [{self.rows}, axes] on {self._device}")
+            axes = positions.shape[1]
+        xc_qk_norm_rope(self.b, block, qkv, ld, gq, gk, positions, axes, theta, q_out, q_ld)
+
+    def attention(self, block: int, q, out, scale: float = 0.0):
+        """``q`` and ``out`` [rows, q_heads (x) head_dim]."""
+        q_ld = _rows(q, "q", self.rows, self._q_width, self._dtype, self._device)
+        out_ld = _rows(out, "out", self.rows, self._q_width, self._dtype, self._device)
+        xc_branch_attention(self.b, block, q, q_ld, scale, out, out_ld)
+
+    def close(self):
+        if self.b:
+            xc_batch_destroy(self.b)
+            self.b = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class XCache:

@@ -1,0 +1,135 @@
+"""How the attention of branching sequences is cut into workgroups
+(csrc/xc_branch_plan.h), on the CPU: every row meets every key of its
+sequence once, whatever way is taken."""
+import ctypes
+import functools
+import os
+import random
+import subprocess
+import tempfile
+
+import numpy as np
+import pytest
+
+from paper_2604_20289_amd import build
+
+SHIM = r"""
+#include "xc_branch_plan.h"
+using namespace xc;
+static AttnPlan plan;
+extern "C" {
+int make(int n, const int* seqs, int shared_end, int tile_rows, int group, int kv_heads, int D, int elem, int cus) {
+  std::vector<PlanSeq> s;
+  for (int i = 0; i < n; ++i) s.push_back({seqs[4 * i], seqs[4 * i + 1], seqs[4 * i + 2], seqs[4 * i + 3]});
+  plan = plan_attention(s, shared_end, {tile_rows, group, kv_heads, D, elem, cus});
+  return (int)plan.units.size();
+}
+void info(int* out) { out[0] = plan.shared_slots, out[1] = plan.n_slots; }
+void units(int* out) { for (auto& u : plan.units) for (int v : {u.tok0, u.tokens, u.table, u.lo, u.hi, u.slot}) *out++ = v; }
+void own(int* out) { for (auto& o : plan.own) *out++ = o.first, *out++ = o.n; }
+}
+"""
+
+
+@functools.lru_cache(None)
+def lib():
+    d = tempfile.mkdtemp(prefix="xc_plan_")
+    src, so = os.path.join(d, "shim.cpp"), os.path.join(d, "shim.so")
+    with open(src, "w") as f:
+        f.write(SHIM)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-D_GLIBCXX_ASSERTIONS", "-Wall", "-Werror", "-shared", "-fPIC", "-I",
+                    build.CSRC, src, "-o", so], check=True)
+    return ctypes.CDLL(so)
+
+
+def plan(seqs, shared_end, tile_rows=256, group=1, kv_heads=8, D=128, elem=2, cus=256):
+    """seqs: (rows, first, tokens, table)."""
+    flat = [v for s in seqs for v in s]
+    n = lib().make(len(seqs), (ctypes.c_int * len(flat))(*flat), shared_end, tile_rows, group, kv_heads, D, elem, cus)
+    units = np.zeros((n, 6), np.int32)
+    info, own = np.zeros(2, np.int32), np.zeros((len(seqs), 2), np.int32)
+    lib().units(units.ctypes.data_as(ctypes.c_void_p))
+    lib().info(info.ctypes.data_as(ctypes.c_void_p))
+    lib().own(own.ctypes.data_as(ctypes.c_void_p))
+    return units, info[0], info[1], own
+
+
+def check(seqs, shared_end, tile_rows, group, **kw):
+    units, shared, n_slots, own = plan(seqs, shared_end, tile_rows=tile_rows, group=group, **kw)
+    rows = sum(s[0] for s in seqs)
+    first_row = np.cumsum([0] + [s[0] for s in seqs])
+    seq_of = np.repeat(np.arange(len(seqs)), [s[0] for s in seqs])
+    by_row = [[] for _ in range(rows)]
+    for tok0, tokens, table, lo, hi, slot in units.tolist():
+        assert tokens >= 1 and tokens * group <= max(tile_rows, group) and hi > lo
+        assert -1 <= slot < n_slots
+        for t in range(tok0, tok0 + tokens):
+            # the shared places are read through any sequence's table, others through its own
+            assert table == seqs[seq_of[t]][3] or hi <= shared_end
+            by_row[t].append((lo, hi, slot))
+    for t, got in enumerate(by_row):
+        _, first, n, _ = seqs[seq_of[t]]
+        got.sort()
+        assert got[0][0] == first and got[-1][1] == first + n
+        assert all(a[1] == b[0] for a, b in zip(got, got[1:]))
+        slots = [s for _, _, s in got]
+        if slots == [-1]:
+            assert shared == 0 and own[seq_of[t]][1] == 0
+        else:
+            o = own[seq_of[t]]
+            assert sorted(slots) == list(range(shared)) + list(range(o[0], o[0] + o[1]))
+    assert first_row[-1] == rows
+    return units, shared, n_slots
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_every_row_meets_every_key_once(seed):
+    rng = random.Random(seed)
+    page = rng.choice([16, 32, 64, 128, 256])
+    n = rng.choice([1, 2, 3, 9])
+    first = rng.randint(0, page - 1)
+    pages = rng.choice([0, 1, 3, 200])
+    shared_end = pages * page if n > 1 else 0
+    if shared_end <= first:
+        shared_end = 0
+    seqs, table = [], 0
+    for _ in range(n):
+        end = max(shared_end, first + 1) + rng.choice([0, 1, 7, rng.randint(1, 3000)])
+        tokens = end - first
+        rows = rng.choice([0, 1, min(tokens, 5), rng.randint(1, tokens)])
+        seqs.append((rows, first, tokens, table))
+        table += -(-end // page)
+    # sequences without rows do not reach the plan
+    seqs = [s for s in seqs if s[0]]
+    if len(seqs) < 2:
+        shared_end = 0
+    check(seqs, shared_end, rng.choice([128, 256]), rng.choice([1, 2, 3, 5, 12]), kv_heads=rng.choice([1, 4, 12]),
+          D=rng.choice([64, 128]), elem=rng.choice([2, 4]), cus=256)
+
+
+def test_single_tokens_share_their_history():
+    # 16 branches, one row each, behind 14040 tokens: the history in workgroups of all 16 rows
+    seqs = [(1, 0, 14016 + 24 + 10 * i, 1000 * i) for i in range(16)]
+    units, shared, n_slots = check(seqs, 14016, 256, 1, kv_heads=12)
+    assert shared > 1 and n_slots > shared
+    wide = units[units[:, 1] == 16]
+    assert wide[:, 3].min() == 0 and wide[:, 4].max() == 14016
+    # enough workgroups for the chip
+    assert len(units) * 12 >= 256
+
+
+def test_whole_chunks_run_apart():
+    # 7020 rows per branch fill workgroups alone: one pass over history and own keys, nothing to merge
+    seqs = [(7020, 0, 21060, 1000 * i) for i in range(4)]
+    units, shared, n_slots = check(seqs, 14016, 256, 1, kv_heads=12)
+    assert shared == 0 and n_slots == 0 and len(units) == 4 * 28
+
+
+def test_one_long_sequence_is_cut():
+    units, shared, n_slots = check([(1, 3, 48384, 0)], 0, 256, 1, kv_heads=4)
+    assert shared == 0 and n_slots == len(units) > 16
+
+
+def test_no_rows_no_units():
+    units, shared, n_slots, _ = plan([], 0)
+    assert len(units) == 0 and shared == 0 and n_slots == 0
