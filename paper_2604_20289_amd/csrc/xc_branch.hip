@@ -1,23 +1,26 @@
 // Attention of branching sequences over paged keys and values:
 // o = softmax(scale q k^T) v over all keys of the row's sequence.
 //
-// The work is cut on the host (plan_attention): a unit is up to 256 query rows
-// (float32: 128) over a run of keys of one page table.  The rows of a unit are
-// (batch row, query head of one key head); for a shared history they come
-// from many sequences, which is how its keys are read once for all of them.
-// A row whose keys lie in several units gets its pieces merged.
+// The work is cut on the host (plan_attention): a unit is up to tile_rows query
+// rows over a run of keys of one page table.  The rows of a unit are (batch
+// row, query head of one key head); for a shared history they come from many
+// sequences, which is how its keys are read once for all of them.  A row whose
+// keys lie in several units gets its pieces merged.
 //
-// bf16 kernel: 8 waves of 32 query rows.  As in the model's own attention,
-// S^T = K Q^T on v_mfma_f32_32x32x16_bf16 puts one query's scores into one
-// lane, and the K rows sit permuted in LDS so that a lane's scores are the 8
-// consecutive keys its operand of O^T += V^T P^T wants.  What differs:
+// bf16: as in the model's own attention, S^T = K Q^T on
+// v_mfma_f32_32x32x16_bf16 puts one query's scores into one lane, and the K
+// rows sit permuted in LDS so that a lane's scores are the 8 consecutive keys
+// its operand of O^T += V^T P^T wants.  What differs:
 //   * pages hold V row-major (one token is one contiguous write, a page copy
 //     is one run), so its operand is formed by the transposing LDS read;
-//   * tiles of 64 places come through the page table: a 16-place group lies in
-//     one page, so the DMA of 8 rows has a wave-uniform 64-bit base.  A wave
-//     keeps 64 table entries in a register and reads them by lane;
+//   * tiles come through the page table: a 16-place group lies in one page, so
+//     the DMA of 8 rows has a wave-uniform 64-bit base.  A wave keeps 64 table
+//     entries in a register and reads them by lane;
 //   * places outside the unit's keys are not read: their lanes fetch the
 //     nearest valid place, and the scores are masked.
+// Two kernels: branch_wide_kernel, 256 rows that share every tile (bound by the
+// matrix cores and the softmax's arithmetic), and branch_few_kernel, up to 64
+// rows whose keys are dealt to four waves (bound by reading the keys).
 #include "xc_pool.h"
 
 #include "xc_internal.h"
@@ -95,22 +98,136 @@ __device__ __forceinline__ RowOut row_out(const AttnArgs& a, const AttnUnit& un,
   return o;
 }
 
+// The page table of a unit, 64 entries at a time: entry e0 + lane.
+struct TableWindow {
+  const int* table;
+  int e0, e_last, entries, shift, lane;
+  __device__ __forceinline__ TableWindow(const AttnArgs& a, const AttnUnit& un, int ln)
+      : table(a.tables + un.table), e0(un.lo >> a.buf.shift), e_last((un.hi - 1) >> a.buf.shift), shift(a.buf.shift), lane(ln) {
+    entries = table[min(e0 + lane, e_last)];
+  }
+  // from place `from` on the window covers places up to `to`; the load is
+  // waited for here, not where an entry is read
+  __device__ __forceinline__ void cover(int from, int to) {
+    if ((to >> shift) - e0 >= 64) {
+      e0 = from >> shift;
+      entries = table[min(e0 + lane, e_last)];
+      asm volatile("" : "+v"(entries));
+    }
+  }
+  // page of place at, the same in all lanes
+  __device__ __forceinline__ long long page(int at) const {
+    return __builtin_amdgcn_readlane(entries, __builtin_amdgcn_readfirstlane(at >> shift) - e0);
+  }
+};
+
+// Rows of 8 sixteen-byte chunks in LDS, 1 KB blocks of 8 rows.  K: row r,
+// chunk c at ((c % 8) ^ (r / 8 % 2)) * 8 + r % 8: the 16 rows that a quarter
+// wave reads at one chunk fall into 16 bank groups.  V: (r / 4 % 2 * 8 + c) * 4
+// + r % 4: the 4 rows x 4 chunks that half a wave of a transposing read takes
+// are 256 contiguous bytes.  KCG blocks per 8 rows of D columns.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 1) void branch_attn_bf16_kernel(AttnArgs a) {
-  constexpr int KCG = D / 64;             // 1 KB blocks per 8 rows
-  constexpr int NB = 8 * KCG / kWaves;    // blocks per wave, of a K or a V tile
-  constexpr int DT = D / 32, KS = D / 16;
-  // LDS tiles in 1 KB blocks of 8 rows x 8 sixteen-byte chunks.  K: row r,
-  // chunk c at ((c % 8) ^ (r / 8 % 2)) * 8 + r % 8: the 16 rows that a quarter
-  // wave reads at one chunk fall into 16 bank groups.  V: (r / 4 % 2 * 8 + c) *
-  // 4 + r % 4: the 4 rows x 4 chunks that half a wave of a transposing read
-  // takes are 256 contiguous bytes.
-  __shared__ __attribute__((aligned(1024))) char sK0[64 * D * 2];
-  __shared__ __attribute__((aligned(1024))) char sK1[64 * D * 2];
-  __shared__ __attribute__((aligned(1024))) char sK2[64 * D * 2];
-  __shared__ __attribute__((aligned(1024))) char sV0[64 * D * 2];
-  __shared__ __attribute__((aligned(1024))) char sV1[64 * D * 2];
-  __shared__ __attribute__((aligned(1024))) char sV2[64 * D * 2];
+struct Frags {
+  static constexpr int KCG = D / 64, DT = D / 32, KS = D / 16;
+  int k_off, v_off;
+  __device__ __forceinline__ explicit Frags(int lane) {
+    const int hi = lane >> 5, lo = lane & 31;
+    k_off = (lo >> 3) * KCG * 1024 + (hi ^ ((lo >> 3) & 1)) * 128 + (lo & 7) * 16;
+    v_off = hi * KCG * 1024 + (((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) * 64 + ((lane >> 2) & 3) * 16 + (lane & 1) * 8;
+  }
+  // keys of half tile mt, head dims ks * 16 + hi * 8 ..
+  __device__ __forceinline__ bf16x8 k(const char* tile, int mt, int ks) const {
+    return *reinterpret_cast<const bf16x8*>(tile + k_off + mt * 4 * KCG * 1024 + (ks >> 2) * 1024 + (ks & 3) * 256);
+  }
+  // head dim dt * 32 + lo, keys kv * 16 + hi * 8 ..
+  __device__ __forceinline__ bf16x8 v(const char* tile, int kv, int dt) const {
+    const char* p = tile + v_off + kv * 2 * KCG * 1024 + (dt >> 1) * 1024 + (dt & 1) * 256;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 512));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// A block's row and column bytes that lane `lane` fetches: block (rg, cg) of a
+// K or a V tile.
+__device__ __forceinline__ int k_block_row(int rg, int lane) {
+  const int R = rg * 8 + (lane & 7);
+  return key_of_row(R >> 5, R & 31);
+}
+__device__ __forceinline__ unsigned k_block_col(int rg, int cg, int lane) { return (cg * 8 + ((lane >> 3) ^ (rg & 1))) * 16; }
+__device__ __forceinline__ int v_block_row(int rg, int lane) { return rg * 8 + (lane >> 5) * 4 + (lane & 3); }
+__device__ __forceinline__ unsigned v_block_col(int cg, int lane) { return (cg * 8 + ((lane >> 2) & 7)) * 16; }
+
+// The address of a unit's query row r, head dims hi * 8 on.
+__device__ __forceinline__ const bf16* query_row(const AttnArgs& a, const AttnUnit& un, int h, int r, int hi) {
+  return reinterpret_cast<const bf16*>(a.q) + (un.tok0 + r / a.group) * a.q_ld +
+         (long long)(h * a.group + r % a.group) * a.buf.D + hi * 8;
+}
+
+// Scores of keys outside [lo, last]: -infinity.  at0: the place of the half tile's first key.
+__device__ __forceinline__ void mask_half(f32x16& s, int at0, int hi, int lo, int last) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int at = at0 + key_of_row(0, (i >> 2) * 8 + hi * 4 + (i & 3));
+    if (at < lo || at > last) s[i] = -INFINITY;
+  }
+}
+__device__ __forceinline__ float half_max(const f32x16& s) {
+  float m = s[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
+  return m;
+}
+
+// p = 2^(scale s - m), rounded to bf16 for the matrix cores (2^-8 each, of
+// either sign); the sum takes them before that rounding.
+__device__ __forceinline__ float half_probs(const f32x16& s, float scale, float m, bf16x8 (&p)[2]) {
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
+    sum[i & 3] += e;
+    p[i >> 3][i & 7] = (bf16)e;
+  }
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// The maximum that exponents are taken against moves only when a tile's
+// maximum exceeds it by more than this: p stays <= 2^8 in between, which
+// float sums and bf16 carry.
+constexpr float kMaxSlack = 8.0f, kMaxP = 256.0f;
+
+// 8 waves of 32 rows, all on the same tiles of 64 keys, two waves per SIMD in
+// alternation: while one is on the matrix cores (S of the next tile and O of
+// this one, a run of MFMAs and LDS reads), the other takes its softmax
+// (vector instructions alone) and requests tiles; a barrier swaps them.  So
+// both pipes have work at any time without any interleaving within a wave, and
+// a wave needs one score tile instead of two.
+//
+// K and V rings of four slots.  Tile j + 3 is requested between the products
+// of tile j, where the wave has issue slots to spare, and has landed three
+// phases later at the earliest it may be read; the slot it goes to was last
+// read by tile j - 1.
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a) {
+  using F = Frags<D>;
+  constexpr int KCG = F::KCG, DT = F::DT, KS = F::KS;
+  constexpr int NB = 8 * KCG / kWaves;  // blocks per wave, of a K or a V tile
+  // d = 64, where the softmax is the longer phase: its row sums are products
+  // with a row of ones
+  constexpr int ONES = D == 64;
+  constexpr int SLOT = 64 * D * 2;
+  // an array per slot: its reads then do not wait for requests into the others
+  // (K's come after V's in LDS, in order of name: a transposing read's offset
+  // folds into the instruction only below 64 KB)
+  __shared__ __attribute__((aligned(1024))) char tK0[SLOT];
+  __shared__ __attribute__((aligned(1024))) char tK1[SLOT];
+  __shared__ __attribute__((aligned(1024))) char tK2[SLOT];
+  __shared__ __attribute__((aligned(1024))) char tK3[SLOT];
+  __shared__ __attribute__((aligned(1024))) char sV0[SLOT];
+  __shared__ __attribute__((aligned(1024))) char sV1[SLOT];
+  __shared__ __attribute__((aligned(1024))) char sV2[SLOT];
+  __shared__ __attribute__((aligned(1024))) char sV3[SLOT];
   int u, h;
   if (!unit_of(a, u, h)) return;
   const AttnUnit un = a.units[u];
@@ -118,192 +235,232 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_attn_bf16_kernel(AttnAr
   const int hi = lane >> 5, lo = lane & 31;
   const int rows = un.tokens * a.group;
   const int base = un.lo & ~15, n = (un.hi - base + 63) >> 6, last = un.hi - 1;
-  const bool live = wave * 32 < rows;
-  const int shift = a.buf.shift, in_page = (1 << shift) - 1;
-  const long long head_bytes = (long long)D * 2 << shift, page_bytes = head_bytes * a.buf.kv_heads;
+  const bool live = wave * 32 < rows, later = wave >= kWaves / 2;
+  const int in_page = (1 << a.buf.shift) - 1;
+  const long long head_bytes = (long long)D * 2 << a.buf.shift, page_bytes = head_bytes * a.buf.kv_heads;
   const char* Kh = reinterpret_cast<const char*>(a.buf.keys) + h * head_bytes;
   const char* Vh = reinterpret_cast<const char*>(a.buf.values) + h * head_bytes;
+  TableWindow win(a, un, lane);
 
-  // the unit's page table, 64 entries at a time: entry e0 + lane
-  const int* table = a.tables + un.table;
-  const int e_last = last >> shift;
-  int e0 = un.lo >> shift;
-  int entries = table[min(e0 + lane, e_last)];
-
-  // block i of this wave: rows 8 rg .. of the tile, all in the 16-place group rg / 2
+  // Block i of this wave: rows 8 rg .. of the tile, all in the 16-place group
+  // rg / 2.  Past the last key its row is read instead (the scores are masked),
+  // past the last tile that tile: the number of requests in flight is then
+  // always the same, and waits can count them.
   int k_row[NB], v_row[NB];
   unsigned k_col[NB], v_col[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
     const int B = wave + kWaves * i, rg = B / KCG, cg = B % KCG;
-    const int R = rg * 8 + (lane & 7);
-    k_row[i] = key_of_row(R >> 5, R & 31);
-    k_col[i] = (cg * 8 + ((lane >> 3) ^ (rg & 1))) * 16;
-    v_row[i] = rg * 8 + (lane >> 5) * 4 + (lane & 3);
-    v_col[i] = (cg * 8 + ((lane >> 2) & 7)) * 16;
+    k_row[i] = k_block_row(rg, lane) & 15;
+    k_col[i] = k_block_col(rg, cg, lane);
+    v_row[i] = v_block_row(rg, lane) & 15;
+    v_col[i] = v_block_col(cg, lane);
   }
-  auto fetch = [&](const char* buf, int j, int row, unsigned col, char* dst) __attribute__((always_inline)) {
-    const int at = min(max(base + j * 64 + row, un.lo), last);
-    const int e = __builtin_amdgcn_readfirstlane(at >> shift) - e0;
-    const long long page = __builtin_amdgcn_readlane(entries, e);
-    dma16(buf + page * page_bytes, (unsigned)(at & in_page) * (D * 2) + col, dst);
+  const unsigned page_kb = (unsigned)(page_bytes >> 10);
+  long long group_at = 0;  // of block i of the tile being requested: bytes of its 16-place group
+  int group_rows = 15;
+  // half a request: K (first) or V of block i of tile j; j0: the unit's first tile
+  auto fetch = [&](int j, int i, bool is_v, char* dst, bool j0 = false) __attribute__((always_inline)) {
+    if (!is_v) {
+      const int g0 = min(base + min(j, n - 1) * 64 + (wave + kWaves * i) / KCG / 2 * 16, last & ~15);
+      const int page = __builtin_amdgcn_readlane(win.entries, (g0 >> a.buf.shift) - win.e0);
+      group_at = ((long long)((unsigned)page * page_kb) << 10) + (g0 & in_page) * (D * 2);
+      group_rows = min(15, last - g0);
+    }
+    int row = min(is_v ? v_row[i] : k_row[i], group_rows);
+    if (j0) row = max(row, un.lo - base - (wave + kWaves * i) / KCG / 2 * 16);
+    dma16((is_v ? Vh : Kh) + group_at, row * (D * 2) + (is_v ? v_col[i] : k_col[i]), dst + (wave + kWaves * i) * 1024);
   };
-  auto dma_k = [&](int j, char* dst) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < NB; ++i) fetch(Kh, j, k_row[i], k_col[i], dst + (wave + kWaves * i) * 1024);
-  };
-  auto dma_v = [&](int j, char* dst) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < NB; ++i) fetch(Vh, j, v_row[i], v_col[i], dst + (wave + kWaves * i) * 1024);
-  };
-  // the register's entries cover tile j (the next V) to tile j + 1 (the next K)
   auto cover = [&](int j) __attribute__((always_inline)) {
-    const int top = min(base + j * 64 + 127, last) >> shift;
-    if (top - e0 >= 64) {
-      e0 = max(base + j * 64, un.lo) >> shift;
-      entries = table[min(e0 + lane, e_last)];
-      asm volatile("" : "+v"(entries));  // waited for here, not in the loop
+    const int at0 = base + min(j, n - 1) * 64;
+    win.cover(max(at0, un.lo), min(at0 + 63, last));
+  };
+  auto request = [&](int j, char* kd, char* vd, bool j0 = false) __attribute__((always_inline)) {
+    cover(j);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      fetch(j, i, false, kd, j0);
+      fetch(j, i, true, vd, j0);
     }
   };
-
-  dma_k(0, sK0);
-  dma_v(0, sV0);
-  if (n > 1) dma_k(1, sK1), dma_v(1, sV1);
-  if (n > 2) dma_k(2, sK2);
+  request(0, tK0, sV0, true);
+  request(1, tK1, sV1);
+  request(2, tK2, sV2);
+  if (!live) {
+    // waves without rows only stage tiles, between the same barriers
+    XC_WAIT_VM(0);
+    tile_barrier();
+    if (later) tile_barrier();
+    auto stage = [&](int j, char* kd, char* vd) __attribute__((always_inline)) {
+      if (!later) XC_WAIT_VM(2 * NB);
+      tile_barrier();
+      request(j + 3, kd, vd);
+      if (later) XC_WAIT_VM(2 * NB);
+      tile_barrier();
+    };
+    for (int j = 0; j < n - 1; j += 4) {
+      stage(j, tK3, sV3);
+      if (j + 1 >= n - 1) break;
+      stage(j + 1, tK0, sV0);
+      if (j + 2 >= n - 1) break;
+      stage(j + 2, tK1, sV1);
+      if (j + 3 >= n - 1) break;
+      stage(j + 3, tK2, sV2);
+    }
+    if (!later) tile_barrier();
+    return;
+  }
 
   bf16x8 qf[KS];
-  if (live) {
-    const int r = min(wave * 32 + lo, rows - 1);
-    const bf16* q = reinterpret_cast<const bf16*>(a.q) + (un.tok0 + r / a.group) * a.q_ld +
-                    (long long)(h * a.group + r % a.group) * D + hi * 8;
+  {
+    const bf16* q = query_row(a, un, h, min(wave * 32 + lo, rows - 1), hi);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
   }
-  f32x16 oacc[DT];
+  f32x16 s[2], oacc[DT + ONES];
 #pragma unroll
-  for (int i = 0; i < DT; ++i)
+  for (int i = 0; i < DT + ONES; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-
-  const int k_frag = (lo >> 3) * KCG * 1024 + (hi ^ ((lo >> 3) & 1)) * 128 + (lo & 7) * 16;
-  const int v_frag = hi * KCG * 1024 + (((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) * 64 + ((lane >> 2) & 3) * 16 +
-                     (lane & 1) * 8;
-  auto qk = [&](f32x16 (&s)[2], const char* kt) __attribute__((always_inline)) {
+  bf16x8 p[2][2], ones;
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+  for (int i = 0; i < 8; ++i) ones[i] = (bf16)1.0f;
+  const F f(lane);
+  // The matrix phase as a fixed sequence: 4 (DT + ONES) products P V, then 2 KS
+  // products K Q^T, one fragment each, read PF products ahead (an LDS read
+  // takes longer than the one product that the compiler would read ahead).
+  constexpr int PF = 4, NPV = 4 * (DT + ONES), NQK = 2 * KS;
+  bf16x8 fr[PF];
+  auto frag = [&](int i, const char* vt, const char* kt) __attribute__((always_inline)) {
+    if (i >= NPV) return f.k(kt, (i - NPV) & 1, (i - NPV) >> 1);
+    return i % (DT + ONES) < DT ? f.v(vt, i / (DT + ONES), i % (DT + ONES)) : ones;
+  };
+  auto product = [&](int i, const bf16x8& x) __attribute__((always_inline)) {
+    if (i < NPV) {
+      const int kv = i / (DT + ONES), dt = i % (DT + ONES);
+      oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[kv >> 1][kv & 1], oacc[dt], 0, 0, 0);
+    } else {
+      const int mt = (i - NPV) & 1, ks = (i - NPV) >> 1;
+      if (ks == 0) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
-        const bf16x8 k = *reinterpret_cast<const bf16x8*>(kt + k_frag + mt * 4 * KCG * 1024 + (ks >> 2) * 1024 +
-                                                          (ks & 3) * 256);
-        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[ks], s[mt], 0, 0, 0);
+        for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
       }
-  };
-  auto v_half = [&](const char* vt, int off) __attribute__((always_inline)) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + v_frag + off));
-  };
-  auto pv = [&](const bf16x8 (&p)[4], const char* vt) __attribute__((always_inline)) {
-#pragma unroll
-    for (int kv = 0; kv < 4; ++kv)
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const int off = kv * 2 * KCG * 1024 + (dt >> 1) * 1024 + (dt & 1) * 256;
-        const s16x8 v = __builtin_shufflevector(v_half(vt, off), v_half(vt, off + 512), 0, 1, 2, 3, 4, 5, 6, 7);
-        oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p[kv], oacc[dt], 0, 0, 0);
-      }
-  };
-  auto mask = [&](f32x16 (&s)[2], int j) __attribute__((always_inline)) {
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int at = base + j * 64 + key_of_row(mt, (i >> 2) * 8 + hi * 4 + (i & 3));
-        if (at < un.lo || at > last) s[mt][i] = -INFINITY;
-      }
-  };
-  // The running maximum moves only when a tile's maximum exceeds it by more
-  // than 8: p stays <= 2^8 in between, which float sums and bf16 carry.
-  auto update_max = [&](const f32x16 (&s)[2]) __attribute__((always_inline)) {
-    float mx = s[0][0];
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[mt][i]);
-    mx = partner_max(mx) * a.scale;
-    if (mx > m_run + 8.0f) {
-      const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
-      l_run *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
-      m_run = mx;
+      s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[ks], s[mt], 0, 0, 0);
     }
   };
-  // p = 2^(scale s - m), rounded to bf16 for the matrix cores (2^-9 each, of
-  // either sign); the sum takes them before that rounding
-  auto probs = [&](f32x16 (&s)[2], bf16x8 (&p)[4]) __attribute__((always_inline)) {
+  // products [i0, i1); the first PF fragments are in fr; aside(i) goes between them
+  auto products = [&](int i0, int i1, const char* vt, const char* kt, auto&& aside) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NPV + NQK; ++i) {
+      if (i < i0 || i >= i1) continue;
+      const bf16x8 x = fr[i % PF];
+      if (i + PF < i1) fr[i % PF] = frag(i + PF, vt, kt);
+      product(i, x);
+      aside(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto nothing = [](int) __attribute__((always_inline)) {};
+  auto lead = [&](int i0, const char* vt, const char* kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PF; ++i) fr[(i0 + i) % PF] = frag(i0 + i, vt, kt);
+  };
+  // Probabilities of the tile against the maximum so far, which is looked for
+  // only where one of them grew past 2^kMaxSlack (first tile: from -infinity) -
+  // most tiles need none.  Then the tile's own maximum joins in and everything
+  // so far is rescaled.  The limit is checked on the sum or, where there is
+  // none, on the bf16 exponents, whose highest bit stands for 2 and more: the
+  // maximum is taken kMaxSlack higher there.
+  float l_tile = 0.f;
+  auto exps = [&]() __attribute__((always_inline)) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][i], a.scale, -m_run));
-        sum[i & 3] += e;
-        p[mt * 2 + (i >> 3)][i & 7] = (bf16)e;
+        if (!ONES) sum[i & 3] += e;
+        p[mt][i >> 3][i & 7] = (bf16)e;
       }
-    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    if (!ONES) {
+      const float t = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      l_tile = t;
+      return !(t <= 32.f * kMaxP);
+    }
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = __builtin_bit_cast(u32x4, p[k >> 1][k & 1]);
+    const u32x4 o = (b[0] | b[1]) | (b[2] | b[3]);
+    return (((o[0] | o[1]) | (o[2] | o[3])) & 0x40004000u) != 0;
+  };
+  auto softmax = [&]() __attribute__((always_inline)) {
+    const bool grew = exps();
+    if (__builtin_amdgcn_ballot_w64(grew) != 0) {
+      const float mx = partner_max(fmaxf(half_max(s[0]), half_max(s[1]))) * a.scale + (ONES ? kMaxSlack : 0.f);
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT + ONES; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
+      m_run = m_new;
+      exps();
+    }
+    if (!ONES) l_run += l_tile;
+  };
+  // only a unit's first and last tiles reach outside its keys
+  auto mask = [&](int j) __attribute__((always_inline)) {
+    mask_half(s[0], base + j * 64, hi, un.lo, last);
+    mask_half(s[1], base + j * 64 + 32, hi, un.lo, last);
   };
 
-  // tile 0 has landed once at most K(1), V(1), K(2) are in flight (V(0) is
-  // waited for with K(1) below)
   XC_WAIT_VM(0);
   tile_barrier();
-  f32x16 sa[2], sb[2];
-  if (live) {
-    qk(sa, sK0);
-    mask(sa, 0);
-    update_max(sa);
-  }
-  tile_barrier();  // S(0) has read K(0): its slot may be refilled
-
-  // Tile j: S(j + 1) on the matrix cores beside the softmax of S(j), then
-  // O += P(j) V(j).  K(j + 3) and V(j + 2) are requested into the slots that
-  // tile j - 1 was the last to read; what was requested one tile earlier has
-  // landed when the tile ends.
-  auto iter = [&](int j, f32x16 (&s)[2], f32x16 (&sn)[2], const char* kn, const char* vt, char* kd, char* vd)
-      __attribute__((always_inline)) {
-    if (j + 2 < n) cover(j + 2);
-    if (j + 3 < n) dma_k(j + 3, kd);
-    if (j + 2 < n) dma_v(j + 2, vd);
-    if (live) {
-      if (j + 1 < n) qk(sn, kn);
-      bf16x8 p[4];
-      probs(s, p);
-      pv(p, vt);
-      if (j + 1 < n) {
-        if (j + 2 == n) mask(sn, j + 1);
-        update_max(sn);
-      }
-    }
-    if (j + 3 < n) { XC_WAIT_VM(2 * NB); } else { XC_WAIT_VM(0); }
+  lead(NPV, sV0, tK0);
+  products(NPV, NPV + NQK, sV0, tK0, nothing);
+  if (un.lo != base && n > 1) mask(0);
+  if (later) tile_barrier();
+  // tile j: its V, the next K, and the slots of tile j + 3
+  auto iter = [&](int j, const char* vt, const char* kn, char* kd, char* vd) __attribute__((always_inline)) {
+    softmax();
+    // ... all of it here: without this the compiler sinks it behind the barrier, to P's use
+    asm volatile("" : "+v"(p[0][0]), "+v"(p[0][1]), "+v"(p[1][0]), "+v"(p[1][1]), "+v"(l_run));
+    lead(0, vt, kn);  // V has been there for a phase at least
+    if (!later) XC_WAIT_VM(2 * NB);  // all but tile j + 2
+    tile_barrier();
+    cover(j + 3);
+    __builtin_amdgcn_s_setprio(1);
+    products(0, NPV + NQK, vt, kn, [&](int i) __attribute__((always_inline)) {
+      constexpr int GAP = (NPV + NQK) / (2 * NB);
+      if (i % GAP == 1) fetch(j + 3, i / GAP / 2, (i / GAP & 1) != 0, i / GAP & 1 ? vd : kd);
+    });
+    __builtin_amdgcn_s_setprio(0);
+    if (later) XC_WAIT_VM(2 * NB);  // all but tile j + 3
     tile_barrier();
   };
-  for (int j = 0; j < n; j += 6) {
-    iter(j, sa, sb, sK1, sV0, sK0, sV2);
-    if (j + 1 < n) iter(j + 1, sb, sa, sK2, sV1, sK1, sV0);
-    if (j + 2 < n) iter(j + 2, sa, sb, sK0, sV2, sK2, sV1);
-    if (j + 3 < n) iter(j + 3, sb, sa, sK1, sV0, sK0, sV2);
-    if (j + 4 < n) iter(j + 4, sa, sb, sK2, sV1, sK1, sV0);
-    if (j + 5 < n) iter(j + 5, sb, sa, sK0, sV2, sK2, sV1);
+  for (int j = 0; j < n - 1; j += 4) {
+    iter(j, sV0, tK1, tK3, sV3);
+    if (j + 1 >= n - 1) break;
+    iter(j + 1, sV1, tK2, tK0, sV0);
+    if (j + 2 >= n - 1) break;
+    iter(j + 2, sV2, tK3, tK1, sV1);
+    if (j + 3 >= n - 1) break;
+    iter(j + 3, sV3, tK0, tK2, sV2);
   }
-  if (!live) return;
+  if (!later) tile_barrier();
+  {
+    const int slot = (n - 1) & 3;
+    const char* vt = slot == 0 ? sV0 : slot == 1 ? sV1 : slot == 2 ? sV2 : sV3;
+    mask(n - 1);
+    softmax();
+    lead(0, vt, nullptr);
+    products(0, NPV, vt, nullptr, nothing);
+  }
   const int r = wave * 32 + lo;
-  const float l = partner_sum(l_run);
+  const float l = ONES ? oacc[DT][0] : partner_sum(l_run);
   if (r >= rows) return;
   const RowOut o = row_out(a, un, h, r);
   if (un.slot < 0) {
@@ -331,6 +488,234 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_attn_bf16_kernel(AttnAr
       }
     if (hi == 0) a.stats[o.stat] = make_float2(m_run, l);
   }
+}
+
+// Up to 64 rows: four waves, each with all rows (G groups of 32) on keys of
+// its own: tiles of 32 keys (64 at d = 64), dealt in turn.  A wave has a K and a V
+// tile of its own in LDS, asks for the next K as soon as S is formed and for the
+// next V after P V, and waits for nothing but its own requests; there is no
+// barrier until the four partial results are joined in LDS at the end.  80 KB
+// of LDS: two workgroups, eight waves per CU, 128 KB in flight.  Two groups read
+// their queries from LDS in every tile: with two output accumulators there
+// are no registers for them.
+template <int D>
+struct FewShape {
+  static constexpr int HT = 128 / D;                  // 32-key halves of a tile
+  static constexpr int KEYS = 32 * HT;
+  static constexpr int TILE = KEYS * D * 2;           // bytes, 8 KB
+  static constexpr int LOADS = TILE / 1024;
+};
+template <int D, int G>
+__device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, int h, char* sK, char* sV, char* sQ) {
+  using F = Frags<D>;
+  using S = FewShape<D>;
+  constexpr int KCG = F::KCG, DT = F::DT, KS = F::KS, HT = S::HT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hi = lane >> 5, lo = lane & 31;
+  const int rows = un.tokens * a.group;
+  const int base = un.lo & ~15, last = un.hi - 1;
+  const int tiles = (un.hi - base + S::KEYS - 1) / S::KEYS;
+  const int n = (tiles - wave + 3) >> 2;  // this wave's: wave, wave + 4, ..
+  const int in_page = (1 << a.buf.shift) - 1;
+  const long long head_bytes = (long long)D * 2 << a.buf.shift, page_bytes = head_bytes * a.buf.kv_heads;
+  const char* Kh = reinterpret_cast<const char*>(a.buf.keys) + h * head_bytes;
+  const char* Vh = reinterpret_cast<const char*>(a.buf.values) + h * head_bytes;
+  TableWindow win(a, un, lane);
+  // the queries are asked for first and waited for before the loop, which
+  // would otherwise drain the requests behind them in every tile
+  bf16x8 qf[KS];
+  if (G == 1) {
+    const bf16* q = query_row(a, un, h, min(lo, rows - 1), hi);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
+  } else {
+    // fragment (g, ks) as 64 lanes of 16 bytes; a wave brings in a quarter
+#pragma unroll
+    for (int i = 0; i < G * KS / 4; ++i) {
+      const int fi = wave * (G * KS / 4) + i, g = fi / KS, ks = fi % KS;
+      const bf16x8 q = *reinterpret_cast<const bf16x8*>(query_row(a, un, h, min(g * 32 + lo, rows - 1), hi) + ks * 16);
+      *reinterpret_cast<bf16x8*>(sQ + fi * 1024 + lane * 16) = q;
+    }
+  }
+  char* kt = sK + wave * S::TILE;
+  char* vt = sV + wave * S::TILE;
+  // tile i of this wave, of K (is_k) or V
+  auto request = [&](int i, bool is_k) __attribute__((always_inline)) {
+    const int at0 = base + (wave + 4 * i) * S::KEYS;
+#pragma unroll
+    for (int rg = 0; rg < 4 * HT; ++rg) {
+      const int at = min(max(at0 + (is_k ? k_block_row(rg, lane) : v_block_row(rg, lane)), un.lo), last);
+      const char* src = (is_k ? Kh : Vh) + win.page(min(max(at0 + (rg >> 1) * 16, un.lo), last)) * page_bytes;
+#pragma unroll
+      for (int cg = 0; cg < KCG; ++cg)
+        dma16(src, (unsigned)(at & in_page) * (D * 2) + (is_k ? k_block_col(rg, cg, lane) : v_block_col(cg, lane)),
+              (is_k ? kt : vt) + (rg * KCG + cg) * 1024);
+    }
+  };
+  auto cover = [&](int i) __attribute__((always_inline)) {
+    const int at0 = base + (wave + 4 * i) * S::KEYS;
+    win.cover(max(at0, un.lo), min(at0 + S::KEYS - 1, last));
+  };
+  if (n > 0) {
+    cover(0);
+    request(0, true);
+    request(0, false);
+  }
+  if (G == 1) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
+  } else {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    tile_barrier();
+  }
+  f32x16 oacc[G][DT];
+  float m_run[G], l_run[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    m_run[g] = -INFINITY;
+    l_run[g] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[g][i][r] = 0.f;
+  }
+  const F f(lane);
+  for (int i = 0; i < n; ++i) {
+    XC_WAIT_VM(S::LOADS);  // K has landed, V may be on its way
+    asm volatile("" ::: "memory");
+    f32x16 s[G][HT];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int mt = 0; mt < HT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[g][mt][r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 q[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        q[g] = G == 1 ? qf[ks] : *reinterpret_cast<const bf16x8*>(sQ + (g * KS + ks) * 1024 + lane * 16);
+#pragma unroll
+      for (int mt = 0; mt < HT; ++mt) {
+        const bf16x8 k = f.k(kt, mt, ks);
+#pragma unroll
+        for (int g = 0; g < G; ++g) s[g][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[g], s[g][mt], 0, 0, 0);
+      }
+    }
+    const bool more = i + 1 < n;
+    if (more) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this K has been read
+      cover(i + 1);
+      request(i + 1, true);
+    }
+    const int tile = wave + 4 * i;
+    bf16x8 p[G][HT][2];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (tile == 0 || tile == tiles - 1) {
+#pragma unroll
+        for (int mt = 0; mt < HT; ++mt) mask_half(s[g][mt], base + tile * S::KEYS + mt * 32, hi, un.lo, last);
+      }
+      float mx = half_max(s[g][0]);
+#pragma unroll
+      for (int mt = 1; mt < HT; ++mt) mx = fmaxf(mx, half_max(s[g][mt]));
+      mx = partner_max(mx) * a.scale;
+      if (mx > m_run[g] + kMaxSlack) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run[g] - mx);
+        l_run[g] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[g][dt][r] *= alpha;
+        m_run[g] = mx;
+      }
+#pragma unroll
+      for (int mt = 0; mt < HT; ++mt) l_run[g] += half_probs(s[g][mt], a.scale, m_run[g], p[g][mt]);
+    }
+    if (more) { XC_WAIT_VM(S::LOADS); } else { XC_WAIT_VM(0); }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int kv = 0; kv < 2 * HT; ++kv)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const bf16x8 v = f.v(vt, kv, dt);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+          oacc[g][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[g][kv >> 1][kv & 1], oacc[g][dt], 0, 0, 0);
+      }
+    if (more) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this V has been read
+      request(i + 1, false);
+    }
+  }
+
+  // Join the four waves' results, one group of rows after the other: (max, sum)
+  // in the queries' place and unnormalised outputs, waves 0 and 1 in the K
+  // tiles, 2 and 3 in the V tiles; chunk c of row r sits at c ^ r, so that
+  // lanes with different rows meet different banks.
+  constexpr int LPR = D / 4;  // 16-byte chunks, or lanes, per row
+  static_assert(2 * 32 * D * 4 <= 4 * S::TILE, "two partial results per array");
+  float2* stats = reinterpret_cast<float2*>(sQ);
+  auto part = [&](int w, int r, int c) __attribute__((always_inline)) {
+    return reinterpret_cast<f32x4*>(w < 2 ? sK : sV) + ((w & 1) * 32 + r) * LPR + (c ^ (r & (LPR - 1)));
+  };
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    __syncthreads();
+    {
+      const float l = partner_sum(l_run[g]);
+      if (hi == 0) stats[wave * 32 + lo] = make_float2(m_run[g], l);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x4 v;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = oacc[g][dt][e * 4 + k];
+          *part(wave, lo, dt * 8 + e * 2 + hi) = v;
+        }
+    }
+    __syncthreads();
+    const int c = tid % LPR;
+    for (int r = tid / LPR; r < min(32, rows - g * 32); r += 256 / LPR) {
+      float m = stats[r].x, l = 0.f;
+#pragma unroll
+      for (int k = 1; k < 4; ++k) m = fmaxf(m, stats[k * 32 + r].x);
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 st = stats[k * 32 + r];
+        const float w = k < tiles ? __builtin_amdgcn_exp2f(st.x - m) : 0.f;  // a wave without tiles adds nothing
+        l += w * st.y;
+        o += w * *part(k, r, c);
+      }
+      const RowOut ro = row_out(a, un, h, g * 32 + r);
+      if (un.slot < 0) {
+        const float inv = 1.0f / l;
+        bf16x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (bf16)(o[k] * inv);
+        *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16*>(a.out) + ro.out + c * 4) = v;
+      } else {
+        *reinterpret_cast<f32x4*>(a.pieces + ro.piece + c * 4) = o;
+        if (c == 0) a.stats[ro.stat] = make_float2(m, l);
+      }
+    }
+  }
+}
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void branch_few_kernel(AttnArgs a) {
+  // arrays of their own: reads of one then do not wait for requests into another
+  __shared__ __attribute__((aligned(1024))) char sK[4 * FewShape<D>::TILE];
+  __shared__ __attribute__((aligned(1024))) char sV[4 * FewShape<D>::TILE];
+  __shared__ __attribute__((aligned(1024))) char sQ[64 * D * 2];
+  // units outermost, the long ones first: each key is read by one workgroup
+  // (or two in a row), so what counts is that the CUs finish together
+  const int u = blockIdx.x / a.buf.kv_heads, h = blockIdx.x - u * a.buf.kv_heads;
+  const AttnUnit un = a.units[u];
+  if (un.tokens * a.group > 32) few_body<D, 2>(a, un, h, sK, sV, sQ);
+  else few_body<D, 1>(a, un, h, sK, sV, sQ);
 }
 
 // float32: the same division of the work with 4 waves of 32 query rows and
@@ -458,14 +843,17 @@ __global__ __launch_bounds__(64 * kWavesF32, 1) void branch_attn_f32_kernel(Attn
   if (un.slot >= 0 && hi == 0) a.stats[o.stat] = make_float2(m_run, l);
 }
 
-// Joins the pieces of each (row, query head), in slot order:
+// Joins the pieces of each (row, query head):
 // O = sum_p w_p O_p / sum_p w_p l_p, w_p = 2^(m_p - max m).
-// D / 4 lanes own one of them, four head dims each.
+// A wave owns one of them.  It is a chain of memory latencies, so what is
+// independent is in flight together: all statistics (a lane per piece), then
+// the outputs, each of 64 / (D / 4) lane groups taking every so many pieces,
+// four at a time.  Every sum has a fixed order.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
-  constexpr int LPH = D / 4;
-  const long long i = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH;
-  const int d0 = threadIdx.x % LPH * 4;
+  constexpr int LPH = D / 4, NG = 64 / LPH, U = 4;
+  const int lane = threadIdx.x & 63, g = lane / LPH, d0 = lane % LPH * 4;
+  const long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long rq = (long long)a.rows * a.q_heads;
   if (i >= rq) return;
   const int t = (int)(i / a.q_heads);
@@ -475,18 +863,41 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
   auto slot = [&](int p) __attribute__((always_inline)) {
     return (long long)(p < a.shared_slots ? p : own.first + p - a.shared_slots) * rq + i;
   };
-  float m = -INFINITY;
-  for (int p = 0; p < n; ++p) m = fmaxf(m, a.stats[slot(p)].x);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float den = 0.f;
-  for (int p = 0; p < n; ++p) {
-    const long long at = slot(p);
-    const float2 st = a.stats[at];
-    const f32x4 o = *reinterpret_cast<const f32x4*>(a.pieces + at * D + d0);
-    const float w = exp2f(st.x - m);
-    den += w * st.y;
-    acc += w * o;
+  static_assert(kPlanMaxSlots <= 128, "two pieces' statistics per lane");
+  float2 st[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) st[k] = a.stats[slot(min(lane + 64 * k, n - 1))];
+  float m = fmaxf(st[0].x, st[1].x);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  float w[2], den = 0.f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    w[k] = lane + 64 * k < n ? exp2f(st[k].x - m) : 0.f;
+    den += w[k] * st[k].y;
   }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) den += __shfl_xor(den, off, 64);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < n; p0 += NG * U) {
+    f32x4 o[U];
+    float wp[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int p = p0 + k * NG + g;
+      o[k] = *reinterpret_cast<const f32x4*>(a.pieces + slot(min(p, n - 1)) * D + d0);
+      const float w0 = __shfl(w[0], p & 63, 64), w1 = __shfl(w[1], p & 63, 64);
+      wp[k] = p >= n ? 0.f : p < 64 ? w0 : w1;
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (p0 + k * NG + g < n) acc += wp[k] * o[k];
+  }
+#pragma unroll
+  for (int off = 32; off >= LPH; off >>= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
+  if (g != 0) return;
   T* out = reinterpret_cast<T*>(a.out) + t * a.out_ld + (i - (long long)t * a.q_heads) * D + d0;
   const float inv = 1.0f / den;
 #pragma unroll
@@ -496,15 +907,20 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
 }  // namespace
 
 // Requirements (the caller's): D in {64, 128} (float32: 32 too); every unit
-// has at least one key and at most attn_tile_rows query rows; page tables,
-// slots and piece buffers cover what the units name.
+// has at least one key and at most kWideRows query rows (few: kFewRows,
+// float32: kF32Rows); page tables, slots and piece buffers cover what the units name.
 hipError_t launch_branch_attention(int dtype, const AttnArgs& a, hipStream_t st) {
   const int total = a.n_units * a.buf.kv_heads, D = a.buf.D;
   if (total == 0) return hipSuccess;
   const int grid = (total + kXcds - 1) / kXcds * kXcds;
   if (dtype == 1) {
-    if (D == 128) branch_attn_bf16_kernel<128><<<grid, 64 * kWaves, 0, st>>>(a);
-    else branch_attn_bf16_kernel<64><<<grid, 64 * kWaves, 0, st>>>(a);
+    if (a.few) {
+      if (D == 128) branch_few_kernel<128><<<total, 256, 0, st>>>(a);
+      else branch_few_kernel<64><<<total, 256, 0, st>>>(a);
+    } else {
+      if (D == 128) branch_wide_kernel<128><<<grid, 64 * kWaves, 0, st>>>(a);
+      else branch_wide_kernel<64><<<grid, 64 * kWaves, 0, st>>>(a);
+    }
   } else {
     if (D == 128) branch_attn_f32_kernel<128><<<grid, 64 * kWavesF32, 0, st>>>(a);
     else if (D == 64) branch_attn_f32_kernel<64><<<grid, 64 * kWavesF32, 0, st>>>(a);
@@ -512,8 +928,7 @@ hipError_t launch_branch_attention(int dtype, const AttnArgs& a, hipStream_t st)
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_slots == 0) return e;
-  const long long per = 256 / (D / 4), rq = (long long)a.rows * a.q_heads;
-  const unsigned mg = (unsigned)((rq + per - 1) / per);
+  const unsigned mg = (unsigned)(((long long)a.rows * a.q_heads + 3) / 4);
 #define XC_MERGE(T, DD) branch_merge_kernel<T, DD><<<mg, 256, 0, st>>>(a)
   if (dtype == 1) {
     if (D == 128) XC_MERGE(bf16, 128);

@@ -24,8 +24,11 @@ struct PlanSeq {
   int table;
 };
 
+// Query rows (batch row, query head of the group) of a workgroup of the three
+// attention kernels.
+constexpr int kWideRows = 256, kFewRows = 64, kF32Rows = 128;
+
 struct PlanShape {
-  int tile_rows;  // query rows of a workgroup
   int group;      // query heads per key head
   int kv_heads;
   int D;
@@ -42,6 +45,7 @@ struct AttnPlan {
   std::vector<OwnSlots> own;  // per sequence: the slots of its own pieces
   int shared_slots = 0;       // slots 0 .. shared_slots - 1: pieces of the shared history, of every row
   int n_slots = 0;            // 0: no row has pieces
+  bool few = false;           // units for branch_few_kernel
 };
 
 constexpr int kPlanMaxSlots = 96;
@@ -62,23 +66,68 @@ inline int cut(int lo, int hi, int n, int i) {
   return (lo & ~15) + 64 * (int)((long long)tiles_of(lo, hi) * i / n);
 }
 
-// Microseconds of one 64-key tile in a workgroup of `rows` query rows, and of
-// what a workgroup does besides its tiles.
-inline double tile_us(const PlanShape& s, int rows) {
-  const double full = s.elem == 2 ? 2.0 * s.D / 128 : 9.0 * s.D / 128;
-  const double least = s.elem == 2 ? 0.9 : 2.2 * s.D / 128;
-  return std::max(least, full * rows / s.tile_rows);
-}
-constexpr double kUnitUs = 4.0, kMergeUs = 5.0, kBytesPerUs = 4.6e6;
+// What a kernel takes.  A workgroup that has the chip to itself needs tile_us
+// for a 64-key tile and start_us for everything besides; `per_cu` of them share
+// a CU, and together they go at most as fast as `crowd` of them per CU would
+// alone.  Measured at d = 128 / 64: the wide kernel's tile is two phases of its
+// waves, 1.3 us alone and 1.85 with every CU busy (the chip's power limits the
+// clock) / 0.9 either way; the few kernel's is 32 KB, 0.86 us alone (38 KB/us
+// through one workgroup's requests) and 6.0 TB/s in all.
+struct Kernel {
+  int rows;
+  bool few;
+  double tile128, tile64, start;
+  int per_cu;
+  double crowd128, crowd64;
+  double tile_us(const PlanShape& s) const { return s.D == 128 ? tile128 : s.D == 64 ? tile64 : tile64 / 2; }
+  double crowd(const PlanShape& s) const { return s.D == 128 ? crowd128 : crowd64; }
+};
+constexpr Kernel kWide{kWideRows, false, 1.3, 0.9, 5.0, 1, 0.7, 1.0}, kFew{kFewRows, true, 0.86, 0.43, 3.0, 2, 0.62, 0.62},
+    kF32{kF32Rows, false, 9.0, 4.5, 5.0, 1, 1.0, 1.0};
+// distinct keys and values all CUs together read from HBM
+constexpr double kHbmBytesPerUs = 6.0e6;
+// the merge's launch, and its pieces written and read
+constexpr double kMergeUs = 5.0, kPieceBytesPerUs = 1.0e6;
 
+// Time of workgroups on `places` places, the long ones first, each advancing
+// by at most 1 us per us and all together by at most `crowd`: equal shares
+// until the next one ends, its place then taken by the next in line.
 struct Work {
-  double sum = 0, longest = 0;
-  void add(long long units, double us) {
-    if (units <= 0) return;
-    sum += units * us;
-    longest = std::max(longest, us);
+  struct Kind {
+    double us;
+    long long n;
+  };
+  std::vector<Kind> kinds;
+  void add(long long n, double us) {
+    if (n > 0) kinds.push_back({us, n});
   }
-  double us(int cus) const { return std::max(sum / cus, longest); }
+  double us(long long places, double crowd) {
+    std::sort(kinds.begin(), kinds.end(), [](const Kind& a, const Kind& b) { return a.us > b.us; });
+    std::vector<Kind> active;
+    size_t next = 0;
+    long long running = 0;
+    double now = 0;
+    for (;;) {
+      while (next < kinds.size() && running < places) {
+        const long long n = std::min(kinds[next].n, places - running);
+        active.push_back({kinds[next].us, n});
+        running += n;
+        if ((kinds[next].n -= n) == 0) ++next;
+      }
+      if (running == 0) return now;
+      double least = active[0].us;
+      for (const Kind& k : active) least = std::min(least, k.us);
+      const double rate = std::min(1.0, crowd / running);
+      now += least / rate;
+      size_t keep = 0;
+      for (Kind& k : active) {
+        k.us -= least;
+        if (k.us > 0.02 * least) active[keep++] = k;  // those that end within 2% end now
+        else running -= k.n;
+      }
+      active.resize(keep);
+    }
+  }
 };
 
 }  // namespace plan_detail
@@ -95,7 +144,6 @@ struct Work {
 // chip.  The cheaper of all by the times above is taken.
 inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end, const PlanShape& sh) {
   using namespace plan_detail;
-  const int per = std::max(1, sh.tile_rows / sh.group);  // batch rows per workgroup
   long long rows = 0;
   for (const PlanSeq& q : seqs) rows += q.rows;
   AttnPlan best;
@@ -109,37 +157,38 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
   auto slots_of = [](int tiles, int c) { return tiles ? (int)cdiv(tiles, c) : 0; };
   double best_us = 0;
   bool have = false, best_packed = false;
-  int best_c = 0;
+  int best_c = 0, per = 0;
   static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128, 192, 256, 512, 1024, 1 << 26};
-  for (int packed = 0; packed < (shared_end > 0 && seqs.size() > 1 ? 2 : 1); ++packed)
-    for (int c : kCuts) {
-      Work w;
-      int shared = 0, most = 0;
-      double read = 0;
-      auto add = [&](long long r, int lo, int hi) {
-        const int tiles = tiles_of(lo, hi), s = slots_of(tiles, c);
-        if (s == 0) return 0;
-        const long long full = r / per, rest = r % per;
-        const double len = (double)tiles / s;
-        w.add(full * s * sh.kv_heads, kUnitUs + len * tile_us(sh, per * sh.group));
-        if (rest) w.add((long long)s * sh.kv_heads, kUnitUs + len * tile_us(sh, (int)rest * sh.group));
-        read += 2.0 * (hi - lo) * sh.D * sh.elem * sh.kv_heads;
-        return s;
-      };
-      if (packed) shared = add(rows, head->first, shared_end);
-      bool direct = !packed;
-      for (const PlanSeq& q : seqs) {
-        if (q.rows == 0) continue;
-        const int s = add(q.rows, packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens);
-        most = std::max(most, s);
-        if (s > 1) direct = false;
+  std::vector<Kernel> kernels{sh.elem == 4 ? kF32 : kWide};
+  if (sh.elem == 2 && sh.group <= kFewRows) kernels.push_back(kFew);
+  for (const Kernel& k : kernels)
+    for (int packed = 0; packed < (shared_end > 0 && seqs.size() > 1 ? 2 : 1); ++packed)
+      for (int c : kCuts) {
+        const int kper = std::max(1, k.rows / sh.group);  // batch rows per workgroup
+        Work w;
+        int shared = 0, most = 0;
+        double read = 0;
+        auto add = [&](long long r, int lo, int hi) {
+          const int tiles = tiles_of(lo, hi), s = slots_of(tiles, c);
+          if (s == 0) return 0;
+          w.add(cdiv(r, kper) * s * sh.kv_heads, (double)tiles / s * k.tile_us(sh) + k.start);
+          read += 2.0 * (hi - lo) * sh.D * sh.elem * sh.kv_heads;
+          return s;
+        };
+        if (packed) shared = add(rows, head->first, shared_end);
+        bool direct = !packed;
+        for (const PlanSeq& q : seqs) {
+          if (q.rows == 0) continue;
+          const int s = add(q.rows, packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens);
+          most = std::max(most, s);
+          if (s > 1) direct = false;
+        }
+        const int slots = direct ? 0 : shared + most;
+        if (slots > kPlanMaxSlots || (slots > 2 && slots * piece_bytes > (double)kPlanMaxPieceBytes)) continue;
+        const double us = std::max(w.us((long long)k.per_cu * sh.cus, k.crowd(sh) * sh.cus), read / kHbmBytesPerUs) +
+                          (slots ? kMergeUs + slots * piece_bytes / kPieceBytesPerUs : 0);
+        if (!have || us < best_us) have = true, best_us = us, best_packed = packed != 0, best_c = c, per = kper, best.few = k.few;
       }
-      const int slots = direct ? 0 : shared + most;
-      if (slots > kPlanMaxSlots || (slots > 2 && slots * piece_bytes > (double)kPlanMaxPieceBytes)) continue;
-      const double us = std::max(w.us(sh.cus), read / kBytesPerUs) +
-                        (slots ? kMergeUs + 2 * slots * piece_bytes / kBytesPerUs : 0);
-      if (!have || us < best_us) have = true, best_us = us, best_packed = packed != 0, best_c = c;
-    }
 
   auto emit = [&](const PlanSeq& q, int tok0, long long r, int lo, int hi, int slot0, bool direct) {
     const int n = slots_of(tiles_of(lo, hi), best_c);
@@ -160,6 +209,9 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
     if (best_packed || n > 1) best.n_slots = std::max(best.n_slots, best.shared_slots + n);
     tok0 += q.rows;
   }
+  if (best.few)
+    std::stable_sort(best.units.begin(), best.units.end(),
+                     [](const AttnUnit& x, const AttnUnit& y) { return x.hi - x.lo > y.hi - y.lo; });
   return best;
 }
 

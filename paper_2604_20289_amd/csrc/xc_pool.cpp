@@ -243,7 +243,7 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   }
   if (tables.size() > (size_t)kMaxPlaces) return XC_ERR_UNSUPPORTED;
   const int group = p.cfg.q_heads / p.cfg.kv_heads;
-  const PlanShape shape{attn_tile_rows(p.cfg.dtype), group, p.cfg.kv_heads, p.cfg.head_dim, p.esz, p.cus};
+  const PlanShape shape{group, p.cfg.kv_heads, p.cfg.head_dim, p.esz, p.cus};
   const AttnPlan plan = plan_attention(plan_seqs, (int)(shared << shift), shape);
   if ((long long)plan.units.size() * p.cfg.kv_heads > INT32_MAX / 2) return XC_ERR_UNSUPPORTED;
   for (size_t i = 0; i < batch_seqs.size(); ++i) batch_seqs[i].own = plan.own[i];
@@ -311,6 +311,7 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   a.rows = (int)rows;
   a.q_heads = p.cfg.q_heads;
   a.n_slots = plan.n_slots;
+  a.few = plan.few;
   b->place = (const int*)(b->dev + up);
   b->rows = (int)rows;
   b->seqs.swap(seq_copy);
@@ -334,7 +335,7 @@ xc_status xc_pool_init(const xc_pool_config* c, void* keys, void* values, void* 
   while (shift < 8 && (1 << shift) != c->page_tokens) ++shift;
   if ((1 << shift) != c->page_tokens) return XC_ERR_UNSUPPORTED;
   if (c->head_dim != 64 && c->head_dim != 128 && !(c->dtype == XC_F32 && c->head_dim == 32)) return XC_ERR_UNSUPPORTED;
-  if (c->q_heads > kMaxHeads || c->q_heads / c->kv_heads > attn_tile_rows(c->dtype) || c->n_blocks > 4096 ||
+  if (c->q_heads > kMaxHeads || c->q_heads / c->kv_heads > (c->dtype == XC_BF16 ? kWideRows : kF32Rows) || c->n_blocks > 4096 ||
       c->max_seqs > (1 << 20) || (long long)c->n_pages << shift > kMaxPlaces)
     return XC_ERR_UNSUPPORTED;
   if (!aligned16(keys) || !aligned16(values)) return XC_ERR_INVALID_ARG;

@@ -87,10 +87,9 @@ struct AttnArgs {
   int shared_slots;         // slots 0 .. shared_slots - 1 are pieces of every row
   int rows, q_heads;
   int n_slots;              // 0: no row has pieces
+  int few;                  // bf16: units of at most kFewRows query rows, for branch_few_kernel
 };
 
-// Query rows (batch row, query head of the group) of an attention workgroup.
-constexpr int attn_tile_rows(int dtype) { return dtype == 1 ? 256 : 128; }
 
 hipError_t launch_page_copies(const CopyArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes,
                               hipStream_t st);

@@ -18,13 +18,13 @@ SHIM = r"""
 using namespace xc;
 static AttnPlan plan;
 extern "C" {
-int make(int n, const int* seqs, int shared_end, int tile_rows, int group, int kv_heads, int D, int elem, int cus) {
+int make(int n, const int* seqs, int shared_end, int group, int kv_heads, int D, int elem, int cus) {
   std::vector<PlanSeq> s;
   for (int i = 0; i < n; ++i) s.push_back({seqs[4 * i], seqs[4 * i + 1], seqs[4 * i + 2], seqs[4 * i + 3]});
-  plan = plan_attention(s, shared_end, {tile_rows, group, kv_heads, D, elem, cus});
+  plan = plan_attention(s, shared_end, {group, kv_heads, D, elem, cus});
   return (int)plan.units.size();
 }
-void info(int* out) { out[0] = plan.shared_slots, out[1] = plan.n_slots; }
+void info(int* out) { out[0] = plan.shared_slots, out[1] = plan.n_slots, out[2] = plan.few; }
 void units(int* out) { for (auto& u : plan.units) for (int v : {u.tok0, u.tokens, u.table, u.lo, u.hi, u.slot}) *out++ = v; }
 void own(int* out) { for (auto& o : plan.own) *out++ = o.first, *out++ = o.n; }
 }
@@ -42,20 +42,20 @@ def lib():
     return ctypes.CDLL(so)
 
 
-def plan(seqs, shared_end, tile_rows=256, group=1, kv_heads=8, D=128, elem=2, cus=256):
+def plan(seqs, shared_end, group=1, kv_heads=8, D=128, elem=2, cus=256):
     """seqs: (rows, first, tokens, table)."""
     flat = [v for s in seqs for v in s]
-    n = lib().make(len(seqs), (ctypes.c_int * len(flat))(*flat), shared_end, tile_rows, group, kv_heads, D, elem, cus)
+    n = lib().make(len(seqs), (ctypes.c_int * len(flat))(*flat), shared_end, group, kv_heads, D, elem, cus)
     units = np.zeros((n, 6), np.int32)
-    info, own = np.zeros(2, np.int32), np.zeros((len(seqs), 2), np.int32)
+    info, own = np.zeros(3, np.int32), np.zeros((len(seqs), 2), np.int32)
     lib().units(units.ctypes.data_as(ctypes.c_void_p))
     lib().info(info.ctypes.data_as(ctypes.c_void_p))
     lib().own(own.ctypes.data_as(ctypes.c_void_p))
-    return units, info[0], info[1], own
+    return units, info[0], info[1], own, 128 if elem == 4 else 64 if info[2] else 256
 
 
-def check(seqs, shared_end, tile_rows, group, **kw):
-    units, shared, n_slots, own = plan(seqs, shared_end, tile_rows=tile_rows, group=group, **kw)
+def check(seqs, shared_end, group, **kw):
+    units, shared, n_slots, own, tile_rows = plan(seqs, shared_end, group=group, **kw)
     rows = sum(s[0] for s in seqs)
     first_row = np.cumsum([0] + [s[0] for s in seqs])
     seq_of = np.repeat(np.arange(len(seqs)), [s[0] for s in seqs])
@@ -103,14 +103,14 @@ def test_every_row_meets_every_key_once(seed):
     seqs = [s for s in seqs if s[0]]
     if len(seqs) < 2:
         shared_end = 0
-    check(seqs, shared_end, rng.choice([128, 256]), rng.choice([1, 2, 3, 5, 12]), kv_heads=rng.choice([1, 4, 12]),
+    check(seqs, shared_end, rng.choice([1, 2, 3, 5, 12]), kv_heads=rng.choice([1, 4, 12]),
           D=rng.choice([64, 128]), elem=rng.choice([2, 4]), cus=256)
 
 
 def test_single_tokens_share_their_history():
     # 16 branches, one row each, behind 14040 tokens: the history in workgroups of all 16 rows
     seqs = [(1, 0, 14016 + 24 + 10 * i, 1000 * i) for i in range(16)]
-    units, shared, n_slots = check(seqs, 14016, 256, 1, kv_heads=12)
+    units, shared, n_slots = check(seqs, 14016, 1, kv_heads=12)
     assert shared > 1 and n_slots > shared
     wide = units[units[:, 1] == 16]
     assert wide[:, 3].min() == 0 and wide[:, 4].max() == 14016
@@ -121,15 +121,15 @@ def test_single_tokens_share_their_history():
 def test_whole_chunks_run_apart():
     # 7020 rows per branch fill workgroups alone: one pass over history and own keys, nothing to merge
     seqs = [(7020, 0, 21060, 1000 * i) for i in range(4)]
-    units, shared, n_slots = check(seqs, 14016, 256, 1, kv_heads=12)
+    units, shared, n_slots = check(seqs, 14016, 1, kv_heads=12)
     assert shared == 0 and n_slots == 0 and len(units) == 4 * 28
 
 
 def test_one_long_sequence_is_cut():
-    units, shared, n_slots = check([(1, 3, 48384, 0)], 0, 256, 1, kv_heads=4)
+    units, shared, n_slots = check([(1, 3, 48384, 0)], 0, 1, kv_heads=4)
     assert shared == 0 and n_slots == len(units) > 16
 
 
 def test_no_rows_no_units():
-    units, shared, n_slots, _ = plan([], 0)
+    units, shared, n_slots, _, _ = plan([], 0)
     assert len(units) == 0 and shared == 0 and n_slots == 0
