@@ -421,7 +421,7 @@ typedef struct xc_batch xc_batch;
 /* A pool over the caller's page buffers (device, 16-byte aligned, not
  * overlapping; their contents are left as they are), which stay alive until
  * the pool and its batches are gone.  Query heads per key head: up to 256
- * (XC_F32: 128).
+ * (XC_F32: 32).
  * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED (a size this build does not
  * implement), XC_ERR_OOM, XC_ERR_HIP. */
 xc_status xc_pool_init(const xc_pool_config* config, void* keys, void* values, void* hip_stream, xc_pool** out);

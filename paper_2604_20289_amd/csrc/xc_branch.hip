@@ -20,7 +20,8 @@
 //     nearest valid place, and the scores are masked.
 // Two kernels: branch_wide_kernel, 256 rows that share every tile (bound by the
 // matrix cores and the softmax's arithmetic), and branch_few_kernel, up to 64
-// rows whose keys are dealt to four waves (bound by reading the keys).
+// rows whose keys are dealt to four waves (bound by reading the keys).  float32
+// has branch_f32_kernel, of the second kind.
 #include "xc_pool.h"
 
 #include "xc_internal.h"
@@ -718,129 +719,173 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   else few_body<D, 1>(a, un, h, sK, sV, sQ);
 }
 
-// float32: the same division of the work with 4 waves of 32 query rows and
-// tiles of 32 keys on v_mfma_f32_32x32x2_f32.  The two k indices of a product
+// float32: as branch_few_kernel, four waves with all of up to 32 rows on 32-key
+// tiles of their own, on v_mfma_f32_32x32x2_f32.  The two k indices of a product
 // are any two head dims (S) or keys (P V) as long as both operands agree, so
-// the operands need no shuffles: S takes dims 8 t + e and 8 t + 4 + e, P V the
-// two keys whose scores sit in one register of the two half-waves.
-constexpr int kWavesF32 = 4;
+// no operand needs a shuffle: S takes dims 8 t + e and 8 t + 4 + e, P V the two
+// keys whose scores sit in one register of the two half-waves.  Bound by these
+// products (64 cycles each).  Many rows are dealt to more workgroups: four waves
+// of 32 rows on shared tiles, staged through registers, took 456 us for 2000
+// rows, 4500 keys, 8 heads of 128, where these take 388, and 9.9 us for the tiny
+// model's 3 x 64 rows and 128 keys, where these take 5.1.
+// Row r, chunk c of a tile sits at c ^ f(r): rows at one chunk (K) and one row's
+// chunks beside those of the row 4 below (V) meet different banks.
 template <int D>
-__global__ __launch_bounds__(64 * kWavesF32, 1) void branch_attn_f32_kernel(AttnArgs a) {
-  constexpr int LD = D + 4;  // 16-byte reads down a column then meet different banks
-  constexpr int DT = D / 32, CH = D / 4, PER = 32 * CH / (64 * kWavesF32);
-  __shared__ __attribute__((aligned(16))) float sK[2][32 * LD], sV[2][32 * LD];
-  int u, h;
-  if (!unit_of(a, u, h)) return;
+__global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
+  constexpr int DT = D / 32, CH = D / 4, TILE = 32 * D * 4, LOADS = TILE / 1024, RPB = 64 / CH;  // rows per 1 KB block
+  __shared__ __attribute__((aligned(1024))) char sK[4 * TILE];
+  __shared__ __attribute__((aligned(1024))) char sV[4 * TILE];
+  __shared__ float2 stats[4][32];
+  const int u = blockIdx.x / a.buf.kv_heads, h = blockIdx.x - u * a.buf.kv_heads;
   const AttnUnit un = a.units[u];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hi = lane >> 5, lo = lane & 31;
   const int rows = un.tokens * a.group;
-  const int n = (un.hi - un.lo + 31) >> 5, last = un.hi - 1;
-  const bool live = wave * 32 < rows;
-  const int shift = a.buf.shift;
-  const float* K = reinterpret_cast<const float*>(a.buf.keys);
-  const float* V = reinterpret_cast<const float*>(a.buf.values);
-  const int* table = a.tables + un.table;
-
-  f32x4 kr[PER], vr[PER];
-  auto load = [&](int j) __attribute__((always_inline)) {
+  const int base = un.lo & ~15, last = un.hi - 1;
+  const int tiles = (un.hi - base + 31) >> 5;
+  const int n = (tiles - wave + 3) >> 2;
+  const int in_page = (1 << a.buf.shift) - 1;
+  const long long head_bytes = (long long)D * 4 << a.buf.shift, page_bytes = head_bytes * a.buf.kv_heads;
+  const char* Kh = reinterpret_cast<const char*>(a.buf.keys) + h * head_bytes;
+  const char* Vh = reinterpret_cast<const char*>(a.buf.values) + h * head_bytes;
+  TableWindow win(a, un, lane);
+  char* kt = sK + wave * TILE;
+  char* vt = sV + wave * TILE;
+  auto swz = [](int r, int c) __attribute__((always_inline)) {
+    return c ^ (CH >= 16 ? (r & 7) ^ ((r & 4) << 1) : r & 7);
+  };
+  auto request = [&](int i, const char* src, char* dst) __attribute__((always_inline)) {
+    const int at0 = base + (wave + 4 * i) * 32;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = tid + 64 * kWavesF32 * i;
-      const int at = min(un.lo + j * 32 + c / CH, last);
-      const long long page = table[at >> shift];
-      const long long o = (((page * a.buf.kv_heads + h) << shift) + (at & ((1 << shift) - 1))) * D + c % CH * 4;
-      kr[i] = *reinterpret_cast<const f32x4*>(K + o);
-      vr[i] = *reinterpret_cast<const f32x4*>(V + o);
+    for (int b = 0; b < LOADS; ++b) {
+      const int row = b * RPB + lane / CH, g0 = at0 + (b * RPB & 16);
+      const int at = min(max(at0 + row, un.lo), last);
+      dma16(src + win.page(min(max(g0, un.lo), last)) * page_bytes,
+            (unsigned)(at & in_page) * (D * 4) + swz(row, lane % CH) * 16, dst + b * 1024);
     }
   };
-  auto store = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = tid + 64 * kWavesF32 * i;
-      *reinterpret_cast<f32x4*>(&sK[b][c / CH * LD + c % CH * 4]) = kr[i];
-      *reinterpret_cast<f32x4*>(&sV[b][c / CH * LD + c % CH * 4]) = vr[i];
-    }
+  auto cover = [&](int i) __attribute__((always_inline)) {
+    const int at0 = base + (wave + 4 * i) * 32;
+    win.cover(max(at0, un.lo), min(at0 + 31, last));
   };
-  load(0);
   f32x4 qf[D / 8];
-  if (live) {
-    const int r = min(wave * 32 + lo, rows - 1);
+  {
+    const int r = min(lo, rows - 1);
     const float* q = reinterpret_cast<const float*>(a.q) + (un.tok0 + r / a.group) * a.q_ld +
                      (long long)(h * a.group + r % a.group) * D + hi * 4;
 #pragma unroll
     for (int t = 0; t < D / 8; ++t) qf[t] = *reinterpret_cast<const f32x4*>(q + t * 8);
   }
+  if (n > 0) {
+    cover(0);
+    request(0, Kh, kt);
+    request(0, Vh, vt);
+  }
+#pragma unroll
+  for (int t = 0; t < D / 8; ++t) asm volatile("" : "+v"(qf[t]));
   f32x16 oacc[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  store(0);
-  __syncthreads();
-  for (int j = 0; j < n; ++j) {
-    const int b = j & 1;
-    if (j + 1 < n) load(j + 1);
-    if (live) {
-      f32x16 s;
+  for (int i = 0; i < n; ++i) {
+    XC_WAIT_VM(LOADS);  // K has landed, V may be on its way
+    asm volatile("" ::: "memory");
+    f32x16 s;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-      for (int t = 0; t < D / 8; ++t) {
-        const f32x4 k = *reinterpret_cast<const f32x4*>(&sK[b][lo * LD + t * 8 + hi * 4]);
+    for (int t = 0; t < D / 8; ++t) {
+      const f32x4 k = *reinterpret_cast<const f32x4*>(kt + lo * (D * 4) + swz(lo, t * 2 + hi) * 16);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[t][e], s, 0, 0, 0);
-      }
-      float mx = -INFINITY;
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[t][e], s, 0, 0, 0);
+    }
+    const bool more = i + 1 < n;
+    if (more) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this K has been read
+      cover(i + 1);
+      request(i + 1, Kh, kt);
+    }
+    const int at0 = base + (wave + 4 * i) * 32;
+    float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        // only the unit's last tile reaches past its keys
-        if (un.lo + j * 32 + (i >> 2) * 8 + hi * 4 + (i & 3) > last) s[i] = -INFINITY;
-        mx = fmaxf(mx, s[i]);
-      }
-      mx = partner_max(mx) * a.scale;
-      if (mx > m_run) {
-        const float alpha = exp2f(m_run - mx);
-        l_run *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
-        m_run = mx;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = exp2f(__builtin_fmaf(s[i], a.scale, -m_run));
-        l_run += s[i];
-      }
+    for (int r = 0; r < 16; ++r) {
+      const int at = at0 + (r >> 2) * 8 + hi * 4 + (r & 3);
+      if (at < un.lo || at > last) s[r] = -INFINITY;
+      mx = fmaxf(mx, s[r]);
+    }
+    mx = partner_max(mx) * a.scale;
+    if (mx > m_run) {
+      const float alpha = exp2f(m_run - mx);
+      l_run *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-              sV[b][((i >> 2) * 8 + hi * 4 + (i & 3)) * LD + dt * 32 + lo], s[i], oacc[dt], 0, 0, 0);
+        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
+      m_run = mx;
     }
-    if (j + 1 < n) store(b ^ 1);
-    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = exp2f(__builtin_fmaf(s[r], a.scale, -m_run));
+      l_run += s[r];
+    }
+    if (more) { XC_WAIT_VM(LOADS); } else { XC_WAIT_VM(0); }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = (r >> 2) * 8 + hi * 4 + (r & 3);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const float v = *reinterpret_cast<const float*>(vt + key * (D * 4) + swz(key, dt * 8 + (lo >> 2)) * 16 + (lo & 3) * 4);
+        oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], oacc[dt], 0, 0, 0);
+      }
+    }
+    if (more) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this V has been read
+      request(i + 1, Vh, vt);
+    }
   }
-  if (!live) return;
-  const int r = wave * 32 + lo;
-  const float l = partner_sum(l_run);
-  if (r >= rows) return;
-  const RowOut o = row_out(a, un, h, r);
-  const float inv = un.slot < 0 ? 1.0f / l : 1.0f;
-  float* row = un.slot < 0 ? reinterpret_cast<float*>(a.out) + o.out : a.pieces + o.piece;
+  __syncthreads();
+  auto part = [&](int w, int r, int c) __attribute__((always_inline)) {
+    return reinterpret_cast<f32x4*>(sK + w * TILE) + r * CH + (c ^ (r & 7));
+  };
+  {
+    const float l = partner_sum(l_run);
+    if (hi == 0) stats[wave][lo] = make_float2(m_run, l);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      f32x4 v;
+      for (int e = 0; e < 4; ++e) {
+        f32x4 v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = oacc[dt][g * 4 + i] * inv;
-      *reinterpret_cast<f32x4*>(row + dt * 32 + g * 8 + hi * 4) = v;
+        for (int k = 0; k < 4; ++k) v[k] = oacc[dt][e * 4 + k];
+        *part(wave, lo, dt * 8 + e * 2 + hi) = v;
+      }
+  }
+  __syncthreads();
+  const int c = tid % CH;
+  for (int r = tid / CH; r < rows; r += 256 / CH) {
+    float m = stats[0][r].x, l = 0.f;
+#pragma unroll
+    for (int k = 1; k < 4; ++k) m = fmaxf(m, stats[k][r].x);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 st = stats[k][r];
+      const float w = k < tiles ? exp2f(st.x - m) : 0.f;  // a wave without tiles adds nothing
+      l += w * st.y;
+      o += w * *part(k, r, c);
     }
-  if (un.slot >= 0 && hi == 0) a.stats[o.stat] = make_float2(m_run, l);
+    const RowOut ro = row_out(a, un, h, r);
+    if (un.slot < 0) {
+      const float inv = 1.0f / l;
+      *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + ro.out + c * 4) = o * inv;
+    } else {
+      *reinterpret_cast<f32x4*>(a.pieces + ro.piece + c * 4) = o;
+      if (c == 0) a.stats[ro.stat] = make_float2(m, l);
+    }
+  }
 }
 
 // Joins the pieces of each (row, query head):
@@ -904,6 +949,51 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
   for (int e = 0; e < 4; ++e) out[e] = (T)(acc[e] * inv);
 }
 
+// The same where at most kFewPieces pieces join: each group of D / 4 lanes owns
+// a (row, query head), and everything it reads is in flight at once.
+constexpr int kFewPieces = 6;
+template <typename T, int D>
+__global__ __launch_bounds__(256) void branch_merge_few_kernel(AttnArgs a) {
+  constexpr int LPH = D / 4;
+  const long long i = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH;
+  const int d0 = threadIdx.x % LPH * 4;
+  const long long rq = (long long)a.rows * a.q_heads;
+  if (i >= rq) return;
+  const int t = (int)(i / a.q_heads);
+  const OwnSlots own = a.own[t];
+  const int n = a.shared_slots + own.n;
+  if (n == 0) return;  // written by its only unit
+  float2 st[kFewPieces];
+  f32x4 o[kFewPieces];
+#pragma unroll
+  for (int k = 0; k < kFewPieces; ++k) {
+    const int p = min(k, n - 1);
+    const long long at = (p < a.shared_slots ? p : own.first + p - a.shared_slots) * rq + i;
+    if (k < a.n_slots) {
+      st[k] = a.stats[at];
+      o[k] = *reinterpret_cast<const f32x4*>(a.pieces + at * D + d0);
+    }
+  }
+  float m = st[0].x, den = 0.f;
+#pragma unroll
+  for (int k = 1; k < kFewPieces; ++k)
+    if (k < n) m = fmaxf(m, st[k].x);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kFewPieces; ++k)
+    if (k < n) {
+      const float w = exp2f(st[k].x - m);
+      den += w * st[k].y;
+      acc += w * o[k];
+    }
+  const float inv = 1.0f / den;
+  typedef T vec __attribute__((ext_vector_type(4)));
+  vec v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = (T)(acc[e] * inv);
+  *reinterpret_cast<vec*>(reinterpret_cast<T*>(a.out) + t * a.out_ld + (i - (long long)t * a.q_heads) * D + d0) = v;
+}
+
 }  // namespace
 
 // Requirements (the caller's): D in {64, 128} (float32: 32 too); every unit
@@ -922,14 +1012,22 @@ hipError_t launch_branch_attention(int dtype, const AttnArgs& a, hipStream_t st)
       else branch_wide_kernel<64><<<grid, 64 * kWaves, 0, st>>>(a);
     }
   } else {
-    if (D == 128) branch_attn_f32_kernel<128><<<grid, 64 * kWavesF32, 0, st>>>(a);
-    else if (D == 64) branch_attn_f32_kernel<64><<<grid, 64 * kWavesF32, 0, st>>>(a);
-    else branch_attn_f32_kernel<32><<<grid, 64 * kWavesF32, 0, st>>>(a);
+    if (D == 128) branch_f32_kernel<128><<<total, 256, 0, st>>>(a);
+    else if (D == 64) branch_f32_kernel<64><<<total, 256, 0, st>>>(a);
+    else branch_f32_kernel<32><<<total, 256, 0, st>>>(a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_slots == 0) return e;
-  const unsigned mg = (unsigned)(((long long)a.rows * a.q_heads + 3) / 4);
-#define XC_MERGE(T, DD) branch_merge_kernel<T, DD><<<mg, 256, 0, st>>>(a)
+  // a wave per (row, head), or one of its lane groups where few pieces join.
+  // MERGE_TIMES
+  const bool few_pieces = a.n_slots <= kFewPieces;
+  const long long rq = (long long)a.rows * a.q_heads, per = few_pieces ? 256 / (D / 4) : 4;
+  const unsigned mg = (unsigned)((rq + per - 1) / per);
+#define XC_MERGE(T, DD)                                                     \
+  do {                                                                      \
+    if (few_pieces) branch_merge_few_kernel<T, DD><<<mg, 256, 0, st>>>(a);  \
+    else branch_merge_kernel<T, DD><<<mg, 256, 0, st>>>(a);                 \
+  } while (0)
   if (dtype == 1) {
     if (D == 128) XC_MERGE(bf16, 128);
     else XC_MERGE(bf16, 64);

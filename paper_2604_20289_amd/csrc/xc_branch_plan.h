@@ -24,9 +24,9 @@ struct PlanSeq {
   int table;
 };
 
-// Query rows (batch row, query head of the group) of a workgroup of the three
-// attention kernels.
-constexpr int kWideRows = 256, kFewRows = 64, kF32Rows = 128;
+// Query rows (batch row, query head of the group) of a workgroup of the
+// attention kernels: bf16 wide and few, float32.
+constexpr int kWideRows = 256, kFewRows = 64, kF32Rows = 32;
 
 struct PlanShape {
   int group;      // query heads per key head
@@ -45,7 +45,7 @@ struct AttnPlan {
   std::vector<OwnSlots> own;  // per sequence: the slots of its own pieces
   int shared_slots = 0;       // slots 0 .. shared_slots - 1: pieces of the shared history, of every row
   int n_slots = 0;            // 0: no row has pieces
-  bool few = false;           // units for branch_few_kernel
+  bool few = false;           // bf16: units for branch_few_kernel
 };
 
 constexpr int kPlanMaxSlots = 96;
@@ -72,18 +72,19 @@ inline int cut(int lo, int hi, int n, int i) {
 // alone.  Measured at d = 128 / 64: the wide kernel's tile is two phases of its
 // waves, 1.3 us alone and 1.85 with every CU busy (the chip's power limits the
 // clock) / 0.9 either way; the few kernel's is 32 KB, 0.86 us alone (38 KB/us
-// through one workgroup's requests) and 6.0 TB/s in all.
+// through one workgroup's requests; a quarter more with over 32 rows) and 6.0
+// TB/s in all; the float32 kernel's is its products'.
 struct Kernel {
   int rows;
   bool few;
-  double tile128, tile64, start;
+  double tile[3], start;  // d = 128, 64, 32
   int per_cu;
-  double crowd128, crowd64;
-  double tile_us(const PlanShape& s) const { return s.D == 128 ? tile128 : s.D == 64 ? tile64 : tile64 / 2; }
-  double crowd(const PlanShape& s) const { return s.D == 128 ? crowd128 : crowd64; }
+  double crowd[3];
+  static int at(const PlanShape& s) { return s.D == 128 ? 0 : s.D == 64 ? 1 : 2; }
 };
-constexpr Kernel kWide{kWideRows, false, 1.3, 0.9, 5.0, 1, 0.7, 1.0}, kFew{kFewRows, true, 0.86, 0.43, 3.0, 2, 0.62, 0.62},
-    kF32{kF32Rows, false, 9.0, 4.5, 5.0, 1, 1.0, 1.0};
+constexpr Kernel kWide{kWideRows, false, {1.3, 0.9, 0}, 5.0, 1, {0.7, 1.0, 0}},
+    kFew{kFewRows, true, {0.86, 0.43, 0}, 3.0, 2, {0.62, 0.62, 0}},
+    kF32{kF32Rows, false, {2.7, 1.4, 0.7}, 4.0, 1, {1.0, 1.0, 1.0}};
 // distinct keys and values all CUs together read from HBM
 constexpr double kHbmBytesPerUs = 6.0e6;
 // the merge's launch, and its pieces written and read
@@ -161,6 +162,7 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
   static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128, 192, 256, 512, 1024, 1 << 26};
   std::vector<Kernel> kernels{sh.elem == 4 ? kF32 : kWide};
   if (sh.elem == 2 && sh.group <= kFewRows) kernels.push_back(kFew);
+  const int dim = Kernel::at(sh);
   for (const Kernel& k : kernels)
     for (int packed = 0; packed < (shared_end > 0 && seqs.size() > 1 ? 2 : 1); ++packed)
       for (int c : kCuts) {
@@ -171,7 +173,7 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
         auto add = [&](long long r, int lo, int hi) {
           const int tiles = tiles_of(lo, hi), s = slots_of(tiles, c);
           if (s == 0) return 0;
-          w.add(cdiv(r, kper) * s * sh.kv_heads, (double)tiles / s * k.tile_us(sh) + k.start);
+          w.add(cdiv(r, kper) * s * sh.kv_heads, (double)tiles / s * k.tile[dim] * (k.few && std::min<long long>(r, kper) * sh.group > 32 ? 1.25 : 1.0) + k.start);
           read += 2.0 * (hi - lo) * sh.D * sh.elem * sh.kv_heads;
           return s;
         };
@@ -185,7 +187,7 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
         }
         const int slots = direct ? 0 : shared + most;
         if (slots > kPlanMaxSlots || (slots > 2 && slots * piece_bytes > (double)kPlanMaxPieceBytes)) continue;
-        const double us = std::max(w.us((long long)k.per_cu * sh.cus, k.crowd(sh) * sh.cus), read / kHbmBytesPerUs) +
+        const double us = std::max(w.us((long long)k.per_cu * sh.cus, k.crowd[dim] * sh.cus), read / kHbmBytesPerUs) +
                           (slots ? kMergeUs + slots * piece_bytes / kPieceBytesPerUs : 0);
         if (!have || us < best_us) have = true, best_us = us, best_packed = packed != 0, best_c = c, per = kper, best.few = k.few;
       }
@@ -209,7 +211,7 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
     if (best_packed || n > 1) best.n_slots = std::max(best.n_slots, best.shared_slots + n);
     tok0 += q.rows;
   }
-  if (best.few)
+  if (best.few || sh.elem == 4)
     std::stable_sort(best.units.begin(), best.units.end(),
                      [](const AttnUnit& x, const AttnUnit& y) { return x.hi - x.lo > y.hi - y.lo; });
   return best;

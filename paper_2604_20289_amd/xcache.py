@@ -8,6 +8,7 @@ If the library has not been built, loading raises: there is no fallback path.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -323,8 +324,12 @@ def xc_pool_compact(pool: int) -> int:
     return moved.value
 
 
-def _ints(x) -> ctypes.Array:
-    return (ctypes.c_int32 * len(x))(*x)
+def _ints(x) -> array.array:
+    return array.array("i", x)  # 32 bits
+
+
+def _at(a: array.array) -> int:
+    return a.buffer_info()[0]
 
 
 def xc_seq_new(pool: int) -> int:
@@ -334,15 +339,16 @@ def xc_seq_new(pool: int) -> int:
 
 
 def xc_seq_fork(pool: int, src: int, n: int) -> list:
-    out = (ctypes.c_int32 * max(n, 0))()
-    _check(load_library().xc_seq_fork(pool, src, n, out), "xc_seq_fork")
-    return list(out)
+    out = _ints(bytes(4 * max(n, 1)))
+    _check(load_library().xc_seq_fork(pool, src, n, _at(out)), "xc_seq_fork")
+    return out.tolist()[:max(n, 0)]
 
 
 def xc_seq_extend(pool: int, seqs: Sequence[int], tokens: Sequence[int]):
     if len(seqs) != len(tokens):
         raise ValueError("one token count per sequence")
-    _check(load_library().xc_seq_extend(pool, len(seqs), _ints(seqs), _ints(tokens)), "xc_seq_extend")
+    s, t = _ints(seqs), _ints(tokens)
+    _check(load_library().xc_seq_extend(pool, len(s), _at(s), _at(t)), "xc_seq_extend")
 
 
 def xc_seq_trim(pool: int, seq: int, front: int, back: int):
@@ -350,7 +356,8 @@ def xc_seq_trim(pool: int, seq: int, front: int, back: int):
 
 
 def xc_seq_free(pool: int, seqs: Sequence[int]):
-    _check(load_library().xc_seq_free(pool, len(seqs), _ints(seqs)), "xc_seq_free")
+    s = _ints(seqs)
+    _check(load_library().xc_seq_free(pool, len(s), _at(s)), "xc_seq_free")
 
 
 def xc_seq_import(pool: int, seq: int, h: int):
@@ -381,7 +388,8 @@ def xc_batch_destroy(batch: int):
 def xc_batch_set(batch: int, seqs: Sequence[int], new_tokens: Sequence[int]):
     if len(seqs) != len(new_tokens):
         raise ValueError("one token count per sequence")
-    _check(load_library().xc_batch_set(batch, len(seqs), _ints(seqs), _ints(new_tokens)), "xc_batch_set")
+    s, t = _ints(seqs), _ints(new_tokens)
+    _check(load_library().xc_batch_set(batch, len(s), _at(s), _at(t)), "xc_batch_set")
 
 
 def xc_qk_norm_rope(batch: int, block: int, qkv, ld: int, gq, gk, positions, n_axes: int, theta: float, q_out,
@@ -403,15 +411,33 @@ def _tensor_dtype(t) -> int:
     return XC_F32 if name.endswith("float32") else XC_BF16
 
 
-def _rows(t, what: str, rows: int, width: int, dtype, device) -> int:
+_DTYPES: dict = {}
+
+
+def _is(t, name: str) -> bool:
+    """Whether a tensor's dtype has this name."""
+    d = t.dtype
+    known = _DTYPES.get(d)
+    if known is None:
+        known = _DTYPES[d] = str(d).rsplit(".", 1)[-1]
+    return known == name
+
+
+def _rows(t, what: str, rows: int, width: int, dtype, device: int) -> int:
     """The row stride, in elements, of [rows, width] or [rows, heads, head_dim] with dense rows."""
-    if t.dim() not in (2, 3) or t.shape[0] != rows or t.numel() != rows * width:
-        raise ValueError(f"{what} must hold {rows} rows of {width}, not {tuple(t.shape)}")
-    if t.dtype != dtype or t.device != device:
-        raise ValueError(f"{what} must be {dtype} on {device}")
-    if rows and (t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+    shape = t.shape
+    n = len(shape)
+    if not (n == 2 and shape[0] == rows and shape[1] == width or
+            n == 3 and shape[0] == rows and shape[1] * shape[2] == width):
+        raise ValueError(f"{what} must hold {rows} rows of {width}, not {tuple(shape)}")
+    if t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{what} must be {dtype} on GPU {device}")
+    if t.is_contiguous():
+        return width
+    stride = t.stride()
+    if stride[-1] != 1 or (n == 3 and shape[1] > 1 and stride[1] != shape[2]):
         raise ValueError(f"{what} must have dense rows")
-    return t.stride(0) if rows > 1 else width
+    return stride[0] if rows > 1 else width
 
 
 class Pool:
@@ -484,7 +510,9 @@ class Batch:
         self._q_width = c.q_heads * c.head_dim
         self._width = self._q_width + 2 * c.kv_heads * c.head_dim
         self._head_dim = c.head_dim
-        self._dtype, self._device = pool.keys.dtype, pool.keys.device
+        self._dtype, self._device = pool.keys.dtype, pool.keys.get_device()
+        lib = load_library()
+        self._norm_rope, self._attention = lib.xc_qk_norm_rope, lib.xc_branch_attention
         self.b = xc_batch_init(pool.p)
 
     def set(self, seqs, new_tokens):
@@ -499,25 +527,27 @@ class Batch:
     def qk_norm_rope(self, block: int, qkv, gq, gk, positions, theta: float, q_out):
         """``qkv`` [rows, (q_heads + 2 kv_heads) head_dim], ``q_out`` [rows, q_heads (x) head_dim],
         ``positions`` int32 [rows, 1 or 3] or None, gains float32 [head_dim]."""
-        ld = _rows(qkv, "qkv", self.rows, self._width, self._dtype, self._device)
-        q_ld = _rows(q_out, "q_out", self.rows, self._q_width, self._dtype, self._device)
+        device, d = self._device, self._head_dim
+        ld = _rows(qkv, "qkv", self.rows, self._width, self._dtype, device)
+        q_ld = _rows(q_out, "q_out", self.rows, self._q_width, self._dtype, device)
         for g in (gq, gk):
-            if str(g.dtype) != "torch.float32" or g.device != self._device or g.numel() != self._head_dim or \
-                    not g.is_contiguous():
-                raise ValueError(f"gains must be float32 [{self._head_dim}] on {self._device}")
-        axes = 1
+            if g.shape != (d,) or not g.is_contiguous() or g.get_device() != device or not _is(g, "float32"):
+                raise ValueError(f"gains must be float32 [{d}] on GPU {device}")
+        axes, pos = 1, None
         if positions is not None:
-            if str(positions.dtype) != "torch.int32" or positions.device != self._device or positions.dim() != 2 or \
-                    positions.shape[0] != self.rows or not positions.is_contiguous():
-                raise ValueError(f"positions must be int32 [{self.rows}, axes] on {self._device}")
-            axes = positions.shape[1]
-        xc_qk_norm_rope(self.b, block, qkv, ld, gq, gk, positions, axes, theta, q_out, q_ld)
+            shape = positions.shape
+            if len(shape) != 2 or shape[0] != self.rows or not positions.is_contiguous() or \
+                    positions.get_device() != device or not _is(positions, "int32"):
+                raise ValueError(f"positions must be int32 [{self.rows}, axes] on GPU {device}")
+            axes, pos = shape[1], positions.data_ptr()
+        _check(self._norm_rope(self.b, block, qkv.data_ptr(), ld, gq.data_ptr(), gk.data_ptr(), pos, axes, theta,
+                               q_out.data_ptr(), q_ld), "xc_qk_norm_rope")
 
     def attention(self, block: int, q, out, scale: float = 0.0):
         """``q`` and ``out`` [rows, q_heads (x) head_dim]."""
         q_ld = _rows(q, "q", self.rows, self._q_width, self._dtype, self._device)
         out_ld = _rows(out, "out", self.rows, self._q_width, self._dtype, self._device)
-        xc_branch_attention(self.b, block, q, q_ld, scale, out, out_ld)
+        _check(self._attention(self.b, block, q.data_ptr(), q_ld, scale, out.data_ptr(), out_ld), "xc_branch_attention")
 
     def close(self):
         if self.b:

@@ -51,7 +51,7 @@ def plan(seqs, shared_end, group=1, kv_heads=8, D=128, elem=2, cus=256):
     lib().units(units.ctypes.data_as(ctypes.c_void_p))
     lib().info(info.ctypes.data_as(ctypes.c_void_p))
     lib().own(own.ctypes.data_as(ctypes.c_void_p))
-    return units, info[0], info[1], own, 128 if elem == 4 else 64 if info[2] else 256
+    return units, info[0], info[1], own, 32 if elem == 4 else 64 if info[2] else 256
 
 
 def check(seqs, shared_end, group, **kw):
