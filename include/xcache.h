@@ -481,7 +481,7 @@ xc_status xc_pool_compact(xc_pool* pool, int32_t* moved);
 xc_status xc_batch_init(xc_pool* pool, xc_batch** out);
 
 /* Releases a batch after its work (NULL is a no-op; synchronises the pool's
- * stream). */
+ * stream).  XC_ERR_STATE, and nothing is released, while that is captured. */
 xc_status xc_batch_destroy(xc_batch* batch);
 
 /* The rows of the batch: the last new_tokens[i] (0 to all) tokens of seqs[i]

@@ -193,6 +193,10 @@ __device__ __forceinline__ float half_probs(const f32x16& s, float scale, float 
   return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
+// The maximum before any key: a finite number, so that a score of -infinity (an
+// overflowing product) is a probability of 0 beside it and not NaN.
+constexpr float kNoMax = -3.402823466e38f;
+
 // The maximum that exponents are taken against moves only when a tile's
 // maximum exceeds it by more than this: p stays <= 2^8 in between, which
 // float sums and bf16 carry.
@@ -323,7 +327,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   for (int i = 0; i < DT + ONES; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = kNoMax, l_run = 0.f;
   bf16x8 p[2][2], ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (bf16)1.0f;
@@ -368,7 +372,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     for (int i = 0; i < PF; ++i) fr[(i0 + i) % PF] = frag(i0 + i, vt, kt);
   };
   // Probabilities of the tile against the maximum so far, which is looked for
-  // only where one of them grew past 2^kMaxSlack (first tile: from -infinity) -
+  // only where one of them grew past 2^kMaxSlack (first tile: from kNoMax) -
   // most tiles need none.  Then the tile's own maximum joins in and everything
   // so far is rescaled.  The limit is checked on the sum or, where there is
   // none, on the bf16 exponents, whose highest bit stands for 2 and more: the
@@ -573,7 +577,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
   float m_run[G], l_run[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    m_run[g] = -INFINITY;
+    m_run[g] = kNoMax;
     l_run[g] = 0.f;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -788,7 +792,7 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = kNoMax, l_run = 0.f;
   for (int i = 0; i < n; ++i) {
     XC_WAIT_VM(LOADS);  // K has landed, V may be on its way
     asm volatile("" ::: "memory");

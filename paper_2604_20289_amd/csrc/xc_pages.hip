@@ -40,7 +40,8 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // one block: a workgroup moves up to 16 KB, its loads issued together.  Bytes
 // alone (both sides of a copy are whole 16-byte chunks).
 constexpr int kCopyLoads = 4;
-__global__ __launch_bounds__(256) void page_copy_kernel(CopyArgs a, char* keys, char* values, int kv_heads,
+template <int N>
+__global__ __launch_bounds__(256) void page_copy_kernel(CopyArgs<N> a, char* keys, char* values, int kv_heads,
                                                         unsigned row_chunks, int page, long long block_bytes) {
   const PageCopy c = a.c[blockIdx.y];
   const unsigned head_chunks = page * row_chunks, seg = c.rows * row_chunks, total = kv_heads * seg;
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(256) void batch_rows_kernel(const int* __restrict__
 // A lane holds 16 bytes of one head (D / E lanes a head), so both numbers of
 // every pair are its own and the sum of squares stays within a row of lanes.
 // A wave keeps to one row: its lanes meet the same dims in every head, so the
-// angles are formed once and serve all heads.  Angles are turns (revolutions)
+// angles are formed once, a pair per lane, and serve all heads.  Angles are turns (revolutions)
 // in double - positions reach 2^31, where a float has lost the fraction - and
 // only the fraction of a turn goes on to sincospi in float.
 template <typename T, int D>
@@ -146,12 +147,15 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, int part
 #pragma unroll
   for (int i = 0; i < E / 2; ++i) c[i] = 1.f, s[i] = 0.f;
   if (a.positions != nullptr) {
+    const int pair = lane % (D / 2);
+    const int axis = pair < a.freqs.n0 ? 0 : pair < a.freqs.n0 + a.freqs.n1 ? 1 : 2;
+    const double t = (double)a.positions[(long long)row * a.freqs.axes + axis] * a.freqs.turns[pair];
+    float sv, cv;
+    sincospif(2.f * (float)(t - rint(t)), &sv, &cv);
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) {
-      const int pair = d0 / 2 + i;
-      const int axis = pair < a.freqs.n0 ? 0 : pair < a.freqs.n0 + a.freqs.n1 ? 1 : 2;
-      const double t = (double)a.positions[(long long)row * a.freqs.axes + axis] * a.freqs.turns[pair];
-      sincospif(2.f * (float)(t - rint(t)), &s[i], &c[i]);
+      c[i] = __shfl(cv, d0 / 2 + i, 64);
+      s[i] = __shfl(sv, d0 / 2 + i, 64);
     }
   }
   const int shift = a.buf.shift;
@@ -195,15 +199,28 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, int part
 
 }  // namespace
 
-hipError_t launch_page_copies(const CopyArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes,
-                              hipStream_t st) {
+namespace {
+template <int N>
+void page_copies(const PageCopy* copies, int n, const PageBuf& whole, int esz, int n_blocks, long long block_bytes,
+                 hipStream_t st) {
   const int page = 1 << whole.shift, row_chunks = whole.D * esz / 16;
+  CopyArgs<N> a;
   int most = 0;
-  for (int i = 0; i < a.n; ++i) most = a.c[i].rows > most ? a.c[i].rows : most;
+  for (int i = 0; i < n; ++i) {
+    a.c[i] = copies[i];
+    most = copies[i].rows > most ? copies[i].rows : most;
+  }
   const long long chunks = (long long)whole.kv_heads * most * row_chunks;
-  const dim3 grid((unsigned)((chunks + 256 * kCopyLoads - 1) / (256 * kCopyLoads)), a.n, 2 * n_blocks);
-  page_copy_kernel<<<grid, 256, 0, st>>>(a, (char*)whole.keys, (char*)whole.values, whole.kv_heads, row_chunks, page,
-                                         block_bytes);
+  const dim3 grid((unsigned)((chunks + 256 * kCopyLoads - 1) / (256 * kCopyLoads)), n, 2 * n_blocks);
+  page_copy_kernel<N><<<grid, 256, 0, st>>>(a, (char*)whole.keys, (char*)whole.values, whole.kv_heads, row_chunks, page,
+                                            block_bytes);
+}
+}  // namespace
+
+hipError_t launch_page_copies(const PageCopy* copies, int n, const PageBuf& whole, int esz, int n_blocks,
+                              long long block_bytes, hipStream_t st) {
+  if (n <= kCopyBatchFew) page_copies<kCopyBatchFew>(copies, n, whole, esz, n_blocks, block_bytes, st);
+  else page_copies<kCopyBatch>(copies, n, whole, esz, n_blocks, block_bytes, st);
   return hipGetLastError();
 }
 

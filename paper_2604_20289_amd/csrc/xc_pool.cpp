@@ -97,12 +97,9 @@ bool capturing(hipStream_t st) {
 }
 
 void copy_pages(Pool& p, const std::vector<PageCopy>& copies) {
-  for (size_t i = 0; i < copies.size(); i += kCopyBatch) {
-    CopyArgs a;
-    a.n = (int)std::min<size_t>(kCopyBatch, copies.size() - i);
-    std::copy(copies.begin() + i, copies.begin() + i + a.n, a.c);
-    XC_HIP(launch_page_copies(a, p.block(0), p.esz, p.cfg.n_blocks, p.block_elems() * p.esz, p.st));
-  }
+  for (size_t i = 0; i < copies.size(); i += kCopyBatch)
+    XC_HIP(launch_page_copies(copies.data() + i, (int)std::min<size_t>(kCopyBatch, copies.size() - i), p.block(0), p.esz,
+                              p.cfg.n_blocks, p.block_elems() * p.esz, p.st));
 }
 
 }  // namespace
@@ -488,6 +485,7 @@ xc_status xc_batch_init(xc_pool* pool, xc_batch** out) {
 
 xc_status xc_batch_destroy(xc_batch* b) {
   if (!b) return XC_OK;
+  if (capturing(b->p->st)) return XC_ERR_STATE;  // waiting would end the capture
   try {
     const DeviceScope scope(b->p->device);
     if (b->dev || b->pieces || b->pinned) (void)hipStreamSynchronize(b->p->st);

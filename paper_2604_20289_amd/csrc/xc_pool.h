@@ -24,13 +24,14 @@ struct PageBuf {
   int D;
 };
 
-// The most page copies of one launch: they travel in its arguments.
-constexpr int kCopyBatch = 300;
+// The most page copies of one launch: they travel in its arguments (the few of
+// a fork in a short form: the arguments of a launch are copied too).
+constexpr int kCopyBatch = 300, kCopyBatchFew = 24;
+template <int N>
 struct CopyArgs {
-  int n;
-  PageCopy c[kCopyBatch];
+  PageCopy c[N];
 };
-static_assert(sizeof(CopyArgs) <= 3800, "kernel arguments");
+static_assert(sizeof(CopyArgs<kCopyBatch>) <= 3800, "kernel arguments");
 
 // The most pages that one launch of the import fills.
 constexpr int kImportPages = 900;
@@ -91,8 +92,9 @@ struct AttnArgs {
 };
 
 
-hipError_t launch_page_copies(const CopyArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes,
-                              hipStream_t st);
+// n <= kCopyBatch copies, sources and destinations disjoint
+hipError_t launch_page_copies(const PageCopy* copies, int n, const PageBuf& whole, int esz, int n_blocks,
+                              long long block_bytes, hipStream_t st);
 hipError_t launch_import(const ImportArgs& a, const HandleWindow& w, int slot, int chunk_token, int place0, int n_tokens,
                          const PageBuf& whole, long long block_elems, hipStream_t st);
 hipError_t launch_norm_rope(int dtype, const NormRopeArgs& a, hipStream_t st);

@@ -121,7 +121,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "xc_pool_init": (i32, [P(PoolConfigC), vp, vp, vp, P(vp)]),
         "xc_pool_destroy": (i32, [vp]),
         "xc_pool_info": (i32, [vp, P(i32), P(i32), P(i32)]),
-        "xc_pool_compact": (i32, [vp, P(i32)]),
+        "xc_pool_compact": (i32, [vp, vp]),
         "xc_seq_new": (i32, [vp, P(i32)]),
         "xc_seq_fork": (i32, [vp, i32, i32, vp]),
         "xc_seq_extend": (i32, [vp, i32, vp, vp]),
@@ -339,9 +339,9 @@ def xc_seq_new(pool: int) -> int:
 
 
 def xc_seq_fork(pool: int, src: int, n: int) -> list:
-    out = _ints(bytes(4 * max(n, 1)))
+    out = _ints(bytes(4 * max(n, 0)))
     _check(load_library().xc_seq_fork(pool, src, n, _at(out)), "xc_seq_fork")
-    return out.tolist()[:max(n, 0)]
+    return out.tolist()
 
 
 def xc_seq_extend(pool: int, seqs: Sequence[int], tokens: Sequence[int]):
@@ -457,25 +457,36 @@ class Pool:
         c.n_blocks, c.n_pages, c.kv_heads, c.page_tokens, c.head_dim = keys.shape
         c.q_heads, c.dtype, c.max_seqs = q_heads, _tensor_dtype(keys), max_seqs
         self.keys, self.values, self.config = keys, values, c
+        lib = load_library()
+        self._fork, self._extend, self._free, self._compact = (lib.xc_seq_fork, lib.xc_seq_extend, lib.xc_seq_free,
+                                                               lib.xc_pool_compact)
+        self._moved = _ints([0])
         self.p = xc_pool_init(c, keys, values, stream)
 
     def new(self) -> int:
         return xc_seq_new(self.p)
 
     def fork(self, seq: int, n: int) -> list:
-        return xc_seq_fork(self.p, seq, n)
+        out = _ints(bytes(4 * max(n, 0)))
+        _check(self._fork(self.p, seq, n, _at(out)), "xc_seq_fork")
+        return out.tolist()
 
     def extend(self, seqs, tokens):
-        xc_seq_extend(self.p, seqs, tokens)
+        s, t = _ints(seqs), _ints(tokens)
+        if len(s) != len(t):
+            raise ValueError("one token count per sequence")
+        _check(self._extend(self.p, len(s), _at(s), _at(t)), "xc_seq_extend")
 
     def trim(self, seq: int, front: int = 0, back: int = 0):
         xc_seq_trim(self.p, seq, front, back)
 
     def free(self, seqs):
-        xc_seq_free(self.p, seqs)
+        s = _ints(seqs)
+        _check(self._free(self.p, len(s), _at(s)), "xc_seq_free")
 
     def compact(self) -> int:
-        return xc_pool_compact(self.p)
+        _check(self._compact(self.p, _at(self._moved)), "xc_pool_compact")
+        return self._moved[0]
 
     def pages(self, seq: int):
         return xc_seq_pages(self.p, seq)

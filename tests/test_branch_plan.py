@@ -130,6 +130,20 @@ def test_one_long_sequence_is_cut():
     assert shared == 0 and n_slots == len(units) > 16
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_which_kernel_the_tile_tests_reach(d):
+    """The shapes of tests/test_gpu_branches.py: 256 heads run in workgroups of 256 rows over 1 to 12 tiles, one head in
+    workgroups of few rows."""
+    tiles = {256: set(), 64: set()}
+    for kv, group, rows in ((1, 1, 200), (1, 1, 511), (256, 1, 65), (256, 1, 200), (256, 1, 257), (256, 4, 3), (256, 4, 40)):
+        for i, more in enumerate((0, 1, 62, 63, 64, 130, 195, 400)):
+            units, _, _, _, tile_rows = plan([(rows, (0, 1, 15, 7)[i % 4], rows + more, 0)], 0, group=group, kv_heads=kv, D=d)
+            if kv == 1 or rows * group > 64:
+                assert tile_rows == (256 if kv == 256 else 64)
+            tiles[tile_rows] |= set((-(-(units[:, 4] - (units[:, 3] & ~15)) // 64)).tolist())
+    assert tiles[256] >= set(range(1, 9)) and tiles[64] >= {1, 2, 3, 4}
+
+
 def test_no_rows_no_units():
     units, shared, n_slots, _, _ = plan([], 0)
     assert len(units) == 0 and shared == 0 and n_slots == 0

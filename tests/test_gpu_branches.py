@@ -42,7 +42,7 @@ def write(pool, seq, k, v, block=0):
     pool.values[block][p, :, r] = v.to(pool.keys)
 
 
-def check_attention(pool, batch, seqs, new, block=0, scale=0.0, seed=0, gain=1.5, q=None):
+def check_attention(pool, batch, seqs, new, block=0, scale=0.0, seed=0, gain=1.5, q=None, only=None):
     heads, d, dtype = pool.config.q_heads, pool.config.head_dim, pool.keys.dtype
     rows = sum(new)
     g = torch.Generator().manual_seed(seed)
@@ -55,9 +55,11 @@ def check_attention(pool, batch, seqs, new, block=0, scale=0.0, seed=0, gain=1.5
         if n:
             table = pool.pages(s)
             k, v = ref.gather(pool.keys, block, table), ref.gather(pool.values, block, table)
-            want, size, spread = ref.attention(q[row:row + n].double().cpu(), k, v, scale or d ** -0.5)
+            pick = list(range(heads)) if only is None else only
+            kv = [h * pool.config.kv_heads // heads for h in pick]
+            want, size, spread = ref.attention(q[row:row + n, pick].double().cpu(), k[:, kv], v[:, kv], scale or d ** -0.5)
             tol = ref.attention_bound(want, size, spread, d, len(k), dtype, ref.EPS_OF[BF16] if dtype == BF16 else 2.0 ** -24)
-            err = (got[row:row + n] - want).abs()
+            err = (got[row:row + n][:, pick] - want).abs()
             assert torch.isfinite(got[row:row + n]).all(), (s, n)
             worst = max(worst, (err / tol).max().item())
             assert (err <= tol).all(), (s, n, table[1], worst)
@@ -135,25 +137,90 @@ def test_attention_over_shared_history(case):
     print(f"[branches] {case} worst error / bound {worst:.3f}", flush=True)
 
 
-@pytest.mark.parametrize("dtype", [BF16, F32])
-def test_extreme_scores_and_values(dtype):
+@pytest.mark.parametrize("dtype,kv,d", [(BF16, 1, 64), (BF16, 256, 64), (BF16, 256, 128), (F32, 1, 64)])
+def test_extreme_scores_and_values(dtype, kv, d):
     """Scores hundreds of log2 units apart in rising, falling and mixed order (the running maximum), values near
     the type's largest, and a scale of the caller's."""
-    pool = make(dtype, pages=64, kv=1, page=16, d=64, seqs=3)
+    rows = 40 if kv == 1 else 200
+    pool = make(dtype, pages=64, kv=kv, page=16, d=d, seqs=3)
     s = pool.new()
     pool.extend([s], [500])
     g = torch.Generator().manual_seed(3)
     batch = Batch(pool)
-    batch.set([s], [40])
-    q = torch.ones(40, 1, 64)
+    batch.set([s], [rows])
+    q = torch.ones(rows, kv, d)
     for order in ("up", "down", "mixed"):
         ramp = torch.linspace(-60, 60, 500)
         ramp = {"up": ramp, "down": ramp.flip(0), "mixed": ramp[torch.randperm(500, generator=g)]}[order]
-        k = ramp[:, None, None].expand(500, 1, 64) + 0.5 * torch.randn(500, 1, 64, generator=g)
-        v = torch.randn(500, 1, 64, generator=g) * 2.0 ** 110
+        k = ramp[:, None, None].expand(500, kv, d) + 0.5 * torch.randn(500, kv, d, generator=g)
+        v = torch.randn(500, kv, d, generator=g) * 2.0 ** 110
         write(pool, s, k, v)
         for scale in (0.0, 0.03, 1.0):
-            check_attention(pool, batch, [s], [40], scale=scale, q=q.to(dtype).cuda())
+            check_attention(pool, batch, [s], [rows], scale=scale, q=q.to(dtype).cuda(), only=sorted({0, kv - 1}))
+
+
+@pytest.mark.parametrize("d,rows", [(64, 300), (128, 300), (64, 40), (128, 40)])
+def test_scores_past_the_range_of_a_float(d, rows):
+    """Keys whose product with every query overflows to -infinity, at the start, inside and at the end: weight 0; one run
+    of rising scores crosses every limit at which a running maximum moves."""
+    for dtype in (BF16, F32):
+        pool = make(dtype, pages=64, kv=1, page=16, d=d, seqs=2)
+        s = pool.new()
+        pool.extend([s], [500])
+        g = torch.Generator().manual_seed(4)
+        q = torch.full((rows, 1, d), 2.0 ** 60) * (1 + torch.rand(rows, 1, d, generator=g))
+        k = torch.randn(500, 1, d, generator=g).abs() * 2.0 ** -60 * torch.linspace(0.01, 3, 500)[:, None, None]
+        k[:130] = -2.0 ** 100
+        k[200:210] = -2.0 ** 100
+        k[499] = -2.0 ** 100
+        write(pool, s, k, torch.randn(500, 1, d, generator=g))
+        batch = Batch(pool)
+        batch.set([s], [rows])
+        q = q.to(dtype).cuda()
+        out = torch.empty_like(q)
+        batch.attention(0, q, out)
+        kk, vv = ref.gather(pool.keys, 0, pool.pages(s)), ref.gather(pool.values, 0, pool.pages(s))
+        keep = (kk[:, 0, 0] > 0)
+        want, size, spread = ref.attention(q.double().cpu(), kk[keep], vv[keep], d ** -0.5)
+        tol = ref.attention_bound(want, size, spread, d, 500, dtype, ref.EPS_OF[BF16] if dtype == BF16 else 2.0 ** -24)
+        assert ((out.double().cpu() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv,group,rows", [(1, 1, 200), (1, 1, 511), (256, 1, 65), (256, 1, 200), (256, 1, 257), (256, 4, 3),
+                                           (256, 4, 40)])
+def test_many_rows_over_every_number_of_tiles(kv, group, rows, d):
+    """One to eleven tiles of keys, ending anywhere in a tile, starting anywhere in a page; one to three workgroups of rows
+    (with 256 heads: workgroups of 256 rows, tests/test_branch_plan.py).  Three of the heads are compared."""
+    heads = sorted({0, kv * group // 2 + 1, kv * group - 1} & set(range(kv * group)))
+    for i, more in enumerate((0, 1, 62, 63, 64, 130, 195, 400)):
+        keys, drop = rows + more, (0, 1, 15, 7)[i % 4]
+        pool = make(BF16, pages=-(-(keys + 16) // 16) + 1, kv=kv, heads=kv * group, page=16, d=d, seqs=2, fill="nan")
+        s = pool.new()
+        pool.extend([s], [keys + drop])
+        pool.trim(s, front=drop)
+        g = torch.Generator().manual_seed(i)
+        write(pool, s, *torch.randn(2, keys, kv, d, generator=g))
+        batch = Batch(pool)
+        batch.set([s], [rows])
+        check_attention(pool, batch, [s], [rows], seed=i, only=heads)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 32), (F32, 64), (F32, 128)])
+def test_few_rows_over_every_number_of_tiles(dtype, d):
+    for rows in (1, 31, 32, 33, 64):
+        for i, keys in enumerate((rows, 64, 65, 97, 128, 129, 160, 256, 300, 511)):
+            pool = make(dtype, pages=40, kv=2, page=16, d=d, seqs=2, fill="nan")
+            s = pool.new()
+            drop = (0, 1, 15, 7)[i % 4]
+            keys = max(keys, rows)
+            pool.extend([s], [keys + drop])
+            pool.trim(s, front=drop)
+            g = torch.Generator().manual_seed(i)
+            write(pool, s, *torch.randn(2, keys, 2, d, generator=g))
+            batch = Batch(pool)
+            batch.set([s], [rows])
+            check_attention(pool, batch, [s], [rows], seed=i)
 
 
 def test_infinite_and_nan_tokens_stay_in_their_branch():
