@@ -385,6 +385,33 @@ def test_norm_rope_agrees_with_the_models_positions():
     assert abs(scores[0] - scores[1]) <= 4 * 2.0 ** -18 * d
 
 
+@pytest.mark.parametrize("dtype,heads,kv,d", [(BF16, 12, 6, 128), (BF16, 6, 3, 64), (F32, 3, 3, 32), (F32, 6, 2, 64),
+                                              (F32, 2, 1, 128)])
+def test_norm_rope_of_more_than_a_cache_holds(dtype, heads, kv, d):
+    """More than 256 MB in and out; 400 rows from end to end are compared, the values of all of them."""
+    row = (heads + 2 * kv) * d * (2 if dtype == BF16 else 4)
+    rows, page = (256 << 20) // (2 * row) + 17, 64
+    pool = make(dtype, pages=-(-rows // page) + 4, kv=kv, heads=heads, page=page, d=d, fill="nan")
+    s = pool.new()
+    pool.extend([s], [rows])
+    batch = Batch(pool)
+    batch.set([s], [rows])
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn(rows, heads + 2 * kv, d, generator=g, device="cuda").to(dtype)
+    gq, gk = 1 + 0.3 * torch.randn(2, d, generator=g, device="cuda")
+    pos = torch.randint(0, 10 ** 6, (rows, 3), generator=g, device="cuda").to(torch.int32)
+    q = torch.full((rows, heads, d), math.nan, dtype=dtype, device="cuda")
+    batch.qk_norm_rope(0, x, gq, gk, pos, 10000.0, q)
+    pages = torch.from_numpy(pool.pages(s)[2].astype(np.int64)).cuda()
+    keys, values = (b[0][pages].transpose(1, 2).reshape(-1, kv, d)[:rows] for b in (pool.keys, pool.values))
+    assert torch.equal(values, x[:, heads + kv:]) and torch.isfinite(keys).all() and torch.isfinite(q).all()
+    at = torch.linspace(0, rows - 1, 400, device="cuda").long()
+    some = x[at].double().cpu()
+    for got, src, gain in ((q, some[:, :heads], gq), (keys, some[:, heads:heads + kv], gk)):
+        want, tol = ref.norm_rope(src, gain.double().cpu(), pos[at].cpu(), 10000.0, dtype)
+        assert ((got[at].double().cpu() - want).abs() <= tol).all()
+
+
 # ---------------------------------------------------------------- pages
 
 @pytest.mark.parametrize("dtype,blocks,kv,d,page", [(BF16, 1, 1, 64, 16), (BF16, 3, 4, 128, 64), (F32, 2, 3, 32, 256),
@@ -425,6 +452,22 @@ def test_page_copies(dtype, blocks, kv, d, page):
         new = old.clone()
         new[:, dst] = old[:, src]
         assert torch.equal(buf, new)
+
+
+def test_copies_of_more_than_a_cache_holds():
+    """80 branches, each with its own copy of the last page they share, 255 tokens of it: 2 x 196 MB."""
+    pool = make(BF16, blocks=2, pages=84, kv=9, page=256, d=128, seqs=82)
+    parent = pool.new()
+    pool.extend([parent], [255])
+    old = int(pool.pages(parent)[2][0])
+    keys, values = pool.keys.clone(), pool.values.clone()
+    kids = pool.fork(parent, 80)
+    pool.extend(kids, [1] * 80)
+    to = torch.tensor([int(pool.pages(k)[2][0]) for k in kids])
+    assert old not in to and len(set(to.tolist())) == 80
+    for buf, was in ((pool.keys, keys), (pool.values, values)):
+        was[:, to, :, :255] = was[:, old:old + 1, :, :255]
+        assert torch.equal(buf, was)
 
 
 def test_many_copies_in_one_call():
