@@ -39,7 +39,6 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kXcds = 8;  // each has its own L2
 constexpr int kWaves = 8;
 
 // MFMA row R of a 32-key half tile -> key offset within the 64-key tile
@@ -72,18 +71,6 @@ __device__ __forceinline__ float partner_max(float x) {
 __device__ __forceinline__ float partner_sum(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// (unit, key head) of a workgroup: heads outermost, dealt to the XCDs in
-// contiguous ranges, so that the workgroups of one XCD read the same keys
-__device__ __forceinline__ bool unit_of(const AttnArgs& a, int& u, int& h) {
-  const int total = a.n_units * a.buf.kv_heads;
-  const int per_xcd = (total + kXcds - 1) / kXcds;
-  const int i = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
-  if ((int)(blockIdx.x / kXcds) >= per_xcd || i >= total) return false;
-  h = i / a.n_units;
-  u = i - h * a.n_units;
-  return true;
 }
 
 // Where a query row's results go.
@@ -234,7 +221,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   __shared__ __attribute__((aligned(1024))) char sV2[SLOT];
   __shared__ __attribute__((aligned(1024))) char sV3[SLOT];
   int u, h;
-  if (!unit_of(a, u, h)) return;
+  if (!xcd_pair(blockIdx.x, a.n_units, a.buf.kv_heads, u, h)) return;
   const AttnUnit un = a.units[u];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hi = lane >> 5, lo = lane & 31;
@@ -1006,7 +993,7 @@ __global__ __launch_bounds__(256) void branch_merge_few_kernel(AttnArgs a) {
 hipError_t launch_branch_attention(int dtype, const AttnArgs& a, hipStream_t st) {
   const int total = a.n_units * a.buf.kv_heads, D = a.buf.D;
   if (total == 0) return hipSuccess;
-  const int grid = (total + kXcds - 1) / kXcds * kXcds;
+  const unsigned grid = (unsigned)xcd_grid(a.n_units, a.buf.kv_heads);
   if (dtype == 1) {
     if (a.few) {
       if (D == 128) branch_few_kernel<128><<<total, 256, 0, st>>>(a);

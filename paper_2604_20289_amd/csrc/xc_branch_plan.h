@@ -49,6 +49,7 @@ struct AttnPlan {
 };
 
 constexpr int kPlanMaxSlots = 96;
+constexpr int kXcds = 8;  // each has its own L2
 constexpr long long kPlanMaxPieceBytes = 1ll << 30;
 
 namespace plan_detail {
@@ -211,10 +212,37 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
     if (best_packed || n > 1) best.n_slots = std::max(best.n_slots, best.shared_slots + n);
     tok0 += q.rows;
   }
-  if (best.few || sh.elem == 4)
-    std::stable_sort(best.units.begin(), best.units.end(),
-                     [](const AttnUnit& x, const AttnUnit& y) { return x.hi - x.lo > y.hi - y.lo; });
+  // the long ones first: what begins last is short
+  std::stable_sort(best.units.begin(), best.units.end(),
+                   [](const AttnUnit& x, const AttnUnit& y) { return x.hi - x.lo > y.hi - y.lo; });
   return best;
+}
+
+// The (key head, unit) pairs of the wide kernel, dealt to the XCDs so that the
+// workgroups that run on one of them read the same keys and all have a like
+// mixture of long and short ones: the heads in runs, a run to `sharers` XCDs,
+// its pairs (heads outermost) to these in turn.  (Runs of pairs as they come,
+// where one XCD may get the long ones and the next the short: 63 us instead of
+// 50 for 4 heads with 54 long units each and 24 short ones.)
+struct XcdDeal {
+  int sharers, run;  // XCDs of a run of heads, heads of a run
+};
+constexpr XcdDeal xcd_deal(int kv_heads) {
+  const int runs = (kv_heads & -kv_heads) < kXcds ? (kv_heads & -kv_heads) : kXcds;
+  return {kXcds / runs, kv_heads / runs};
+}
+inline long long xcd_grid(long long n_units, int kv_heads) {
+  const XcdDeal d = xcd_deal(kv_heads);
+  return (d.run * n_units + d.sharers - 1) / d.sharers * kXcds;
+}
+// workgroup -> pair; false: none
+constexpr bool xcd_pair(int workgroup, int n_units, int kv_heads, int& u, int& h) {
+  const XcdDeal d = xcd_deal(kv_heads);
+  const int x = workgroup % kXcds, i = workgroup / kXcds * d.sharers + x % d.sharers;
+  if (i >= d.run * n_units) return false;
+  h = x / d.sharers * d.run + i / n_units;
+  u = i % n_units;
+  return true;
 }
 
 }  // namespace xc

@@ -242,7 +242,9 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const int group = p.cfg.q_heads / p.cfg.kv_heads;
   const PlanShape shape{group, p.cfg.kv_heads, p.cfg.head_dim, p.esz, p.cus};
   const AttnPlan plan = plan_attention(plan_seqs, (int)(shared << shift), shape);
-  if ((long long)plan.units.size() * p.cfg.kv_heads > INT32_MAX / 2) return XC_ERR_UNSUPPORTED;
+  const long long threads = std::max(((long long)plan.units.size() * p.cfg.kv_heads + kXcds * kXcds) * 512,
+                                     plan.n_slots ? rows * p.cfg.q_heads * (p.cfg.head_dim / 4) : 0);
+  if (threads >> 32) return XC_ERR_UNSUPPORTED;  // more than a launch takes
   for (size_t i = 0; i < batch_seqs.size(); ++i) batch_seqs[i].own = plan.own[i];
 
   // uploaded: tables, sequences, units; written on the device: places, own slots

@@ -26,6 +26,11 @@ int make(int n, const int* seqs, int shared_end, int group, int kv_heads, int D,
 }
 void info(int* out) { out[0] = plan.shared_slots, out[1] = plan.n_slots, out[2] = plan.few; }
 void units(int* out) { for (auto& u : plan.units) for (int v : {u.tok0, u.tokens, u.table, u.lo, u.hi, u.slot}) *out++ = v; }
+int grid(int units, int heads) { return (int)xcd_grid(units, heads); }
+int pair(int wg, int units, int heads) {
+  int u = -1, h = -1;
+  return xcd_pair(wg, units, heads, u, h) ? h * units + u : -1;
+}
 void own(int* out) { for (auto& o : plan.own) *out++ = o.first, *out++ = o.n; }
 }
 """
@@ -105,6 +110,20 @@ def test_every_row_meets_every_key_once(seed):
         shared_end = 0
     check(seqs, shared_end, rng.choice([1, 2, 3, 5, 12]), kv_heads=rng.choice([1, 4, 12]),
           D=rng.choice([64, 128]), elem=rng.choice([2, 4]), cus=256)
+
+
+@pytest.mark.parametrize("heads", [1, 2, 3, 4, 5, 8, 12, 24, 31, 256])
+@pytest.mark.parametrize("units", [1, 2, 7, 8, 60, 333])
+def test_every_pair_has_one_workgroup(units, heads):
+    """Each (head, unit) once; an XCD (workgroup number modulo 8) has its share of every unit, and few heads."""
+    grid = lib().grid(units, heads)
+    pairs = np.array([lib().pair(w, units, heads) for w in range(grid)])
+    assert sorted(pairs[pairs >= 0]) == list(range(units * heads))
+    assert grid % 8 == 0 and grid - units * heads < 64
+    for x in range(8):
+        mine = pairs[x::8][pairs[x::8] >= 0]
+        assert (np.diff(mine) > 0).all()  # heads outermost
+        assert len(set(mine // units)) <= max(1, heads // min(heads & -heads, 8))
 
 
 def test_single_tokens_share_their_history():
