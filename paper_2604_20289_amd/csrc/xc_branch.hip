@@ -200,6 +200,16 @@ constexpr float kMaxSlack = 8.0f, kMaxP = 256.0f;
 // of tile j, where the wave has issue slots to spare, and has landed three
 // phases later at the earliest it may be read; the slot it goes to was last
 // read by tile j - 1.
+//
+// Bound by the two phases: at d = 128 about 1150 cycles of softmax and 1430 of
+// products, at d = 64 about 940 and 900, where the products alone are 1024
+// and 640; a clock of 1.5 to 1.8 GHz is what the chip's power leaves with all
+// CUs at it.  28080 rows, 21060 keys, 12 heads of 128: 3.4 ms, 1070 TFLOP/s;
+// 6144 rows, 2304 keys, 8 heads of 64: 42 us, 690 TFLOP/s.  The former with
+// other choices: the matrix phase without a raised wave priority 3760 us
+// instead of 3440, the softmax raised instead 4010; the softmax not held before
+// its barrier 3800; a maximum per tile 3440 instead of 3330 (51 us instead of 45
+// for the latter).
 template <int D>
 __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a) {
   using F = Frags<D>;
@@ -490,6 +500,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
 // of LDS: two workgroups, eight waves per CU, 128 KB in flight.  Two groups read
 // their queries from LDS in every tile: with two output accumulators there
 // are no registers for them.
+//
+// Bound by reading keys and values: 16 rows over 14200 keys, 12 heads of 128
+// (101 MB) 27 us with the merge, 64 rows over 36600 keys, 16 heads of 128
+// (559 MB) 125 us, 4.5 TB/s (141 us as two workgroups of one row group each).
 template <int D>
 struct FewShape {
   static constexpr int HT = 128 / D;                  // 32-key halves of a tile
@@ -884,7 +898,8 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
 // A wave owns one of them.  It is a chain of memory latencies, so what is
 // independent is in flight together: all statistics (a lane per piece), then
 // the outputs, each of 64 / (D / 4) lane groups taking every so many pieces,
-// four at a time.  Every sum has a fixed order.
+// four at a time.  Every sum has a fixed order.  4 to 5 us for 192 rows of 15
+// pieces and for 1024 of 13.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
   constexpr int LPH = D / 4, NG = 64 / LPH, U = 4;
@@ -1010,7 +1025,8 @@ hipError_t launch_branch_attention(int dtype, const AttnArgs& a, hipStream_t st)
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_slots == 0) return e;
   // a wave per (row, head), or one of its lane groups where few pieces join.
-  // MERGE_TIMES
+  // 18096 of them with 3 pieces, d = 64: 48.3 us for the call, 50.7 with a wave
+  // each; 1024 with 13 pieces need a wave each (no group could hold them).
   const bool few_pieces = a.n_slots <= kFewPieces;
   const long long rq = (long long)a.rows * a.q_heads, per = few_pieces ? 256 / (D / 4) : 4;
   const unsigned mg = (unsigned)((rq + per - 1) / per);
