@@ -109,27 +109,34 @@ struct TableWindow {
   }
 };
 
-// Rows of 8 sixteen-byte chunks in LDS, 1 KB blocks of 8 rows.  K: row r,
-// chunk c at ((c % 8) ^ (r / 8 % 2)) * 8 + r % 8: the 16 rows that a quarter
-// wave reads at one chunk fall into 16 bank groups.  V: (r / 4 % 2 * 8 + c) * 4
-// + r % 4: the 4 rows x 4 chunks that half a wave of a transposing read takes
-// are 256 contiguous bytes.  KCG blocks per 8 rows of D columns.
+// Rows of 8 sixteen-byte chunks in LDS, 1 KB blocks of 8 rows; 8 lanes of a
+// request fetch 128 contiguous bytes.  K: row r, chunk c at (r % 8 ^ r / 8 % 2)
+// * 8 + (c ^ r % 8): the 16 rows that a quarter wave reads at one chunk fall
+// into 16 bank groups.  V: r % 8 * 8 + (c ^ r / 2 % 2 * 4): so do the 4 rows x 4
+// chunks that half a wave of a transposing read takes.  KCG blocks per 8 rows
+// of D columns.
 template <int D>
 struct Frags {
   static constexpr int KCG = D / 64, DT = D / 32, KS = D / 16;
-  int k_off, v_off;
+  int k_off[4], v_off[2];
   __device__ __forceinline__ explicit Frags(int lane) {
     const int hi = lane >> 5, lo = lane & 31;
-    k_off = (lo >> 3) * KCG * 1024 + (hi ^ ((lo >> 3) & 1)) * 128 + (lo & 7) * 16;
-    v_off = hi * KCG * 1024 + (((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) * 64 + ((lane >> 2) & 3) * 16 + (lane & 1) * 8;
+    const int row = (lane >> 2) & 3;  // of a transposing read
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      k_off[i] = (lo >> 3) * KCG * 1024 + ((lo & 7) ^ ((lo >> 3) & 1)) * 128 + ((2 * i + hi) ^ (lo & 7)) * 16;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      v_off[i] = hi * KCG * 1024 + row * 128 + (i ^ (row >> 1)) * 64 + (((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) * 16 +
+                 (lane & 1) * 8;
   }
   // keys of half tile mt, head dims ks * 16 + hi * 8 ..
   __device__ __forceinline__ bf16x8 k(const char* tile, int mt, int ks) const {
-    return *reinterpret_cast<const bf16x8*>(tile + k_off + mt * 4 * KCG * 1024 + (ks >> 2) * 1024 + (ks & 3) * 256);
+    return *reinterpret_cast<const bf16x8*>(tile + k_off[ks & 3] + mt * 4 * KCG * 1024 + (ks >> 2) * 1024);
   }
   // head dim dt * 32 + lo, keys kv * 16 + hi * 8 ..
   __device__ __forceinline__ bf16x8 v(const char* tile, int kv, int dt) const {
-    const char* p = tile + v_off + kv * 2 * KCG * 1024 + (dt >> 1) * 1024 + (dt & 1) * 256;
+    const char* p = tile + v_off[dt & 1] + kv * 2 * KCG * 1024 + (dt >> 1) * 1024;
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
     const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 512));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -139,12 +146,12 @@ struct Frags {
 // A block's row and column bytes that lane `lane` fetches: block (rg, cg) of a
 // K or a V tile.
 __device__ __forceinline__ int k_block_row(int rg, int lane) {
-  const int R = rg * 8 + (lane & 7);
+  const int R = rg * 8 + ((lane >> 3) ^ (rg & 1));
   return key_of_row(R >> 5, R & 31);
 }
-__device__ __forceinline__ unsigned k_block_col(int rg, int cg, int lane) { return (cg * 8 + ((lane >> 3) ^ (rg & 1))) * 16; }
-__device__ __forceinline__ int v_block_row(int rg, int lane) { return rg * 8 + (lane >> 5) * 4 + (lane & 3); }
-__device__ __forceinline__ unsigned v_block_col(int cg, int lane) { return (cg * 8 + ((lane >> 2) & 7)) * 16; }
+__device__ __forceinline__ unsigned k_block_col(int rg, int cg, int lane) { return (cg * 8 + ((lane & 7) ^ (lane >> 3) ^ (rg & 1))) * 16; }
+__device__ __forceinline__ int v_block_row(int rg, int lane) { return rg * 8 + (lane >> 3); }
+__device__ __forceinline__ unsigned v_block_col(int cg, int lane) { return (cg * 8 + ((lane & 7) ^ (((lane >> 4) & 1) << 2))) * 16; }
 
 // The address of a unit's query row r, head dims hi * 8 on.
 __device__ __forceinline__ const bf16* query_row(const AttnArgs& a, const AttnUnit& un, int h, int r, int hi) {
