@@ -81,7 +81,7 @@ __device__ __forceinline__ RowOut row_out(const AttnArgs& a, const AttnUnit& un,
   const int t = un.tok0 + r / a.group, qh = h * a.group + r % a.group;
   RowOut o;
   o.out = (long long)t * a.out_ld + qh * a.buf.D;
-  o.stat = ((long long)un.slot * a.rows + t) * a.q_heads + qh;
+  o.stat = ((long long)un.slot * a.piece_rows + t - a.piece_row0) * a.q_heads + qh;
   o.piece = o.stat * a.buf.D;
   return o;
 }
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   __shared__ __attribute__((aligned(1024))) char sV2[SLOT];
   __shared__ __attribute__((aligned(1024))) char sV3[SLOT];
   int u, h;
-  if (!xcd_pair(blockIdx.x, a.n_units, a.buf.kv_heads, u, h)) return;
+  if (!xcd_pair(blockIdx.x, a.n_units, a.n_long, a.buf.kv_heads, u, h)) return;
   const AttnUnit un = a.units[u];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hi = lane >> 5, lo = lane & 31;
@@ -914,9 +914,9 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
   constexpr int LPH = D / 4, NG = 64 / LPH, U = 4;
   const int lane = threadIdx.x & 63, g = lane / LPH, d0 = lane % LPH * 4;
   const long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long rq = (long long)a.rows * a.q_heads;
+  const long long rq = (long long)a.piece_rows * a.q_heads;
   if (i >= rq) return;
-  const int t = (int)(i / a.q_heads);
+  const int t = a.piece_row0 + (int)(i / a.q_heads);
   const OwnSlots own = a.own[t];
   const int n = a.shared_slots + own.n;
   if (n == 0) return;  // written by its only unit
@@ -958,7 +958,7 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
   if (g != 0) return;
-  T* out = reinterpret_cast<T*>(a.out) + t * a.out_ld + (i - (long long)t * a.q_heads) * D + d0;
+  T* out = reinterpret_cast<T*>(a.out) + t * a.out_ld + (i % a.q_heads) * D + d0;
   const float inv = 1.0f / den;
 #pragma unroll
   for (int e = 0; e < 4; ++e) out[e] = (T)(acc[e] * inv);
@@ -972,9 +972,9 @@ __global__ __launch_bounds__(256) void branch_merge_few_kernel(AttnArgs a) {
   constexpr int LPH = D / 4;
   const long long i = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH;
   const int d0 = threadIdx.x % LPH * 4;
-  const long long rq = (long long)a.rows * a.q_heads;
+  const long long rq = (long long)a.piece_rows * a.q_heads;
   if (i >= rq) return;
-  const int t = (int)(i / a.q_heads);
+  const int t = a.piece_row0 + (int)(i / a.q_heads);
   const OwnSlots own = a.own[t];
   const int n = a.shared_slots + own.n;
   if (n == 0) return;  // written by its only unit
@@ -1006,7 +1006,7 @@ __global__ __launch_bounds__(256) void branch_merge_few_kernel(AttnArgs a) {
   vec v;
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = (T)(acc[e] * inv);
-  *reinterpret_cast<vec*>(reinterpret_cast<T*>(a.out) + t * a.out_ld + (i - (long long)t * a.q_heads) * D + d0) = v;
+  *reinterpret_cast<vec*>(reinterpret_cast<T*>(a.out) + t * a.out_ld + (i % a.q_heads) * D + d0) = v;
 }
 
 }  // namespace
@@ -1037,7 +1037,7 @@ hipError_t launch_branch_attention(int dtype, const AttnArgs& a, hipStream_t st)
   // 18096 of them with 3 pieces, d = 64: 48.3 us for the call, 50.7 with a wave
   // each; 1024 with 13 pieces need a wave each (no group could hold them).
   const bool few_pieces = a.n_slots <= kFewPieces;
-  const long long rq = (long long)a.rows * a.q_heads, per = few_pieces ? 256 / (D / 4) : 4;
+  const long long rq = (long long)a.piece_rows * a.q_heads, per = few_pieces ? 256 / (D / 4) : 4;
   const unsigned mg = (unsigned)((rq + per - 1) / per);
 #define XC_MERGE(T, DD)                                                     \
   do {                                                                      \

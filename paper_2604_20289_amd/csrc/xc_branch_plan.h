@@ -40,9 +40,16 @@ struct OwnSlots {
   int first, n;
 };
 
+// Batch rows tok0 .. of one sequence whose own pieces are in the same slots.
+struct PlanPart {
+  int seq, tok0, rows;
+  OwnSlots own;
+};
+
 struct AttnPlan {
   std::vector<AttnUnit> units;
-  std::vector<OwnSlots> own;  // per sequence: the slots of its own pieces
+  std::vector<PlanPart> parts;  // all rows, in order
+  int piece_row0 = 0;           // the first row that has pieces
   int shared_slots = 0;       // slots 0 .. shared_slots - 1: pieces of the shared history, of every row
   int n_slots = 0;            // 0: no row has pieces
   bool few = false;           // bf16: units for branch_few_kernel
@@ -90,6 +97,13 @@ constexpr Kernel kWide{kWideRows, false, {1.3, 0.9, 0}, 5.0, 1, {0.7, 1.0, 0}},
 constexpr double kHbmBytesPerUs = 6.0e6;
 // the merge's launch, and its pieces written and read
 constexpr double kMergeUs = 5.0, kPieceBytesPerUs = 1.0e6;
+
+// of `rows` rows in blocks of `per`, those of the last `left` blocks; `left` less these
+inline long long tail_of(long long rows, int per, long long& left) {
+  const long long blocks = cdiv(rows, per), mine = std::min(blocks, left);
+  left -= mine;
+  return mine == blocks ? rows : mine == 0 ? 0 : rows - (blocks - mine) * per;
+}
 
 // Time of workgroups on `places` places, the long ones first, each advancing
 // by at most 1 us per us and all together by at most `crowd`: equal shares
@@ -143,13 +157,14 @@ struct Work {
 // over its history and its own keys in one go: a sequence whose rows fill
 // workgroups by themselves gains nothing by packing.  Either way a long run of
 // keys is cut into pieces of about `c` tiles, so that few rows still fill the
-// chip.  The cheaper of all by the times above is taken.
+// chip.  Workgroups that are whole but leave a last round partly filled have
+// the keys of just the last rows cut, as many as that round holds.  The
+// cheapest of all by the times above is taken.
 inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end, const PlanShape& sh) {
   using namespace plan_detail;
   long long rows = 0;
   for (const PlanSeq& q : seqs) rows += q.rows;
   AttnPlan best;
-  best.own.assign(seqs.size(), {0, 0});
   if (rows == 0) return best;
   const PlanSeq* head = nullptr;  // any sequence with rows: the shared places are in all of them
   for (const PlanSeq& q : seqs)
@@ -159,7 +174,7 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
   auto slots_of = [](int tiles, int c) { return tiles ? (int)cdiv(tiles, c) : 0; };
   double best_us = 0;
   bool have = false, best_packed = false;
-  int best_c = 0, per = 0;
+  int best_c = 0, best_tail = 0, best_tail_pieces = 1, per = 0;
   static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128, 192, 256, 512, 1024, 1 << 26};
   std::vector<Kernel> kernels{sh.elem == 4 ? kF32 : kWide};
   if (sh.elem == 2 && sh.group <= kFewRows) kernels.push_back(kFew);
@@ -171,18 +186,18 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
         Work w;
         int shared = 0, most = 0;
         double read = 0;
-        auto add = [&](long long r, int lo, int hi) {
+        auto add = [&](long long r, int lo, int hi, int c) {
           const int tiles = tiles_of(lo, hi), s = slots_of(tiles, c);
           if (s == 0) return 0;
           w.add(cdiv(r, kper) * s * sh.kv_heads, (double)tiles / s * k.tile[dim] * (k.few && std::min<long long>(r, kper) * sh.group > 32 ? 1.25 : 1.0) + k.start);
           read += 2.0 * (hi - lo) * sh.D * sh.elem * sh.kv_heads;
           return s;
         };
-        if (packed) shared = add(rows, head->first, shared_end);
+        if (packed) shared = add(rows, head->first, shared_end, c);
         bool direct = !packed;
         for (const PlanSeq& q : seqs) {
           if (q.rows == 0) continue;
-          const int s = add(q.rows, packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens);
+          const int s = add(q.rows, packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens, c);
           most = std::max(most, s);
           if (s > 1) direct = false;
         }
@@ -190,28 +205,69 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
         if (slots > kPlanMaxSlots || (slots > 2 && slots * piece_bytes > (double)kPlanMaxPieceBytes)) continue;
         const double us = std::max(w.us((long long)k.per_cu * sh.cus, k.crowd[dim] * sh.cus), read / kHbmBytesPerUs) +
                           (slots ? kMergeUs + slots * piece_bytes / kPieceBytesPerUs : 0);
-        if (!have || us < best_us) have = true, best_us = us, best_packed = packed != 0, best_c = c, per = kper, best.few = k.few;
+        if (!have || us < best_us)
+          have = true, best_us = us, best_packed = packed != 0, best_c = c, best_tail = 0, per = kper, best.few = k.few;
+
+        // the last blocks of rows, those past the last full round, in pieces
+        if (!direct || c != kCuts[sizeof kCuts / sizeof *kCuts - 1]) continue;
+        long long blocks = 0;
+        for (const PlanSeq& q : seqs) blocks += cdiv(q.rows, kper);
+        const long long places = (long long)k.per_cu * sh.cus, over = blocks * sh.kv_heads % places;
+        if (blocks * sh.kv_heads <= places || over == 0) continue;
+        for (int more = 0; more < 2; ++more)
+          for (int pieces : {2, 3, 4, 6, 8}) {
+            const long long tail = cdiv(over, sh.kv_heads) + more;
+            if (tail >= blocks) continue;
+            w.kinds.clear();
+            read = 0;
+            long long left = tail, tail_rows = 0;
+            for (size_t i = seqs.size(); i-- > 0;) {
+              const PlanSeq& q = seqs[i];
+              const long long r = tail_of(q.rows, kper, left);
+              add(q.rows - r, q.first, q.first + q.tokens, c);
+              add(r, q.first, q.first + q.tokens, (int)cdiv(tiles_of(q.first, q.first + q.tokens), pieces));
+              tail_rows += r;
+            }
+            const double bytes = (double)pieces * tail_rows / rows * piece_bytes;
+            if (bytes > (double)kPlanMaxPieceBytes) continue;
+            const double t = std::max(w.us(places, k.crowd[dim] * sh.cus), read / kHbmBytesPerUs) + kMergeUs + bytes / kPieceBytesPerUs;
+            if (t < best_us)
+              best_us = t, best_packed = false, best_c = c, best_tail = (int)tail, best_tail_pieces = pieces, per = kper, best.few = k.few;
+          }
       }
 
-  auto emit = [&](const PlanSeq& q, int tok0, long long r, int lo, int hi, int slot0, bool direct) {
-    const int n = slots_of(tiles_of(lo, hi), best_c);
+  auto emit = [&](const PlanSeq& q, int tok0, long long r, int lo, int hi, int slot0, bool direct, int c) {
+    const int n = slots_of(tiles_of(lo, hi), c);
     for (int i = 0; i < n; ++i)
       for (long long t = 0; t < r; t += per)
         best.units.push_back({tok0 + (int)t, (int)std::min<long long>(per, r - t), q.table, cut(lo, hi, n, i),
                               cut(lo, hi, n, i + 1), direct && n == 1 ? -1 : slot0 + i});
     return n;
   };
-  if (best_packed) best.shared_slots = best.n_slots = emit(*head, 0, rows, head->first, shared_end, 0, false);
+  if (best_packed) best.shared_slots = best.n_slots = emit(*head, 0, rows, head->first, shared_end, 0, false, best_c);
+  // the rows that are cut otherwise, from the last sequence backwards
+  std::vector<int> tails(seqs.size());
+  long long left = best_tail;
+  for (size_t i = seqs.size(); i-- > 0;) tails[i] = (int)tail_of(seqs[i].rows, per, left);
+  best.piece_row0 = -1;
   int tok0 = 0;
   for (size_t i = 0; i < seqs.size(); ++i) {
     const PlanSeq& q = seqs[i];
-    if (q.rows == 0) continue;
-    const int n = emit(q, tok0, q.rows, best_packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens,
-                       best.shared_slots, !best_packed);
-    best.own[i] = {best.shared_slots, !best_packed && n == 1 ? 0 : n};
-    if (best_packed || n > 1) best.n_slots = std::max(best.n_slots, best.shared_slots + n);
-    tok0 += q.rows;
+    for (const bool tail : {false, true}) {
+      const int r = tail ? tails[i] : q.rows - tails[i];
+      if (r == 0) continue;
+      const int lo = best_packed ? std::max(shared_end, q.first) : q.first, hi = q.first + q.tokens;
+      const int c = tail ? (int)cdiv(tiles_of(lo, hi), best_tail_pieces) : best_c;
+      const int n = emit(q, tok0, r, lo, hi, best.shared_slots, !best_packed, c);
+      best.parts.push_back({(int)i, tok0, r, {best.shared_slots, !best_packed && n == 1 ? 0 : n}});
+      if (best_packed || n > 1) {
+        best.n_slots = std::max(best.n_slots, best.shared_slots + n);
+        if (best.piece_row0 < 0) best.piece_row0 = tok0;
+      }
+      tok0 += r;
+    }
   }
+  best.piece_row0 = std::max(best.piece_row0, 0);
   // the long ones first: what begins last is short
   std::stable_sort(best.units.begin(), best.units.end(),
                    [](const AttnUnit& x, const AttnUnit& y) { return x.hi - x.lo > y.hi - y.lo; });
@@ -221,7 +277,10 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
 // The (key head, unit) pairs of the wide kernel, dealt to the XCDs so that the
 // workgroups that run on one of them read the same keys and all have a like
 // mixture of long and short ones: the heads in runs, a run to `sharers` XCDs,
-// its pairs (heads outermost) to these in turn.  (Runs of pairs as they come,
+// its pairs to these in turn: first the units of over half the longest one's
+// length, then the others, either heads outermost.  (With all units of a head
+// together, the long ones of the last head began late: 550 tiles' time
+// instead of 440 for 28 blocks of 12 heads, 21 of them whole and 7 in thirds.  Runs of pairs as they come,
 // where one XCD may get the long ones and the next the short: 63 us instead of
 // 50 for 4 heads with 54 long units each and 24 short ones.)
 struct XcdDeal {
@@ -231,17 +290,23 @@ constexpr XcdDeal xcd_deal(int kv_heads) {
   const int runs = (kv_heads & -kv_heads) < kXcds ? (kv_heads & -kv_heads) : kXcds;
   return {kXcds / runs, kv_heads / runs};
 }
+inline int long_units(const std::vector<AttnUnit>& units) {  // sorted
+  int n = 0;
+  while (n < (int)units.size() && units[n].hi - units[n].lo > (units[0].hi - units[0].lo) / 2) ++n;
+  return n;
+}
 inline long long xcd_grid(long long n_units, int kv_heads) {
   const XcdDeal d = xcd_deal(kv_heads);
   return (d.run * n_units + d.sharers - 1) / d.sharers * kXcds;
 }
 // workgroup -> pair; false: none
-constexpr bool xcd_pair(int workgroup, int n_units, int kv_heads, int& u, int& h) {
+constexpr bool xcd_pair(int workgroup, int n_units, int n_long, int kv_heads, int& u, int& h) {
   const XcdDeal d = xcd_deal(kv_heads);
   const int x = workgroup % kXcds, i = workgroup / kXcds * d.sharers + x % d.sharers;
   if (i >= d.run * n_units) return false;
-  h = x / d.sharers * d.run + i / n_units;
-  u = i % n_units;
+  const int first = d.run * n_long, n = i < first ? n_long : n_units - n_long, k = i < first ? i : i - first;
+  h = x / d.sharers * d.run + k / n;
+  u = (i < first ? 0 : n_long) + k % n;
   return true;
 }
 

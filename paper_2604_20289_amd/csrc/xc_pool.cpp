@@ -224,7 +224,7 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
 
   std::vector<PlanSeq> plan_seqs;
   std::vector<BatchSeq> batch_seqs;
-  std::vector<int> tables, written;
+  std::vector<int> tables, written, first_row;
   std::vector<uint64_t> versions(n);
   int row0 = 0;
   for (int i = 0; i < n; ++i) {
@@ -233,7 +233,7 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     if (new_tokens[i] == 0) continue;
     const int at = q.first + q.tokens - new_tokens[i];
     plan_seqs.push_back({new_tokens[i], q.first, q.tokens, (int)tables.size()});
-    batch_seqs.push_back({row0, at, (int)tables.size(), {0, 0}});
+    first_row.push_back(row0);
     tables.insert(tables.end(), q.pages.begin(), q.pages.end());
     written.insert(written.end(), q.pages.begin() + (at >> shift), q.pages.end());
     row0 += new_tokens[i];
@@ -245,7 +245,11 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const long long threads = std::max(((long long)plan.units.size() * p.cfg.kv_heads + kXcds * kXcds) * 512,
                                      plan.n_slots ? rows * p.cfg.q_heads * (p.cfg.head_dim / 4) : 0);
   if (threads >> 32) return XC_ERR_UNSUPPORTED;  // more than a launch takes
-  for (size_t i = 0; i < batch_seqs.size(); ++i) batch_seqs[i].own = plan.own[i];
+  for (const PlanPart& part : plan.parts) {
+    const PlanSeq& q = plan_seqs[part.seq];
+    const int at = q.first + q.tokens - q.rows + (part.tok0 - first_row[part.seq]);
+    batch_seqs.push_back({part.tok0, at, q.table, part.own});
+  }
 
   // uploaded: tables, sequences, units; written on the device: places, own slots
   const size_t o_seqs = align256(tables.size() * sizeof(int));
@@ -253,7 +257,8 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const size_t up = o_units + align256(plan.units.size() * sizeof(AttnUnit));
   const size_t o_own = up + align256(rows * sizeof(int));
   const size_t need = o_own + align256(rows * sizeof(OwnSlots));
-  const size_t stat_rows = (size_t)plan.n_slots * rows * p.cfg.q_heads;
+  const long long piece_rows = rows - plan.piece_row0;
+  const size_t stat_rows = (size_t)plan.n_slots * piece_rows * p.cfg.q_heads;
   const size_t o_stats = align256(stat_rows * p.cfg.head_dim * sizeof(float));
   const size_t piece_need = plan.n_slots ? o_stats + stat_rows * sizeof(float2) : 0;
   std::vector<int> seq_copy(seqs, seqs + n);
@@ -302,6 +307,7 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   a.tables = (const int*)b->dev;
   a.units = (const AttnUnit*)(b->dev + o_units);
   a.n_units = (int)plan.units.size();
+  a.n_long = long_units(plan.units);
   a.group = group;
   a.pieces = (float*)b->pieces;
   a.stats = (float2*)(b->pieces + o_stats);
@@ -310,6 +316,8 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   a.rows = (int)rows;
   a.q_heads = p.cfg.q_heads;
   a.n_slots = plan.n_slots;
+  a.piece_row0 = plan.piece_row0;
+  a.piece_rows = (int)piece_rows;
   a.few = plan.few;
   b->place = (const int*)(b->dev + up);
   b->rows = (int)rows;

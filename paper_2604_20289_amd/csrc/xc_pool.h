@@ -80,13 +80,15 @@ struct AttnArgs {
   PageBuf buf;
   const int* tables;
   const AttnUnit* units;
-  int n_units, group;       // group: query heads per key head
+  int n_units, n_long;      // the first n_long of them are the long ones
+  int group;                // query heads per key head
   float scale;              // of q . k, in log2 units
-  float* pieces;            // [slot][row][q_heads][D] unnormalised outputs
-  float2* stats;            // [slot][row][q_heads] (running maximum in log2 units, sum)
+  float* pieces;            // [slot][row - piece_row0][q_heads][D] unnormalised outputs
+  float2* stats;            // [slot][row - piece_row0][q_heads] (running maximum in log2 units, sum)
   const OwnSlots* own;      // [rows] the slots of the row's own pieces; n = 0 and no shared slots: none
   int shared_slots;         // slots 0 .. shared_slots - 1 are pieces of every row
   int rows, q_heads;
+  int piece_row0, piece_rows;  // the rows that have pieces: from piece_row0 to the last
   int n_slots;              // 0: no row has pieces
   int few;                  // bf16: units of at most kFewRows query rows, for branch_few_kernel
 };

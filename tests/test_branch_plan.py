@@ -27,11 +27,14 @@ int make(int n, const int* seqs, int shared_end, int group, int kv_heads, int D,
 void info(int* out) { out[0] = plan.shared_slots, out[1] = plan.n_slots, out[2] = plan.few; }
 void units(int* out) { for (auto& u : plan.units) for (int v : {u.tok0, u.tokens, u.table, u.lo, u.hi, u.slot}) *out++ = v; }
 int grid(int units, int heads) { return (int)xcd_grid(units, heads); }
-int pair(int wg, int units, int heads) {
+int pair(int wg, int units, int n_long, int heads) {
   int u = -1, h = -1;
-  return xcd_pair(wg, units, heads, u, h) ? h * units + u : -1;
+  return xcd_pair(wg, units, n_long, heads, u, h) ? h * units + u : -1;
 }
-void own(int* out) { for (auto& o : plan.own) *out++ = o.first, *out++ = o.n; }
+int own(int* out) {  // of every row
+  for (auto& p : plan.parts) for (int i = 0; i < p.rows; ++i) *out++ = p.seq, *out++ = p.own.first, *out++ = p.own.n;
+  return plan.piece_row0;
+}
 }
 """
 
@@ -52,11 +55,16 @@ def plan(seqs, shared_end, group=1, kv_heads=8, D=128, elem=2, cus=256):
     flat = [v for s in seqs for v in s]
     n = lib().make(len(seqs), (ctypes.c_int * len(flat))(*flat), shared_end, group, kv_heads, D, elem, cus)
     units = np.zeros((n, 6), np.int32)
-    info, own = np.zeros(3, np.int32), np.zeros((len(seqs), 2), np.int32)
+    info, own = np.zeros(3, np.int32), np.full((sum(s[0] for s in seqs), 3), -1, np.int32)
     lib().units(units.ctypes.data_as(ctypes.c_void_p))
     lib().info(info.ctypes.data_as(ctypes.c_void_p))
-    lib().own(own.ctypes.data_as(ctypes.c_void_p))
-    return units, info[0], info[1], own, 32 if elem == 4 else 64 if info[2] else 256
+    row0 = lib().own(own.ctypes.data_as(ctypes.c_void_p))
+    assert (own[:, 0] == np.repeat(np.arange(len(seqs)), [s[0] for s in seqs])).all()
+    if info[1] == 0:
+        assert row0 == 0
+    elif row0:  # rows before it are whole
+        assert info[0] == 0 and (own[:row0, 2] == 0).all() and own[row0, 2] > 1
+    return units, info[0], info[1], own[:, 1:], 32 if elem == 4 else 64 if info[2] else 256
 
 
 def check(seqs, shared_end, group, **kw):
@@ -79,9 +87,9 @@ def check(seqs, shared_end, group, **kw):
         assert all(a[1] == b[0] for a, b in zip(got, got[1:]))
         slots = [s for _, _, s in got]
         if slots == [-1]:
-            assert shared == 0 and own[seq_of[t]][1] == 0
+            assert shared == 0 and own[t][1] == 0
         else:
-            o = own[seq_of[t]]
+            o = own[t]
             assert sorted(slots) == list(range(shared)) + list(range(o[0], o[0] + o[1]))
     assert first_row[-1] == rows
     return units, shared, n_slots
@@ -113,17 +121,33 @@ def test_every_row_meets_every_key_once(seed):
 
 
 @pytest.mark.parametrize("heads", [1, 2, 3, 4, 5, 8, 12, 24, 31, 256])
-@pytest.mark.parametrize("units", [1, 2, 7, 8, 60, 333])
-def test_every_pair_has_one_workgroup(units, heads):
+@pytest.mark.parametrize("units,n_long", [(1, 1), (2, 1), (7, 7), (8, 3), (60, 36), (333, 332)])
+def test_every_pair_has_one_workgroup(units, n_long, heads):
     """Each (head, unit) once; an XCD (workgroup number modulo 8) has its share of every unit, and few heads."""
     grid = lib().grid(units, heads)
-    pairs = np.array([lib().pair(w, units, heads) for w in range(grid)])
+    pairs = np.array([lib().pair(w, units, n_long, heads) for w in range(grid)])
     assert sorted(pairs[pairs >= 0]) == list(range(units * heads))
     assert grid % 8 == 0 and grid - units * heads < 64
     for x in range(8):
         mine = pairs[x::8][pairs[x::8] >= 0]
-        assert (np.diff(mine) > 0).all()  # heads outermost
+        for part in (mine[mine % units < n_long], mine[mine % units >= n_long]):
+            assert (np.diff(part) > 0).all()  # heads outermost
+        late = mine % units >= n_long
+        assert (np.diff(late.astype(int)) >= 0).all()  # the long ones first
         assert len(set(mine // units)) <= max(1, heads // min(heads & -heads, 8))
+
+
+@pytest.mark.parametrize("elem,D,kv,rows,tokens", [(2, 128, 12, [7020] * 4, 21060), (2, 64, 16, [5200, 1, 700, 6000], 9000),
+                                                   (4, 128, 8, [900, 1200], 4000), (2, 128, 20, [256 * 14], 9000)])
+def test_the_last_rows_fill_the_last_round(elem, D, kv, rows, tokens):
+    """Many whole workgroups of a few more than full rounds: only the last blocks of rows are cut."""
+    seqs = [(r, 3 * i, tokens + r, 1000 * i) for i, r in enumerate(rows)]
+    units, shared, n_slots = check(seqs, 0, 1, kv_heads=kv, D=D, elem=elem)
+    per = 32 if elem == 4 else 256
+    blocks, cut = sum(-(-r // per) for r in rows), set(units[units[:, 5] >= 0][:, 0])
+    whole = set(units[units[:, 5] < 0][:, 0])
+    assert shared == 0 and n_slots > 1 and len(whole) + len(cut) == blocks and not whole & cut
+    assert 0 < len(cut) <= 256 // kv + 1 and max(whole) < min(cut)  # a round at most, and one block
 
 
 def test_single_tokens_share_their_history():
@@ -138,10 +162,12 @@ def test_single_tokens_share_their_history():
 
 
 def test_whole_chunks_run_apart():
-    # 7020 rows per branch fill workgroups alone: one pass over history and own keys, nothing to merge
+    # 7020 rows per branch fill workgroups alone: one pass over history and own keys, nothing to merge but for
+    # the rows that five rounds of 256 workgroups leave
     seqs = [(7020, 0, 21060, 1000 * i) for i in range(4)]
     units, shared, n_slots = check(seqs, 14016, 1, kv_heads=12)
-    assert shared == 0 and n_slots == 0 and len(units) == 4 * 28
+    assert shared == 0 and (units[:, 5] < 0).sum() >= 256 * 5 // 12 - 2
+    assert units[units[:, 5] >= 0][:, 0].min() >= 3 * 7020
 
 
 def test_one_long_sequence_is_cut():
