@@ -96,7 +96,7 @@ constexpr Kernel kWide{kWideRows, false, {1.3, 0.9, 0}, 5.0, 1, {0.7, 1.0, 0}},
 // distinct keys and values all CUs together read from HBM
 constexpr double kHbmBytesPerUs = 6.0e6;
 // the merge's launch, and its pieces written and read
-constexpr double kMergeUs = 5.0, kPieceBytesPerUs = 1.0e6;
+constexpr double kMergeUs = 5.0, kPieceBytesPerUs = 3.0e6;
 
 // of `rows` rows in blocks of `per`, those of the last `left` blocks; `left` less these
 inline long long tail_of(long long rows, int per, long long& left) {
