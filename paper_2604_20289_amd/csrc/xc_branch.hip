@@ -211,12 +211,15 @@ constexpr float kMaxSlack = 8.0f, kMaxP = 256.0f;
 // Bound by the two phases: at d = 128 about 1150 cycles of softmax and 1430 of
 // products, at d = 64 about 940 and 900, where the products alone are 1024
 // and 640; a clock of 1.5 to 1.8 GHz is what the chip's power leaves with all
-// CUs at it.  28080 rows, 21060 keys, 12 heads of 128: 3.4 ms, 1070 TFLOP/s;
-// 6144 rows, 2304 keys, 8 heads of 64: 42 us, 690 TFLOP/s.  The former with
-// other choices: the matrix phase without a raised wave priority 3760 us
+// CUs at it.  28080 rows, 21060 keys, 12 heads of 128: 3.0 ms, 1200 TFLOP/s;
+// 6144 rows, 2304 keys, 8 heads of 64: 40 us, 720 TFLOP/s.  The former with
+// other choices, at 3440 or 3330 us before the last round of workgroups was
+// filled: the matrix phase without a raised wave priority 3760 us
 // instead of 3440, the softmax raised instead 4010; the softmax not held before
 // its barrier 3800; a maximum per tile 3440 instead of 3330 (51 us instead of 45
-// for the latter).
+// for the latter).  One wave of 64 rows per SIMD, its softmax between its own
+// products, halves the LDS reads but has nothing to hide the requests' address
+// arithmetic behind: 3650 instead of 3310 (47 instead of 43).
 template <int D>
 __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a) {
   using F = Frags<D>;
