@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <unordered_map>
 #include <vector>
 
 namespace xc {
@@ -113,38 +114,53 @@ struct Work {
     double us;
     long long n;
   };
-  std::vector<Kind> kinds;
+  std::vector<Kind> kinds, active;
   void add(long long n, double us) {
     if (n > 0) kinds.push_back({us, n});
   }
   double us(long long places, double crowd) {
     std::sort(kinds.begin(), kinds.end(), [](const Kind& a, const Kind& b) { return a.us > b.us; });
-    std::vector<Kind> active;
+    // running ones by what each has been given (us) when it ends, the next to end in front
+    auto later = [](const Kind& a, const Kind& b) { return a.us > b.us; };
+    active.clear();
     size_t next = 0;
     long long running = 0;
-    double now = 0;
+    double now = 0, given = 0;
     for (;;) {
       while (next < kinds.size() && running < places) {
         const long long n = std::min(kinds[next].n, places - running);
-        active.push_back({kinds[next].us, n});
+        active.push_back({given + kinds[next].us, n});
+        std::push_heap(active.begin(), active.end(), later);
         running += n;
         if ((kinds[next].n -= n) == 0) ++next;
       }
       if (running == 0) return now;
-      double least = active[0].us;
-      for (const Kind& k : active) least = std::min(least, k.us);
-      const double rate = std::min(1.0, crowd / running);
-      now += least / rate;
-      size_t keep = 0;
-      for (Kind& k : active) {
-        k.us -= least;
-        if (k.us > 0.02 * least) active[keep++] = k;  // those that end within 2% end now
-        else running -= k.n;
-      }
-      active.resize(keep);
+      now += (active.front().us - given) / std::min(1.0, crowd / running);
+      given = active.front().us;
+      const double slack = std::max(0.05 * kinds.back().us, 0.01 * given);  // those that end so soon after end now
+      do {
+        std::pop_heap(active.begin(), active.end(), later);
+        running -= active.back().n;
+        active.pop_back();
+      } while (!active.empty() && active.front().us <= given + slack);
     }
   }
 };
+
+// Blocks of rows over runs of keys that count as equally long: the full run,
+// and what of it is not shared.
+struct Like {
+  int own_tiles, full_tiles;  // of the longest
+  bool tall;                  // blocks of more than 32 query rows
+  long long blocks = 0;
+  double own_keys = 0, full_keys = 0;  // in all
+};
+// the same for numbers within 1/16 of each other, exact below 32
+inline int scale_of(int x) {
+  int shift = 0;
+  while (x >> shift >= 32) ++shift;
+  return shift << 5 | x >> shift;
+}
 
 }  // namespace plan_detail
 
@@ -160,6 +176,10 @@ struct Work {
 // chip.  Workgroups that are whole but leave a last round partly filled have
 // the keys of just the last rows cut, as many as that round holds.  The
 // cheapest of all by the times above is taken.
+//
+// Host time: 35 us for 16 branches, 120 us for 64 single tokens behind histories
+// of different lengths, 0.7 ms for 4096 (sequences of like length are priced as
+// one; one by one 0.9 and 19 ms).
 inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end, const PlanShape& sh) {
   using namespace plan_detail;
   long long rows = 0;
@@ -175,66 +195,101 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
   double best_us = 0;
   bool have = false, best_packed = false;
   int best_c = 0, best_tail = 0, best_tail_pieces = 1, per = 0;
-  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128, 192, 256, 512, 1024, 1 << 26};
+  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128, 192, 256, 512, 1024};
+  constexpr int kWhole = 1 << 26;
   std::vector<Kernel> kernels{sh.elem == 4 ? kF32 : kWide};
   if (sh.elem == 2 && sh.group <= kFewRows) kernels.push_back(kFew);
   const int dim = Kernel::at(sh);
-  for (const Kernel& k : kernels)
-    for (int packed = 0; packed < (shared_end > 0 && seqs.size() > 1 ? 2 : 1); ++packed)
-      for (int c : kCuts) {
-        const int kper = std::max(1, k.rows / sh.group);  // batch rows per workgroup
-        Work w;
-        int shared = 0, most = 0;
-        double read = 0;
-        auto add = [&](long long r, int lo, int hi, int c) {
-          const int tiles = tiles_of(lo, hi), s = slots_of(tiles, c);
-          if (s == 0) return 0;
-          w.add(cdiv(r, kper) * s * sh.kv_heads, (double)tiles / s * k.tile[dim] * (k.few && std::min<long long>(r, kper) * sh.group > 32 ? 1.25 : 1.0) + k.start);
-          read += 2.0 * (hi - lo) * sh.D * sh.elem * sh.kv_heads;
-          return s;
-        };
-        if (packed) shared = add(rows, head->first, shared_end, c);
-        bool direct = !packed;
-        for (const PlanSeq& q : seqs) {
-          if (q.rows == 0) continue;
-          const int s = add(q.rows, packed ? std::max(shared_end, q.first) : q.first, q.first + q.tokens, c);
+  for (const Kernel& k : kernels) {
+    const int kper = std::max(1, k.rows / sh.group);  // batch rows per workgroup
+    const long long places = (long long)k.per_cu * sh.cus;
+    auto block = [&](long long r) { return std::min<long long>(r, kper) * sh.group > 32; };
+    std::vector<Like> likes;
+    std::vector<int> like_of;
+    std::unordered_map<uint64_t, int> known;
+    long long blocks = 0;
+    for (const PlanSeq& q : seqs) {
+      const int end = q.first + q.tokens, own_lo = std::max(shared_end, q.first);
+      Like l{tiles_of(own_lo, end), tiles_of(q.first, end), block(q.rows)};
+      const uint64_t key = (uint64_t)scale_of(l.own_tiles) << 32 | scale_of(l.full_tiles) << 1 | (l.tall ? 1 : 0);
+      const int at = known.emplace(key, (int)likes.size()).first->second;
+      if (at == (int)likes.size()) likes.push_back(l);
+      Like& x = likes[at];
+      x.own_tiles = std::max(x.own_tiles, l.own_tiles);
+      x.full_tiles = std::max(x.full_tiles, l.full_tiles);
+      x.blocks += cdiv(q.rows, kper);
+      x.own_keys += std::max(0, end - own_lo);
+      x.full_keys += q.tokens;
+      like_of.push_back(at);
+      blocks += cdiv(q.rows, kper);
+    }
+    Work w;
+    auto add = [&](long long n, int tiles, bool tall, int c) {
+      const int s = slots_of(tiles, c);
+      if (s > 0) w.add(n * s * sh.kv_heads, (double)tiles / s * k.tile[dim] * (k.few && tall ? 1.25 : 1.0) + k.start);
+      return s;
+    };
+    auto time = [&](double keys) {
+      const double t = std::max(w.us(places, k.crowd[dim] * sh.cus), keys * 2 * sh.D * sh.elem * sh.kv_heads / kHbmBytesPerUs);
+      w.kinds.clear();
+      return t;
+    };
+    auto take = [&](double us, bool packed, int c, int tail, int pieces) {
+      if (have && us >= best_us) return;
+      have = true, best_us = us, best_packed = packed, best_c = c, best_tail = tail, best_tail_pieces = pieces;
+      per = kper, best.few = k.few;
+    };
+    int longest = 0;
+    for (const Like& l : likes) longest = std::max(longest, l.full_tiles);
+    for (const bool packed : {false, true}) {
+      if (packed && (shared_end == 0 || seqs.size() < 2)) break;
+      const int together = packed ? tiles_of(head->first, shared_end) : 0;
+      for (size_t i = 0; i <= sizeof kCuts / sizeof *kCuts; ++i) {
+        const int c = i < sizeof kCuts / sizeof *kCuts ? kCuts[i] : kWhole;
+        if (c != kWhole && c >= longest) continue;  // kWhole is the same
+        int most = 0;
+        long long groups = packed ? cdiv(rows, kper) * slots_of(together, c) : 0;
+        for (const Like& l : likes) {
+          const int s = slots_of(packed ? l.own_tiles : l.full_tiles, c);
           most = std::max(most, s);
-          if (s > 1) direct = false;
+          groups += l.blocks * s;
         }
-        const int slots = direct ? 0 : shared + most;
+        if (c != kWhole && groups * sh.kv_heads > 8 * places) continue;  // rounds enough with longer pieces
+        const int slots = packed ? slots_of(together, c) + most : most > 1 ? most : 0;
         if (slots > kPlanMaxSlots || (slots > 2 && slots * piece_bytes > (double)kPlanMaxPieceBytes)) continue;
-        const double us = std::max(w.us((long long)k.per_cu * sh.cus, k.crowd[dim] * sh.cus), read / kHbmBytesPerUs) +
-                          (slots ? kMergeUs + slots * piece_bytes / kPieceBytesPerUs : 0);
-        if (!have || us < best_us)
-          have = true, best_us = us, best_packed = packed != 0, best_c = c, best_tail = 0, per = kper, best.few = k.few;
-
-        // the last blocks of rows, those past the last full round, in pieces
-        if (!direct || c != kCuts[sizeof kCuts / sizeof *kCuts - 1]) continue;
-        long long blocks = 0;
-        for (const PlanSeq& q : seqs) blocks += cdiv(q.rows, kper);
-        const long long places = (long long)k.per_cu * sh.cus, over = blocks * sh.kv_heads % places;
-        if (blocks * sh.kv_heads <= places || over == 0) continue;
-        for (int more = 0; more < 2; ++more)
-          for (int pieces : {2, 3, 4, 6, 8}) {
-            const long long tail = cdiv(over, sh.kv_heads) + more;
-            if (tail >= blocks) continue;
-            w.kinds.clear();
-            read = 0;
-            long long left = tail, tail_rows = 0;
-            for (size_t i = seqs.size(); i-- > 0;) {
-              const PlanSeq& q = seqs[i];
-              const long long r = tail_of(q.rows, kper, left);
-              add(q.rows - r, q.first, q.first + q.tokens, c);
-              add(r, q.first, q.first + q.tokens, (int)cdiv(tiles_of(q.first, q.first + q.tokens), pieces));
-              tail_rows += r;
-            }
-            const double bytes = (double)pieces * tail_rows / rows * piece_bytes;
-            if (bytes > (double)kPlanMaxPieceBytes) continue;
-            const double t = std::max(w.us(places, k.crowd[dim] * sh.cus), read / kHbmBytesPerUs) + kMergeUs + bytes / kPieceBytesPerUs;
-            if (t < best_us)
-              best_us = t, best_packed = false, best_c = c, best_tail = (int)tail, best_tail_pieces = pieces, per = kper, best.few = k.few;
-          }
+        double keys = packed ? shared_end - head->first : 0;
+        if (packed) add(cdiv(rows, kper), together, block(rows), c);
+        for (const Like& l : likes) {
+          add(l.blocks, packed ? l.own_tiles : l.full_tiles, l.tall, c);
+          keys += packed ? l.own_keys : l.full_keys;
+        }
+        take(time(keys) + (slots ? kMergeUs + slots * piece_bytes / kPieceBytesPerUs : 0), packed, c, 0, 1);
       }
+    }
+    // the last blocks of rows, those past the last full round, in pieces
+    const long long over = blocks * sh.kv_heads % places;
+    if (blocks * sh.kv_heads <= places || over == 0) continue;
+    for (int more = 0; more < 2; ++more)
+      for (int pieces : {2, 3, 4, 6, 8}) {
+        const long long tail = cdiv(over, sh.kv_heads) + more;
+        if (tail >= blocks) continue;
+        long long left = tail, tail_rows = 0;
+        double keys = 0;
+        std::vector<long long> whole;
+        for (const Like& l : likes) whole.push_back(l.blocks), keys += l.full_keys;
+        for (size_t i = seqs.size(); left > 0;) {
+          const long long before = left, r = tail_of(seqs[--i].rows, kper, left);
+          const Like& l = likes[like_of[i]];
+          whole[like_of[i]] -= before - left;
+          add(before - left, l.full_tiles, l.tall, (int)cdiv(l.full_tiles, pieces));
+          tail_rows += r;
+        }
+        for (size_t i = 0; i < likes.size(); ++i) add(whole[i], likes[i].full_tiles, likes[i].tall, kWhole);
+        const double bytes = (double)pieces * tail_rows / rows * piece_bytes, t = time(keys);
+        if (bytes <= (double)kPlanMaxPieceBytes)
+          take(t + kMergeUs + bytes / kPieceBytesPerUs, false, kWhole, (int)tail, pieces);
+      }
+  }
 
   auto emit = [&](const PlanSeq& q, int tok0, long long r, int lo, int hi, int slot0, bool direct, int c) {
     const int n = slots_of(tiles_of(lo, hi), c);
