@@ -507,8 +507,9 @@ xc_status xc_batch_set(xc_batch* batch, int32_t n, const int32_t* seqs, const in
  *                xc_model_config's rope).
  *   theta      : rotary base > 1.
  *   q_out      : device [rows][q_ld], columns as the q part of qkv.
- * ld and q_ld in elements, rows 16-byte aligned; qkv and q_out do not
- * overlap (a batch without rows reads neither, they may be NULL).  Arithmetic in float32 with one rounding, angles in 64 bits.
+ * ld and q_ld in elements, rows 16-byte aligned; qkv, q_out and the page
+ * buffers do not overlap (a batch without rows reads none of them, they may be
+ * NULL).  Arithmetic in float32 with one rounding, angles in 64 bits.
  * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (the batch is not set or out of
  * date, or a page to be written is shared with another sequence), XC_ERR_HIP
  * (sticky). */
@@ -521,7 +522,8 @@ xc_status xc_qk_norm_rope(xc_batch* batch, int32_t block, const void* qkv, int64
  * with rows have in common are read once for the batch where that pays.
  *   q      : device [rows][q_ld], out: device [rows][out_ld], both q_heads *
  *            head_dim columns in the pool's dtype, rows 16-byte aligned, not
- *            overlapping; NULL where the batch has no rows.
+ *            overlapping (nor out and the page buffers); NULL where the batch
+ *            has no rows.
  *   scale  : positive (a normal number); 0 takes 1 / sqrt(head_dim).
  * Scores, softmax statistics and sums are float32; bf16 pools round the
  * probabilities to bf16 for the product with v.  The same call gives the same

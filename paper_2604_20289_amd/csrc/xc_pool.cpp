@@ -26,6 +26,7 @@ namespace {
 constexpr long long kMaxPlaces = 1ll << 30;
 constexpr int kMaxRows = 1 << 24;
 constexpr int kMaxHeads = 1024;
+constexpr long long kMaxStride = 1ll << 36;  // a row stride; keeps extents in 64 bits
 
 struct Fail {
   xc_status s;
@@ -65,6 +66,11 @@ xc_status status_of(PageStatus s) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + bn && y < x + an;
+}
+
 struct Pool {
   Pool(const xc_pool_config& c, int shift) : cfg(c), book(c.n_pages, shift, c.max_seqs) {}
   xc_pool_config cfg;
@@ -78,6 +84,11 @@ struct Pool {
 
   long long block_elems() const {
     return ((long long)cfg.n_pages << book.shift()) * cfg.kv_heads * cfg.head_dim;
+  }
+  // whether bytes lie in the page buffers
+  bool holds(const void* x, size_t n) const {
+    const size_t bytes = (size_t)block_elems() * cfg.n_blocks * esz;
+    return overlap(x, n, keys, bytes) || overlap(x, n, values, bytes);
   }
   PageBuf block(int b) const {
     const long long o = b * block_elems() * esz;
@@ -167,11 +178,6 @@ void committed(F&& f) {
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-
-bool overlap(const void* a, size_t an, const void* b, size_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + bn && y < x + an;
-}
 
 // bytes from the first element of [rows][ld] to the end of its last row
 size_t extent(long long rows, long long ld, long long width, int esz) {
@@ -525,13 +531,14 @@ xc_status xc_qk_norm_rope(xc_batch* b, int32_t block, const void* qkv, int64_t l
   Pool& p = *b->p;
   const xc_pool_config& c = p.cfg;
   const long long width = (long long)(c.q_heads + 2 * c.kv_heads) * c.head_dim, q_width = (long long)c.q_heads * c.head_dim;
-  if (block < 0 || block >= c.n_blocks || ld < width || q_ld < q_width || ld > (1ll << 40) || q_ld > (1ll << 40) ||
+  if (block < 0 || block >= c.n_blocks || ld < width || q_ld < q_width || ld > kMaxStride || q_ld > kMaxStride ||
       ld * p.esz % 16 || q_ld * p.esz % 16 || !aligned16(qkv) || !aligned16(q_out))
     return XC_ERR_INVALID_ARG;
   if (positions && ((n_axes != 1 && n_axes != 3) || !std::isfinite(theta) || theta <= 1.0)) return XC_ERR_INVALID_ARG;
   return guarded(p, [&]() -> xc_status {
     if (!b->current()) return XC_ERR_STATE;
-    if (overlap(qkv, extent(b->rows, ld, width, p.esz), q_out, extent(b->rows, q_ld, q_width, p.esz)))
+    const size_t in_bytes = extent(b->rows, ld, width, p.esz), out_bytes = extent(b->rows, q_ld, q_width, p.esz);
+    if (overlap(qkv, in_bytes, q_out, out_bytes) || p.holds(qkv, in_bytes) || p.holds(q_out, out_bytes))
       return XC_ERR_INVALID_ARG;
     // a page that another sequence reads too is not written
     for (int page : b->written)
@@ -564,15 +571,15 @@ xc_status xc_branch_attention(xc_batch* b, int32_t block, const void* q, int64_t
   Pool& p = *b->p;
   const xc_pool_config& c = p.cfg;
   const long long width = (long long)c.q_heads * c.head_dim;
-  if (block < 0 || block >= c.n_blocks || q_ld < width || out_ld < width || q_ld > (1ll << 40) || out_ld > (1ll << 40) ||
+  if (block < 0 || block >= c.n_blocks || q_ld < width || out_ld < width || q_ld > kMaxStride || out_ld > kMaxStride ||
       q_ld * p.esz % 16 || out_ld * p.esz % 16 || !aligned16(q) || !aligned16(out))
     return XC_ERR_INVALID_ARG;
   const float log2_scale = (scale == 0.f ? 1.0f / std::sqrt((float)c.head_dim) : scale) * 1.4426950408889634f;
   if (!(scale >= 0.f) || !std::isnormal(log2_scale)) return XC_ERR_INVALID_ARG;
   return guarded(p, [&]() -> xc_status {
     if (!b->current()) return XC_ERR_STATE;
-    if (overlap(q, extent(b->rows, q_ld, width, p.esz), out, extent(b->rows, out_ld, width, p.esz)))
-      return XC_ERR_INVALID_ARG;
+    const size_t in_bytes = extent(b->rows, q_ld, width, p.esz), out_bytes = extent(b->rows, out_ld, width, p.esz);
+    if (overlap(q, in_bytes, out, out_bytes) || p.holds(out, out_bytes)) return XC_ERR_INVALID_ARG;
     if (b->rows == 0) return XC_OK;
     AttnArgs a = b->attn;
     a.q = q;

@@ -703,12 +703,13 @@ def test_refused_arguments():
     for bad in (dict(b=None), dict(block=-1), dict(block=2), dict(q=None), dict(out=None), dict(q_ld=255), dict(q_ld=248),
                 dict(q_ld=260), dict(ld=-256), dict(ld=1 << 62), dict(scale=math.nan), dict(scale=math.inf), dict(scale=-1.0),
                 dict(scale=1e-45), dict(scale=3.4e38), dict(q=q.data_ptr() + 2), dict(out=out.data_ptr() + 8),
-                dict(out=q.data_ptr()), dict(out=q.data_ptr() + 4 * 512)):
+                dict(out=q.data_ptr()), dict(out=q.data_ptr() + 4 * 512), dict(out=pool.keys.data_ptr()),
+                dict(out=pool.values.data_ptr() + 4096)):
         assert lib.xc_branch_attention(*{**good_a, **bad}.values()) == INVALID, bad
     for bad in (dict(b=None), dict(block=2), dict(x=None), dict(gq=None), dict(gk=None), dict(q=None), dict(ld=511),
                 dict(ld=504), dict(ld=516), dict(q_ld=0), dict(axes=2), dict(axes=0), dict(theta=1.0),
                 dict(theta=math.nan), dict(theta=math.inf), dict(x=x.data_ptr() + 4), dict(q=q.data_ptr() + 4),
-                dict(q=x.data_ptr(), q_ld=512)):
+                dict(q=x.data_ptr(), q_ld=512), dict(q=pool.values.data_ptr()), dict(x=pool.keys.data_ptr())):
         assert lib.xc_qk_norm_rope(*{**good_n, **bad}.values()) == INVALID, bad
     ints = lambda *v: (ctypes.c_int32 * len(v))(*v)  # noqa: E731
     for seqs, new in (((s,), (6,)), ((s,), (-1,)), ((s, s), (1, 1)), ((9,), (0,)), ((-1,), (0,)), ((99,), (0,))):
