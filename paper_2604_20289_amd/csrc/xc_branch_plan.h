@@ -244,8 +244,10 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
     for (const bool packed : {false, true}) {
       if (packed && (shared_end == 0 || seqs.size() < 2)) break;
       const int together = packed ? tiles_of(head->first, shared_end) : 0;
-      for (size_t i = 0; i <= sizeof kCuts / sizeof *kCuts; ++i) {
-        const int c = i < sizeof kCuts / sizeof *kCuts ? kCuts[i] : kWhole;
+      constexpr size_t kNumCuts = sizeof kCuts / sizeof *kCuts;
+      for (size_t i = 0; i <= kNumCuts + 1; ++i) {
+        // past the list: as many pieces as the slots hold (histories of millions of tokens), one
+        const int c = i < kNumCuts ? kCuts[i] : i == kNumCuts ? (int)cdiv(longest, kPlanMaxSlots - 6) : kWhole;
         if (c != kWhole && c >= longest) continue;  // kWhole is the same
         int most = 0;
         long long groups = packed ? cdiv(rows, kper) * slots_of(together, c) : 0;

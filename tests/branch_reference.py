@@ -6,6 +6,13 @@ import torch
 EPS_OF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}  # half a step, relative
 
 
+# Sequences (tokens before, new tokens) whose workgroups are a few more than full rounds of 256, so that the keys of the
+# last rows are cut: float32 or bf16, head_dim, key heads, query heads per key head, sequences.
+LAST_ROUND = [(torch.bfloat16, 128, 24, 1, [(900, 1500), (1100, 1321)]), (torch.bfloat16, 64, 40, 2, [(3000, 800)]),
+              (torch.bfloat16, 64, 7, 1, [(2000, 5000), (0, 1), (600, 4900)]), (torch.float32, 64, 33, 1, [(700, 290)]),
+              (torch.float32, 32, 5, 4, [(900, 210), (1000, 230)])]
+
+
 def gather(buf, block, table):
     """[tokens, kv_heads, d] of a sequence, float64 on the CPU."""
     first, tokens, pages = table

@@ -11,7 +11,10 @@ import tempfile
 import numpy as np
 import pytest
 
-from paper_2604_20289_amd import build
+torch = pytest.importorskip("torch")
+
+import branch_reference as ref  # noqa: E402
+from paper_2604_20289_amd import build  # noqa: E402
 
 SHIM = r"""
 #include "xc_branch_plan.h"
@@ -148,6 +151,21 @@ def test_the_last_rows_fill_the_last_round(elem, D, kv, rows, tokens):
     whole = set(units[units[:, 5] < 0][:, 0])
     assert shared == 0 and n_slots > 1 and len(whole) + len(cut) == blocks and not whole & cut
     assert 0 < len(cut) <= 256 // kv + 1 and max(whole) < min(cut)  # a round at most, and one block
+
+
+@pytest.mark.parametrize("case", range(len(ref.LAST_ROUND)))
+def test_the_gpu_tests_reach_cut_last_rows(case):
+    dtype, d, kv, group, lengths = ref.LAST_ROUND[case]
+    seqs = [(n, 0, a + n, 1000 * i) for i, (a, n) in enumerate(lengths)]
+    units, shared, n_slots = check(seqs, 0, group, kv_heads=kv, D=d, elem=2 if dtype == torch.bfloat16 else 4)
+    assert shared == 0 and n_slots > 1 and (units[:, 5] < 0).any() and (units[:, 5] >= 0).any()
+
+
+@pytest.mark.parametrize("tokens", [10 ** 6, 2 * 10 ** 7, 2 ** 30 - 1])
+def test_histories_of_millions_of_tokens_are_cut(tokens):
+    for n, end in ((1, 0), (2, (tokens - 100) // 64 * 64)):
+        units, shared, n_slots = check([(1, 0, tokens, 0)] * n, end, 1, kv_heads=1)
+        assert 64 <= n_slots <= 96
 
 
 def test_single_tokens_share_their_history():

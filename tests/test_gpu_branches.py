@@ -223,6 +223,24 @@ def test_few_rows_over_every_number_of_tiles(dtype, d):
             check_attention(pool, batch, [s], [rows], seed=i)
 
 
+@pytest.mark.parametrize("dtype,d,kv,group,lengths", ref.LAST_ROUND)
+def test_a_cut_last_round(dtype, d, kv, group, lengths):
+    """Most rows whole, the last ones in pieces (tests/test_branch_plan.py): both, and the rows between them."""
+    pool = make(dtype, pages=sum(-(-sum(x) // 64) for x in lengths), kv=kv, heads=kv * group, page=64, d=d, fill="nan")
+    seqs, g = [], torch.Generator().manual_seed(8)
+    for before, new in lengths:
+        seqs.append(pool.new())
+        pool.extend(seqs[-1:], [before + new])
+        write(pool, seqs[-1], *torch.randn(2, before + new, kv, d, generator=g))
+    batch = Batch(pool)
+    new = [n for _, n in lengths]
+    batch.set(seqs, new)
+    heads = sorted({0, kv * group // 2, kv * group - 1})
+    out, _ = check_attention(pool, batch, seqs, new, seed=9, only=heads)
+    again, _ = check_attention(pool, batch, seqs, new, seed=9, only=heads)
+    assert torch.equal(out, again)
+
+
 def test_infinite_and_nan_tokens_stay_in_their_branch():
     pool = make(BF16, pages=64, kv=1, page=16, d=64)
     parent, seqs = grow(pool, 100, 0, [(20, 3), (20, 3), (20, 3)])
