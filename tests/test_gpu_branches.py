@@ -787,8 +787,9 @@ def test_batches_grow_and_shrink():
 
 # ---------------------------------------------------------------- from a rollout
 
+@pytest.mark.parametrize("grid", [None, (1, 5, 7), (3, 9, 11)])
 @pytest.mark.parametrize("dtype,generations", [("f32", 1), ("f32", 3), ("bf16", 2), ("bf16", 5)])
-def test_a_rollouts_history_is_shared_by_branches(dtype, generations):
+def test_a_rollouts_history_is_shared_by_branches(dtype, generations, grid):
     """A model handle's window, imported: the tokens of the kept chunks, oldest first, in every block; then
     branches of it."""
     import synth
@@ -796,6 +797,8 @@ def test_a_rollouts_history_is_shared_by_branches(dtype, generations):
     w = synth.workload(0)
     w = synth.with_model(w, rope=1, kv_window=3, n_heads=4, head_dim=64 if dtype == "bf16" else 32,
                          hidden=256 if dtype == "bf16" else 128, mlp_hidden=512, dtype=dtype)
+    if grid:  # an odd number of tokens
+        w = synth.with_model(w, groups=(synth.ViewGroup(1, *grid),))
     m = w.model
     L, D, H = m.tokens, m.head_dim, m.n_heads
     h = XCache(m, w.gate, synth.make_weights(m), stream())
