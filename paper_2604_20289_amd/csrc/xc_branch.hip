@@ -279,6 +279,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
       group_at = ((long long)((unsigned)page * page_kb) << 10) + (g0 & in_page) * (D * 2);
       group_rows = min(15, last - g0);
     }
+    if (dst == nullptr) return;  // only the address
     int row = min(is_v ? v_row[i] : k_row[i], group_rows);
     if (j0) row = max(row, un.lo - base - (wave + kWaves * i) / KCG / 2 * 16);
     dma16((is_v ? Vh : Kh) + group_at, row * (D * 2) + (is_v ? v_col[i] : k_col[i]), dst + (wave + kWaves * i) * 1024);
@@ -295,12 +296,27 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
       fetch(j, i, true, vd, j0);
     }
   };
-  request(0, tK0, sV0, true);
+  // What S of the first tile needs is asked for first and waited for alone (36
+  // tiles, d = 128: 64 us instead of 65).
+#pragma unroll
+  for (int i = 0; i < NB; ++i) fetch(0, i, false, tK0, true);
+  bf16x8 qf[KS];
+  if (live) {
+    const bf16* q = query_row(a, un, h, min(wave * 32 + lo, rows - 1), hi);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    fetch(0, i, false, nullptr, true);
+    fetch(0, i, true, sV0, true);
+  }
   request(1, tK1, sV1);
   request(2, tK2, sV2);
   if (!live) {
     // waves without rows only stage tiles, between the same barriers
     XC_WAIT_VM(0);
+    tile_barrier();
     tile_barrier();
     if (later) tile_barrier();
     auto stage = [&](int j, char* kd, char* vd) __attribute__((always_inline)) {
@@ -323,12 +339,6 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     return;
   }
 
-  bf16x8 qf[KS];
-  {
-    const bf16* q = query_row(a, un, h, min(wave * 32 + lo, rows - 1), hi);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
-  }
   f32x16 s[2], oacc[DT + ONES];
 #pragma unroll
   for (int i = 0; i < DT + ONES; ++i)
@@ -379,8 +389,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     for (int i = 0; i < PF; ++i) fr[(i0 + i) % PF] = frag(i0 + i, vt, kt);
   };
   // Probabilities of the tile against the maximum so far, which is looked for
-  // only where one of them grew past 2^kMaxSlack (first tile: from kNoMax) -
-  // most tiles need none.  Then the tile's own maximum joins in and everything
+  // only where one of them grew past 2^kMaxSlack (from the first tile's
+  // maximum) - most tiles need none.  Then the tile's own maximum joins in and everything
   // so far is rescaled.  The limit is checked on the sum or, where there is
   // none, on the bf16 exponents, whose highest bit stands for 2 and more: the
   // maximum is taken kMaxSlack higher there.
@@ -429,12 +439,21 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     mask_half(s[1], base + j * 64 + 32, hi, un.lo, last);
   };
 
-  XC_WAIT_VM(0);
+  XC_WAIT_VM(5 * NB);  // the first K, the queries
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
   tile_barrier();
   lead(NPV, sV0, tK0);
   products(NPV, NPV + NQK, sV0, tK0, nothing);
   if (un.lo != base && n > 1) mask(0);
-  if (later) tile_barrier();
+  // (keys that are yet to be masked are copies of valid ones)
+  m_run = fmaxf(kNoMax, partner_max(fmaxf(half_max(s[0]), half_max(s[1]))) * a.scale + (ONES ? kMaxSlack : 0.f));
+  XC_WAIT_VM(4 * NB);  // the first V
+  tile_barrier();
+  if (later) {
+    XC_WAIT_VM(2 * NB);  // the second tile
+    tile_barrier();
+  }
   // tile j: its V, the next K, and the slots of tile j + 3
   auto iter = [&](int j, const char* vt, const char* kn, char* kd, char* vd) __attribute__((always_inline)) {
     softmax();
