@@ -532,7 +532,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
 //
 // Bound by reading keys and values: 16 rows over 14200 keys, 12 heads of 128
 // (101 MB) 25.6 us with the merge, 64 rows over 36600 keys, 16 heads of 128
-// (559 MB) 121 us (141 as two workgroups of one row group each, before requests
+// (658 MB) 120 us (141 as two workgroups of one row group each, before requests
 // fetched whole 128-byte lines), 64 rows over 2000 keys of their own, 16 heads of
 // 128 (1049 MB) 172 us, 6.1 TB/s.
 template <int D>
