@@ -490,8 +490,8 @@ xc_status xc_batch_destroy(xc_batch* batch);
  * the sequences changes (extend, trim, free, compact, import; a fork of it
  * changes nothing): the calls below then return XC_ERR_STATE.  After
  * XC_ERR_OOM or XC_ERR_HIP the batch has no rows.
- * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED, XC_ERR_OOM, XC_ERR_STATE,
- * XC_ERR_HIP (sticky). */
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED (more rows, or more rows and
+ * heads than a launch takes), XC_ERR_OOM, XC_ERR_STATE, XC_ERR_HIP (sticky). */
 xc_status xc_batch_set(xc_batch* batch, int32_t n, const int32_t* seqs, const int32_t* new_tokens);
 
 /* Norms and rotation of the batch's queries and keys in one pass: per head

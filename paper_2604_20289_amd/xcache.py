@@ -128,7 +128,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "xc_seq_trim": (i32, [vp, i32, i32, i32]),
         "xc_seq_free": (i32, [vp, i32, vp]),
         "xc_seq_import": (i32, [vp, i32, vp]),
-        "xc_seq_pages": (i32, [vp, i32, P(i32), P(i32), vp, sz, P(sz)]),
+        "xc_seq_pages": (i32, [vp, i32, vp, vp, vp, sz, vp]),
         "xc_batch_init": (i32, [vp, P(vp)]),
         "xc_batch_destroy": (i32, [vp]),
         "xc_batch_set": (i32, [vp, i32, vp, vp]),
@@ -364,15 +364,18 @@ def xc_seq_import(pool: int, seq: int, h: int):
     _check(load_library().xc_seq_import(pool, seq, h), "xc_seq_import")
 
 
+_ROOM = bytes(4 * 512)
+
+
 def xc_seq_pages(pool: int, seq: int):
     """(place of the first token, tokens, page numbers) of a sequence."""
-    first, tokens, n = ctypes.c_int32(), ctypes.c_int32(), ctypes.c_size_t()
-    lib = load_library()
-    _check(lib.xc_seq_pages(pool, seq, None, None, None, 0, ctypes.byref(n)), "xc_seq_pages")
-    pages = np.empty(n.value, np.int32)
-    _check(lib.xc_seq_pages(pool, seq, ctypes.byref(first), ctypes.byref(tokens), pages.ctypes.data, n.value,
-                            ctypes.byref(n)), "xc_seq_pages")
-    return first.value, tokens.value, pages
+    f, head, n, pages = load_library().xc_seq_pages, _ints((0, 0)), array.array("Q", (0,)), _ints(_ROOM)
+    at = _at(head)
+    _check(f(pool, seq, at, at + 4, _at(pages), len(pages), _at(n)), "xc_seq_pages")
+    if n[0] > len(pages):  # again, with room for all
+        pages = _ints(bytes(4 * n[0]))
+        _check(f(pool, seq, at, at + 4, _at(pages), len(pages), _at(n)), "xc_seq_pages")
+    return head[0], head[1], np.frombuffer(pages, np.int32, n[0])
 
 
 def xc_batch_init(pool: int) -> int:

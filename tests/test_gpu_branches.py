@@ -504,6 +504,11 @@ def test_many_copies_in_one_call():
     pool.free([parent] + kids[::2])
     assert pool.compact() > 100
     assert torch.equal(pool.keys[0, torch.tensor([int(pool.pages(k)[2][0]) for k in kids[1::2]])], before)
+    long = pool.new()
+    pool.extend([long], [16 * 700 - 3])
+    first, tokens, pages = pool.pages(long)
+    live = pool.info()["live_pages"] - 700
+    assert (first, tokens) == (0, 16 * 700 - 3) and pages.tolist() == list(range(live, live + 700))
 
 
 # ---------------------------------------------------------------- together
