@@ -927,13 +927,13 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
 // Joins the pieces of each (row, query head):
 // O = sum_p w_p O_p / sum_p w_p l_p, w_p = 2^(m_p - max m).
 // A wave owns one of them.  It is a chain of memory latencies, so what is
-// independent is in flight together: all statistics (a lane per piece), then
+// independent is in flight together: all statistics (a lane per piece) and
 // the outputs, each of 64 / (D / 4) lane groups taking every so many pieces,
-// four at a time.  Every sum has a fixed order.  4 to 5 us for 192 rows of 15
+// eight at a time.  Every sum has a fixed order.  4 to 5 us for 192 rows of 15
 // pieces and for 1024 of 13.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
-  constexpr int LPH = D / 4, NG = 64 / LPH, U = 4;
+  constexpr int LPH = D / 4, NG = 64 / LPH, U = 8;
   const int lane = threadIdx.x & 63, g = lane / LPH, d0 = lane % LPH * 4;
   const long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long rq = (long long)a.piece_rows * a.q_heads;
@@ -949,6 +949,15 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
   float2 st[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) st[k] = a.stats[slot(min(lane + 64 * k, n - 1))];
+  f32x4 o[U];
+  auto fetch = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int p = p0 + k * NG + g;
+      if (p < n) o[k] = *reinterpret_cast<const f32x4*>(a.pieces + slot(p) * D + d0);
+    }
+  };
+  fetch(0);
   float m = fmaxf(st[0].x, st[1].x);
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
@@ -961,19 +970,16 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) den += __shfl_xor(den, off, 64);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = 0; p0 < n; p0 += NG * U) {
-    f32x4 o[U];
-    float wp[U];
+  for (int p0 = 0;;) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int p = p0 + k * NG + g;
-      o[k] = *reinterpret_cast<const f32x4*>(a.pieces + slot(min(p, n - 1)) * D + d0);
       const float w0 = __shfl(w[0], p & 63, 64), w1 = __shfl(w[1], p & 63, 64);
-      wp[k] = p >= n ? 0.f : p < 64 ? w0 : w1;
+      if (p < n) acc += (p < 64 ? w0 : w1) * o[k];
     }
-#pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (p0 + k * NG + g < n) acc += wp[k] * o[k];
+    p0 += NG * U;
+    if (p0 >= n) break;
+    fetch(p0);
   }
 #pragma unroll
   for (int off = 32; off >= LPH; off >>= 1)
