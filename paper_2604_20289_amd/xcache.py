@@ -463,7 +463,10 @@ class Pool:
         lib = load_library()
         self._fork, self._extend, self._free, self._compact = (lib.xc_seq_fork, lib.xc_seq_extend, lib.xc_seq_free,
                                                                lib.xc_pool_compact)
-        self._moved = _ints([0])
+        self._moved, self._pages = _ints([0]), lib.xc_seq_pages
+        self._head = _ints((0, 0, 0, 0))  # first, tokens, pages (64 bits)
+        at = _at(self._head)
+        self._heads = at, at + 4, at + 8
         self.p = xc_pool_init(c, keys, values, stream)
 
     def new(self) -> int:
@@ -492,7 +495,13 @@ class Pool:
         return self._moved[0]
 
     def pages(self, seq: int):
-        return xc_seq_pages(self.p, seq)
+        """(place of the first token, tokens, page numbers) of a sequence."""
+        table, head = _ints(_ROOM), self._head
+        first, tokens, n = self._heads
+        _check(self._pages(self.p, seq, first, tokens, _at(table), len(table), n), "xc_seq_pages")
+        if head[2] > len(table):
+            return xc_seq_pages(self.p, seq)
+        return head[0], head[1], np.frombuffer(table, np.int32, head[2])
 
     def import_window(self, seq: int, xcache: "XCache"):
         """Append the past chunks of a rollout's window (xc_seq_import)."""
