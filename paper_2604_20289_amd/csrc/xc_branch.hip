@@ -828,32 +828,38 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
   for (int i = 0; i < n; ++i) {
     XC_WAIT_VM(LOADS);  // K has landed, V may be on its way
     asm volatile("" ::: "memory");
-    f32x16 s;
+    f32x16 s, s1;  // two sums: no product waits for the one before it
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    for (int r = 0; r < 16; ++r) s[r] = s1[r] = 0.f;
 #pragma unroll
     for (int t = 0; t < D / 8; ++t) {
       const f32x4 k = *reinterpret_cast<const f32x4*>(kt + lo * (D * 4) + swz(lo, t * 2 + hi) * 16);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[t][e], s, 0, 0, 0);
+      for (int e = 0; e < 4; e += 2) {
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[t][e], s, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e + 1], qf[t][e + 1], s1, 0, 0, 0);
+      }
     }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] += s1[r];
     const bool more = i + 1 < n;
     if (more) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this K has been read
       cover(i + 1);
       request(i + 1, Kh, kt);
     }
-    const int at0 = base + (wave + 4 * i) * 32;
-    float mx = -INFINITY;
+    const int tile = wave + 4 * i;
+    if (tile == 0 || tile == tiles - 1) {  // only these reach outside the unit's keys
+      const int at0 = base + tile * 32;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int at = at0 + (r >> 2) * 8 + hi * 4 + (r & 3);
-      if (at < un.lo || at > last) s[r] = -INFINITY;
-      mx = fmaxf(mx, s[r]);
+      for (int r = 0; r < 16; ++r) {
+        const int at = at0 + (r >> 2) * 8 + hi * 4 + (r & 3);
+        if (at < un.lo || at > last) s[r] = -INFINITY;
+      }
     }
-    mx = partner_max(mx) * a.scale;
-    if (mx > m_run) {
-      const float alpha = exp2f(m_run - mx);
+    const float mx = partner_max(half_max(s)) * a.scale;
+    if (mx > m_run + kMaxSlack) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
       l_run *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -863,7 +869,7 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = exp2f(__builtin_fmaf(s[r], a.scale, -m_run));
+      s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale, -m_run));
       l_run += s[r];
     }
     if (more) { XC_WAIT_VM(LOADS); } else { XC_WAIT_VM(0); }
