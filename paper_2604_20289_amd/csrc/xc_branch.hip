@@ -762,7 +762,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // keys whose scores sit in one register of the two half-waves.  Bound by these
 // products (64 cycles each).  Many rows are dealt to more workgroups: four waves
 // of 32 rows on shared tiles, staged through registers, took 456 us for 2000
-// rows, 4500 keys, 8 heads of 128, where these take 388, and 9.9 us for the tiny
+// rows, 4500 keys, 8 heads of 128, where these took 388 (350 now, 105
+// TFLOP/s: the matrix units are busy 70% of the cycles), and 9.9 us for the tiny
 // model's 3 x 64 rows and 128 keys, where these take 5.1.
 // Row r, chunk c of a tile sits at c ^ f(r): rows at one chunk (K) and one row's
 // chunks beside those of the row 4 below (V) meet different banks.

@@ -93,7 +93,7 @@ struct Kernel {
 };
 constexpr Kernel kWide{kWideRows, false, {1.3, 0.9, 0}, 5.0, 1, {0.7, 1.0, 0}},
     kFew{kFewRows, true, {0.86, 0.43, 0}, 3.0, 2, {0.62, 0.62, 0}},
-    kF32{kF32Rows, false, {2.7, 1.4, 0.7}, 4.0, 1, {1.0, 1.0, 1.0}};
+    kF32{kF32Rows, false, {2.45, 1.2, 0.67}, 4.0, 1, {1.0, 1.0, 1.0}};
 // distinct keys and values all CUs together read from HBM
 constexpr double kHbmBytesPerUs = 6.0e6;
 // the merge's launch, and its pieces written and read
