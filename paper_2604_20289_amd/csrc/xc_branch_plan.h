@@ -58,7 +58,8 @@ struct AttnPlan {
 
 constexpr int kPlanMaxSlots = 96;
 constexpr int kXcds = 8;  // each has its own L2
-constexpr long long kPlanMaxPieceBytes = 1ll << 30;
+// pieces of a plan at most; a plan without any always exists
+constexpr long long kPlanMaxPieceBytes = 4ll << 30;
 
 namespace plan_detail {
 
@@ -175,12 +176,14 @@ inline int scale_of(int x) {
 // keys is cut into pieces of about `c` tiles, so that few rows still fill the
 // chip.  Workgroups that are whole but leave a last round partly filled have
 // the keys of just the last rows cut, as many as that round holds.  The
-// cheapest of all by the times above is taken.
+// cheapest of all by the times above is taken, of those whose pieces take at
+// most max_piece_bytes (0: no pieces, each sequence's rows in one go).
 //
 // Host time: 35 us for 16 branches, 120 us for 64 single tokens behind histories
 // of different lengths, 0.7 ms for 4096 (sequences of like length are priced as
 // one; one by one 0.9 and 19 ms).
-inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end, const PlanShape& sh) {
+inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end, const PlanShape& sh,
+                               long long max_piece_bytes = kPlanMaxPieceBytes) {
   using namespace plan_detail;
   long long rows = 0;
   for (const PlanSeq& q : seqs) rows += q.rows;
@@ -258,7 +261,7 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
         }
         if (c != kWhole && groups * sh.kv_heads > 8 * places) continue;  // rounds enough with longer pieces
         const int slots = packed ? slots_of(together, c) + most : most > 1 ? most : 0;
-        if (slots > kPlanMaxSlots || (slots > 2 && slots * piece_bytes > (double)kPlanMaxPieceBytes)) continue;
+        if (slots > kPlanMaxSlots || slots * piece_bytes > (double)max_piece_bytes) continue;
         double keys = packed ? shared_end - head->first : 0;
         if (packed) add(cdiv(rows, kper), together, block(rows), c);
         for (const Like& l : likes) {
@@ -288,7 +291,7 @@ inline AttnPlan plan_attention(const std::vector<PlanSeq>& seqs, int shared_end,
         }
         for (size_t i = 0; i < likes.size(); ++i) add(whole[i], likes[i].full_tiles, likes[i].tall, kWhole);
         const double bytes = (double)pieces * tail_rows / rows * piece_bytes, t = time(keys);
-        if (bytes <= (double)kPlanMaxPieceBytes)
+        if (bytes <= (double)max_piece_bytes)
           take(t + kMergeUs + bytes / kPieceBytesPerUs, false, kWhole, (int)tail, pieces);
       }
   }

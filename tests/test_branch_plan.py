@@ -210,3 +210,16 @@ def test_which_kernel_the_tile_tests_reach(d):
 def test_no_rows_no_units():
     units, shared, n_slots, _, _ = plan([], 0)
     assert len(units) == 0 and shared == 0 and n_slots == 0
+
+
+@pytest.mark.parametrize("branches,rows,history,heads,D,elem", [(1000, 257, 8192, 16, 128, 2), (2000, 100, 8192, 16, 128, 2),
+                                                               (2000, 260, 8192, 16, 128, 2), (8192, 64, 8192, 16, 128, 2),
+                                                               (20000, 20, 8192, 16, 128, 2), (100000, 160, 8192, 16, 128, 2),
+                                                               (3000, 300, 4096, 40, 64, 2), (100000, 30, 4096, 16, 32, 4)])
+def test_pieces_of_many_branches_stay_within_their_bound(branches, rows, history, heads, D, elem):
+    seqs = [(rows, 0, history + rows, 1000 * i) for i in range(branches)]
+    units, shared, n_slots, own, _ = plan(seqs, history, kv_heads=heads, D=D, elem=elem)
+    with_pieces = (own[:, 1] > 0).any() or shared > 0
+    assert (n_slots > 0) == with_pieces
+    first = np.flatnonzero(own[:, 1] > 0)[0] if with_pieces and not shared else 0
+    assert int(n_slots) * (branches * rows - int(first)) * heads * (4 * D + 8) <= 4 << 30
