@@ -390,7 +390,7 @@ xc_status xc_lds_dma_rate(int32_t row_bytes, void* stream, double* tbytes_per_s)
  * The conventions above hold, with the pool's stream and device (those of
  * xc_pool_init; another current device is restored before return).  Further:
  *   - XC_ERR_OOM also reports too few free pages or sequence numbers; the
- *     call has then changed nothing.
+ *     call has then changed nothing (xc_batch_set: the batch has no rows).
  *   - The lowest free page and sequence number are always taken first.
  *   - Calls that change tables (xc_seq_extend, xc_seq_import, xc_pool_compact,
  *     xc_batch_set) return XC_ERR_STATE while the stream is being captured.

@@ -269,7 +269,6 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const size_t piece_need = plan.n_slots ? o_stats + stat_rows * sizeof(float2) : 0;
   std::vector<int> seq_copy(seqs, seqs + n);
   b->outgrown.reserve(b->outgrown.size() + 2);
-  b->set = false;  // from here on a failure leaves the batch without rows
 
   if (need > b->dev_bytes) {
     void* d = nullptr;
@@ -518,11 +517,13 @@ xc_status xc_batch_destroy(xc_batch* b) {
 
 xc_status xc_batch_set(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* new_tokens) {
   if (!b || n < 0 || (n > 0 && (!seqs || !new_tokens))) return XC_ERR_INVALID_ARG;
-  return guarded(*b->p, [&]() -> xc_status {
+  const xc_status s = guarded(*b->p, [&]() -> xc_status {
     if (!b->p->book.distinct(n, seqs)) return XC_ERR_INVALID_ARG;
     if (capturing(b->p->st)) return XC_ERR_STATE;
     return set_batch(b, n, seqs, new_tokens);
   });
+  if (s == XC_ERR_OOM || s == XC_ERR_HIP) b->set = false, b->rows = 0;  // wherever it failed
+  return s;
 }
 
 xc_status xc_qk_norm_rope(xc_batch* b, int32_t block, const void* qkv, int64_t ld, const float* gq, const float* gk,

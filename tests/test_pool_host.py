@@ -1,0 +1,97 @@
+"""Failures and memory of the branching cache's host side, forced on the CPU (tests/pool_host.py)."""
+import pytest
+
+import pool_host as host
+from paper_2604_20289_amd.xcache import (XC_ERR_HIP, XC_ERR_INVALID_ARG, XC_ERR_OOM, XC_ERR_STATE, XC_ERR_UNSUPPORTED,
+                                         XC_OK)
+
+pytestmark = pytest.mark.skipif(host.shutil.which("g++") is None, reason="no host compiler")
+
+
+def _grown(pool, n=6, history=5000):
+    parent = pool.new(history)
+    kids = pool.fork(parent, n)
+    assert host.lib().xc_seq_extend(pool.p, n, host.ints(*kids), host.ints(*range(1, n + 1))) == XC_OK
+    return kids
+
+
+@pytest.mark.parametrize("where", ["host", "device"])
+def test_a_batch_that_runs_out_of_memory_has_no_rows(where):
+    """Every allocation of xc_batch_set in turn: either the call is whole, or the batch is without rows."""
+    statuses = []
+    for n in range(200):
+        pool = host.HostPool(n_pages=2000)
+        kids, b = _grown(pool), pool.batch()
+        assert host.set_batch(b, kids[:1], [1]) == XC_OK and host.attention(b) == XC_OK
+        host.lib().fake_faults(*((n, -1) if where == "device" else (-1, n)), -1)
+        status = host.set_batch(b, kids, [1] * len(kids))
+        host.lib().fake_faults(-1, -1, -1)
+        statuses.append(status)
+        if status == XC_ERR_OOM:
+            launches = host.info()["launches"]
+            assert host.attention(b) == XC_ERR_STATE
+            assert host.lib().xc_branch_attention(b, 0, None, 64, 0.0, None, 64) == XC_ERR_STATE
+            assert host.info()["launches"] == launches
+            assert host.set_batch(b, kids, [1] * len(kids)) == XC_OK
+        assert host.attention(b) == XC_OK
+        assert host.lib().xc_batch_destroy(b) == XC_OK
+        assert host.info()["freed_unknown"] == 0 and host.info()["freed_in_use"] == 0 and host.info()["blocks"] == 0
+        pool.close()
+        if status == XC_OK:
+            break
+    assert statuses[-1] == XC_OK and set(statuses[:-1]) == {XC_ERR_OOM} and len(statuses) > (2 if where == "device" else 20)
+
+
+def test_refused_rows_leave_the_earlier_ones():
+    pool = host.HostPool(n_pages=70000, page_tokens=256)
+    s, b = pool.new((1 << 24) + 1), pool.batch()
+    assert host.set_batch(b, [s], [2]) == XC_OK
+    for new, status in (((1 << 24) + 1, XC_ERR_UNSUPPORTED), ((1 << 24) + 2, XC_ERR_INVALID_ARG), (-1, XC_ERR_INVALID_ARG)):
+        assert host.set_batch(b, [s], [new]) == status
+        assert host.attention(b) == XC_OK
+    host.lib().xc_batch_destroy(b)
+    pool.close()
+
+
+def test_a_failed_launch_sticks():
+    pool = host.HostPool(n_pages=2000)
+    kids, b = _grown(pool), pool.batch()
+    host.lib().fake_faults(-1, -1, 0)
+    assert host.set_batch(b, kids, [1] * len(kids)) == XC_ERR_HIP
+    assert host.attention(b) == XC_ERR_HIP and host.set_batch(b, kids, [1] * len(kids)) == XC_ERR_HIP
+    assert host.lib().xc_batch_destroy(b) == XC_OK
+    pool.close()
+
+
+def test_tables_are_unchanged_where_the_host_runs_out_of_memory():
+    """Every allocation of a fork, a growth, a free and a compaction in turn."""
+    pool = host.HostPool(n_pages=400, max_seqs=40)
+    kids = _grown(pool, history=37)
+    lib, n = host.lib(), len(kids)
+
+    def tables():
+        out = []
+        for s in range(40):
+            first, tokens, count, pages = host.ints(0), host.ints(0), (host.ctypes.c_size_t * 1)(), host.ints(*[0] * 400)
+            if lib.xc_seq_pages(pool.p, s, first, tokens, pages, 400, count) == XC_OK:
+                out.append((s, first[0], tokens[0], list(pages[:count[0]])))
+        live = [host.ctypes.c_int32() for _ in range(3)]
+        assert lib.xc_pool_info(pool.p, *map(host.ctypes.byref, live)) == XC_OK
+        return out, [x.value for x in live]
+
+    assert lib.xc_seq_free(pool.p, 1, host.ints(kids[0])) == XC_OK  # leaves a hole to compact into
+    kids, n = kids[1:], n - 1
+    for call in (lambda: lib.xc_seq_fork(pool.p, kids[0], 3, host.ints(0, 0, 0)),
+                 lambda: lib.xc_seq_extend(pool.p, n, host.ints(*kids), host.ints(*[20] * n)),
+                 lambda: lib.xc_seq_free(pool.p, 2, host.ints(kids[0], kids[2])),
+                 lambda: lib.xc_pool_compact(pool.p, None)):
+        before = tables()
+        for i in range(100):
+            lib.fake_faults(-1, i, -1)
+            status = call()
+            lib.fake_faults(-1, -1, -1)
+            if status == XC_OK:
+                break
+            assert status == XC_ERR_OOM and tables() == before
+        assert status == XC_OK and 0 < i < 100
+    pool.close()
