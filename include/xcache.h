@@ -486,7 +486,8 @@ xc_status xc_batch_destroy(xc_batch* batch);
 
 /* The rows of the batch: the last new_tokens[i] (0 to all) tokens of seqs[i]
  * (distinct), packed in this order, at most 2^24 rows.  Uploads the tables
- * and plans the attention; may allocate.  Valid until the table of one of
+ * and plans the attention; allocates where the batch has to hold more than
+ * before, then waiting for the stream.  Valid until the table of one of
  * the sequences changes (extend, trim, free, compact, import; a fork of it
  * changes nothing): the calls below then return XC_ERR_STATE.  After
  * XC_ERR_OOM or XC_ERR_HIP the batch has no rows.

@@ -4,8 +4,8 @@
 // Device state of a batch: the page tables of its sequences, the attention's
 // units and, per row, the place its token has in the pages and the slots of
 // its pieces; and the pieces themselves.  Tables go up from pinned memory on
-// the pool's stream.  Buffers that became too small are kept until the batch
-// is destroyed: work enqueued or captured before still names them.
+// the pool's stream.  A buffer that became too small goes once the work before
+// is done (a graph captured before is not replayed after a new xc_batch_set).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -134,7 +134,6 @@ struct xc_batch {
   size_t dev_bytes = 0;
   char* pieces = nullptr;
   size_t piece_bytes = 0;
-  std::vector<void*> outgrown;
   char* pinned = nullptr;
   size_t pinned_bytes = 0;
   hipEvent_t uploaded = nullptr;
@@ -197,6 +196,26 @@ RopeFreqs rope_freqs(int d, int axes, double theta) {
   return f;
 }
 
+// Device memory of at least `need` bytes at buf, its contents lost; false: there is none.  Work before may still use the
+// smaller buffer, and is waited for.
+bool enlarge(Pool& p, char*& buf, size_t& have, size_t need, size_t reserve) {
+  if (need <= have) return true;
+  if (buf) {
+    XC_HIP(hipStreamSynchronize(p.st));
+    char* old = buf;
+    buf = nullptr;
+    have = 0;
+    XC_HIP(hipFree(old));
+  }
+  void* d = nullptr;
+  const hipError_t e = hipMalloc(&d, need + reserve);
+  if (e == hipErrorOutOfMemory) return (void)hipGetLastError(), false;
+  XC_HIP(e);
+  buf = (char*)d;
+  have = need + reserve;
+  return true;
+}
+
 xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* new_tokens) {
   Pool& p = *b->p;
   const PageBook& book = p.book;
@@ -247,10 +266,21 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   if (tables.size() > (size_t)kMaxPlaces) return XC_ERR_UNSUPPORTED;
   const int group = p.cfg.q_heads / p.cfg.kv_heads;
   const PlanShape shape{group, p.cfg.kv_heads, p.cfg.head_dim, p.esz, p.cus};
-  const AttnPlan plan = plan_attention(plan_seqs, (int)(shared << shift), shape);
-  const long long threads = std::max(((long long)plan.units.size() * p.cfg.kv_heads + kXcds * kXcds) * 512,
-                                     plan.n_slots ? rows * p.cfg.q_heads * (p.cfg.head_dim / 4) : 0);
-  if (threads >> 32) return XC_ERR_UNSUPPORTED;  // more than a launch takes
+  AttnPlan plan = plan_attention(plan_seqs, (int)(shared << shift), shape);
+  auto launches = [&] {  // a launch takes fewer than 2^32 threads
+    const long long threads = std::max(((long long)plan.units.size() * p.cfg.kv_heads + kXcds * kXcds) * 512,
+                                       plan.n_slots ? rows * p.cfg.q_heads * (p.cfg.head_dim / 4) : 0);
+    return threads >> 32 == 0;
+  };
+  if (!launches()) return XC_ERR_UNSUPPORTED;
+  // pieces [slot][row][head][D], then their statistics
+  auto stat_rows = [&] { return (size_t)plan.n_slots * (rows - plan.piece_row0) * p.cfg.q_heads; };
+  auto stats_at = [&] { return align256(stat_rows() * p.cfg.head_dim * sizeof(float)); };
+  const size_t piece_need = plan.n_slots ? stats_at() + stat_rows() * sizeof(float2) : 0;
+  if (!enlarge(p, b->pieces, b->piece_bytes, piece_need, piece_need / 4)) {
+    plan = plan_attention(plan_seqs, (int)(shared << shift), shape, 0);  // no memory: without pieces
+    if (!launches()) return XC_ERR_OOM;
+  }
   for (const PlanPart& part : plan.parts) {
     const PlanSeq& q = plan_seqs[part.seq];
     const int at = q.first + q.tokens - q.rows + (part.tok0 - first_row[part.seq]);
@@ -263,27 +293,9 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const size_t up = o_units + align256(plan.units.size() * sizeof(AttnUnit));
   const size_t o_own = up + align256(rows * sizeof(int));
   const size_t need = o_own + align256(rows * sizeof(OwnSlots));
-  const long long piece_rows = rows - plan.piece_row0;
-  const size_t stat_rows = (size_t)plan.n_slots * piece_rows * p.cfg.q_heads;
-  const size_t o_stats = align256(stat_rows * p.cfg.head_dim * sizeof(float));
-  const size_t piece_need = plan.n_slots ? o_stats + stat_rows * sizeof(float2) : 0;
   std::vector<int> seq_copy(seqs, seqs + n);
-  b->outgrown.reserve(b->outgrown.size() + 2);
 
-  if (need > b->dev_bytes) {
-    void* d = nullptr;
-    XC_HIP(hipMalloc(&d, need + need / 2));
-    if (b->dev) b->outgrown.push_back(b->dev);
-    b->dev = (char*)d;
-    b->dev_bytes = need + need / 2;
-  }
-  if (piece_need > b->piece_bytes) {
-    void* d = nullptr;
-    XC_HIP(hipMalloc(&d, piece_need + piece_need / 4));
-    if (b->pieces) b->outgrown.push_back(b->pieces);
-    b->pieces = (char*)d;
-    b->piece_bytes = piece_need + piece_need / 4;
-  }
+  if (!enlarge(p, b->dev, b->dev_bytes, need, need / 2)) return XC_ERR_OOM;
   if (b->upload_pending) {  // the staging memory is being read
     XC_HIP(hipEventSynchronize(b->uploaded));
     b->upload_pending = false;
@@ -315,14 +327,14 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   a.n_long = long_units(plan.units);
   a.group = group;
   a.pieces = (float*)b->pieces;
-  a.stats = (float2*)(b->pieces + o_stats);
+  a.stats = (float2*)(b->pieces + stats_at());
   a.own = (const OwnSlots*)(b->dev + o_own);
   a.shared_slots = plan.shared_slots;
   a.rows = (int)rows;
   a.q_heads = p.cfg.q_heads;
   a.n_slots = plan.n_slots;
   a.piece_row0 = plan.piece_row0;
-  a.piece_rows = (int)piece_rows;
+  a.piece_rows = (int)rows - plan.piece_row0;
   a.few = plan.few;
   b->place = (const int*)(b->dev + up);
   b->rows = (int)rows;
@@ -504,7 +516,6 @@ xc_status xc_batch_destroy(xc_batch* b) {
   try {
     const DeviceScope scope(b->p->device);
     if (b->dev || b->pieces || b->pinned) (void)hipStreamSynchronize(b->p->st);
-    for (void* d : b->outgrown) (void)hipFree(d);
     if (b->dev) (void)hipFree(b->dev);
     if (b->pieces) (void)hipFree(b->pieces);
     if (b->pinned) (void)hipHostFree(b->pinned);

@@ -121,7 +121,8 @@ void fake_faults(int dev, int host, int kernel) { device_fails = dev, new_fails 
 void fake_memory(u64 most) { most_bytes = most; }
 u64 fake_info(int what) {
   const u64 v[] = {live_bytes, peak_bytes, (u64)freed_in_use, (u64)freed_unknown, blocks->size(), (u64)device,
-                   (u64)calls->size(), (u64)last_attention.n_slots, (u64)(calls->empty() ? -1 : calls->back())};
+                   (u64)calls->size(), (u64)last_attention.n_slots, (u64)(calls->empty() ? -1 : calls->back()),
+                   (u64)(device_fails >= 0 || new_fails >= 0)};
   return v[what];
 }
 }
@@ -151,7 +152,8 @@ hipError_t launch_branch_attention(int, const AttnArgs& a, hipStream_t) {
 HandleWindow handle_window(const xc_handle*) { return {}; }
 }  // namespace xc
 """
-INFO = ("live_bytes", "peak_bytes", "freed_in_use", "freed_unknown", "blocks", "device", "launches", "n_slots", "last_launch")
+INFO = ("live_bytes", "peak_bytes", "freed_in_use", "freed_unknown", "blocks", "device", "launches", "n_slots", "last_launch",
+        "fault_ahead")
 
 
 @functools.lru_cache(None)

@@ -17,7 +17,8 @@ def _grown(pool, n=6, history=5000):
 
 @pytest.mark.parametrize("where", ["host", "device"])
 def test_a_batch_that_runs_out_of_memory_has_no_rows(where):
-    """Every allocation of xc_batch_set in turn: either the call is whole, or the batch is without rows."""
+    """Every allocation of xc_batch_set in turn: either the call is whole (for pieces there is another way), or the batch is
+    without rows."""
     statuses = []
     for n in range(200):
         pool = host.HostPool(n_pages=2000)
@@ -25,6 +26,7 @@ def test_a_batch_that_runs_out_of_memory_has_no_rows(where):
         assert host.set_batch(b, kids[:1], [1]) == XC_OK and host.attention(b) == XC_OK
         host.lib().fake_faults(*((n, -1) if where == "device" else (-1, n)), -1)
         status = host.set_batch(b, kids, [1] * len(kids))
+        through = host.info()["fault_ahead"]
         host.lib().fake_faults(-1, -1, -1)
         statuses.append(status)
         if status == XC_ERR_OOM:
@@ -37,9 +39,12 @@ def test_a_batch_that_runs_out_of_memory_has_no_rows(where):
         assert host.lib().xc_batch_destroy(b) == XC_OK
         assert host.info()["freed_unknown"] == 0 and host.info()["freed_in_use"] == 0 and host.info()["blocks"] == 0
         pool.close()
-        if status == XC_OK:
+        if through:
             break
-    assert statuses[-1] == XC_OK and set(statuses[:-1]) == {XC_ERR_OOM} and len(statuses) > (2 if where == "device" else 20)
+    if where == "device":  # pieces, tables, staging memory
+        assert statuses == [XC_OK, XC_ERR_OOM, XC_ERR_OOM, XC_OK]
+    else:
+        assert statuses[-1] == XC_OK and set(statuses[:-1]) == {XC_ERR_OOM} and len(statuses) > 20
 
 
 def test_refused_rows_leave_the_earlier_ones():
@@ -94,4 +99,47 @@ def test_tables_are_unchanged_where_the_host_runs_out_of_memory():
                 break
             assert status == XC_ERR_OOM and tables() == before
         assert status == XC_OK and 0 < i < 100
+    pool.close()
+
+
+def test_buffers_that_became_too_small_are_released():
+    """A batch that grows step by step holds what it needs and a reserve, and nothing goes while work reads it."""
+    pool = host.HostPool(n_pages=30000, q_heads=8, kv_heads=8, head_dim=128, max_seqs=400)
+    parent, b = pool.new(9000), pool.batch()
+    kids = pool.fork(parent, 300)
+    assert host.lib().xc_seq_extend(pool.p, 300, host.ints(*kids), host.ints(*[20] * 300)) == XC_OK
+    fresh = {}
+    for n in range(2, 300, 20):  # what a batch of its own takes
+        one, before = pool.batch(), host.info()["live_bytes"]
+        assert host.set_batch(one, kids[:n], [1] * n) == XC_OK
+        fresh[n] = host.info()["live_bytes"] - before
+        host.lib().xc_batch_destroy(one)
+    assert host.info()["live_bytes"] == 0
+    most = 0
+    for n in range(2, 300, 20):
+        assert host.set_batch(b, kids[:n], [1] * n) == XC_OK and host.attention(b, 8 * 128) == XC_OK
+        assert host.info()["n_slots"] > 0
+        most = max(most, fresh[n])
+        assert host.info()["live_bytes"] <= 1.25 * most
+    assert host.info()["freed_in_use"] == 0 and host.info()["freed_unknown"] == 0
+    host.lib().xc_batch_destroy(b)
+    assert host.info()["live_bytes"] == 0 and host.info()["freed_in_use"] == 0
+    pool.close()
+
+
+def test_without_memory_for_pieces_the_rows_go_without():
+    pool = host.HostPool(n_pages=30000, q_heads=8, kv_heads=8, head_dim=128, max_seqs=400)
+    parent, b = pool.new(9000), pool.batch()
+    kids = pool.fork(parent, 300)
+    assert host.lib().xc_seq_extend(pool.p, 300, host.ints(*kids), host.ints(*[20] * 300)) == XC_OK
+    assert host.set_batch(b, kids, [1] * 300) == XC_OK and host.attention(b, 8 * 128) == XC_OK
+    assert host.info()["n_slots"] > 0
+    pieces = 300 * 8 * (4 * 128 + 8)
+    host.lib().xc_batch_destroy(b)
+    b = pool.batch()
+    tables = 4 * 300 * (-(-9020 // 16)) * 3  # table entries, and room for what else a row and a unit need
+    host.lib().fake_memory(tables + 2 * pieces - 1)
+    assert host.set_batch(b, kids, [1] * 300) == XC_OK and host.attention(b, 8 * 128) == XC_OK
+    assert host.info()["n_slots"] == 0
+    host.lib().xc_batch_destroy(b)
     pool.close()
