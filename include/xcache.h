@@ -399,6 +399,8 @@ xc_status xc_lds_dma_rate(int32_t row_bytes, void* stream, double* tbytes_per_s)
  *     alive and neither the batch nor its sequences' tables have changed, one
  *     replay or call of one batch at a time.  Two batches share nothing but
  *     the pool.
+ *   - Inputs and results of a call do not overlap; rows of one stride may
+ *     lie beside each other in one buffer.
  *   - A pool and its batches are used by one thread at a time; a batch may
  *     outlive xc_pool_destroy. */
 

@@ -88,7 +88,7 @@ struct Pool {
   // whether bytes lie in the page buffers
   bool holds(const void* x, size_t n) const {
     const size_t bytes = (size_t)block_elems() * cfg.n_blocks * esz;
-    return overlap(x, n, keys, bytes) || overlap(x, n, values, bytes);
+    return n > 0 && (overlap(x, n, keys, bytes) || overlap(x, n, values, bytes));
   }
   PageBuf block(int b) const {
     const long long o = b * block_elems() * esz;
@@ -178,9 +178,21 @@ void committed(F&& f) {
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// bytes from the first element of [rows][ld] to the end of its last row
-size_t extent(long long rows, long long ld, long long width, int esz) {
-  return rows > 0 ? (size_t)((rows - 1) * ld + width) * esz : 0;
+// A caller's [rows][ld], `width` elements of each row in use; all in bytes.
+struct Rows {
+  uintptr_t at;
+  size_t pitch, width, extent;  // extent: to the end of the last row
+};
+Rows rows_at(const void* p, long long rows, long long ld, long long width, int esz) {
+  return {reinterpret_cast<uintptr_t>(p), (size_t)ld * esz, (size_t)width * esz,
+          rows > 0 ? (size_t)((rows - 1) * ld + width) * esz : 0};
+}
+// Rows of one stride may lie beside each other in a buffer; others are told apart by where they begin and end.
+bool overlap(const Rows& a, const Rows& b) {
+  if (a.at >= b.at + b.extent || b.at >= a.at + a.extent) return false;
+  if (a.pitch != b.pitch) return true;
+  const size_t from = b.at >= a.at ? (b.at - a.at) % a.pitch : (a.pitch - (a.at - b.at) % a.pitch) % a.pitch;
+  return from < a.width || from + b.width > a.pitch;
 }
 
 RopeFreqs rope_freqs(int d, int axes, double theta) {
@@ -549,9 +561,8 @@ xc_status xc_qk_norm_rope(xc_batch* b, int32_t block, const void* qkv, int64_t l
   if (positions && ((n_axes != 1 && n_axes != 3) || !std::isfinite(theta) || theta <= 1.0)) return XC_ERR_INVALID_ARG;
   return guarded(p, [&]() -> xc_status {
     if (!b->current()) return XC_ERR_STATE;
-    const size_t in_bytes = extent(b->rows, ld, width, p.esz), out_bytes = extent(b->rows, q_ld, q_width, p.esz);
-    if (overlap(qkv, in_bytes, q_out, out_bytes) || p.holds(qkv, in_bytes) || p.holds(q_out, out_bytes))
-      return XC_ERR_INVALID_ARG;
+    const Rows in = rows_at(qkv, b->rows, ld, width, p.esz), to = rows_at(q_out, b->rows, q_ld, q_width, p.esz);
+    if (overlap(in, to) || p.holds(qkv, in.extent) || p.holds(q_out, to.extent)) return XC_ERR_INVALID_ARG;
     // a page that another sequence reads too is not written
     for (int page : b->written)
       if (p.book.refs(page) > 1) return XC_ERR_STATE;
@@ -590,8 +601,8 @@ xc_status xc_branch_attention(xc_batch* b, int32_t block, const void* q, int64_t
   if (!(scale >= 0.f) || !std::isnormal(log2_scale)) return XC_ERR_INVALID_ARG;
   return guarded(p, [&]() -> xc_status {
     if (!b->current()) return XC_ERR_STATE;
-    const size_t in_bytes = extent(b->rows, q_ld, width, p.esz), out_bytes = extent(b->rows, out_ld, width, p.esz);
-    if (overlap(q, in_bytes, out, out_bytes) || p.holds(out, out_bytes)) return XC_ERR_INVALID_ARG;
+    const Rows in = rows_at(q, b->rows, q_ld, width, p.esz), to = rows_at(out, b->rows, out_ld, width, p.esz);
+    if (overlap(in, to) || p.holds(out, to.extent)) return XC_ERR_INVALID_ARG;
     if (b->rows == 0) return XC_OK;
     AttnArgs a = b->attn;
     a.q = q;

@@ -143,3 +143,34 @@ def test_without_memory_for_pieces_the_rows_go_without():
     assert host.info()["n_slots"] == 0
     host.lib().xc_batch_destroy(b)
     pool.close()
+
+
+def test_columns_of_one_buffer_are_no_overlap():
+    """Rows of one stride that lie beside each other are taken, in either order; any byte in common is refused."""
+    pool = host.HostPool(q_heads=4, kv_heads=2, head_dim=64)  # q and out rows of 256 elements, qkv rows of 512
+    s, b = pool.new(9), pool.batch()
+    assert host.set_batch(b, [s], [7]) == XC_OK
+    lib, at = host.lib(), host.ROWS
+
+    def attention(q, out, q_ld, out_ld):
+        return lib.xc_branch_attention(b, 0, at + 2 * q, q_ld, 0.0, at + 2 * out, out_ld)
+
+    def norms(qkv, ld, q, q_ld):
+        return lib.xc_qk_norm_rope(b, 0, at + 2 * qkv, ld, 16, 16, None, 1, 2.0, at + 2 * q, q_ld)
+
+    for q, out in ((0, 256), (256, 0), (0, 512 - 256), (8, 264), (0, 512 + 256), (512 + 256, 0), (0, 7 * 512)):
+        assert attention(q, out, 512, 512) == XC_OK, (q, out)
+    for q, out in ((0, 0), (0, 248), (248, 0), (0, 264), (264, 0), (0, 512), (512, 0), (0, 512 + 248), (0, 6 * 512 + 248)):
+        assert attention(q, out, 512, 512) == XC_ERR_INVALID_ARG, (q, out)
+    # of other strides: none of one's bytes between the first and the last of the other's
+    assert attention(0, 256, 512, 520) == XC_ERR_INVALID_ARG
+    assert attention(0, 6 * 512 + 256, 512, 520) == XC_OK and attention(6 * 520 + 256, 0, 512, 520) == XC_OK
+    for qkv, q in ((0, 512), (256, 0), (256, 768), (0, 768 + 512)):
+        assert norms(qkv, 768, q, 768) == XC_OK, (qkv, q)
+    for qkv, q in ((0, 504), (0, 520), (0, 768), (264, 0), (248, 0), (0, 0)):
+        assert norms(qkv, 768, q, 768) == XC_ERR_INVALID_ARG, (qkv, q)
+    # the page buffers, whole
+    pages = host.KEYS - at
+    assert norms(0, 512, pages // 2, 256) == XC_ERR_INVALID_ARG and attention(0, pages // 2 + 64, 256, 256) == XC_ERR_INVALID_ARG
+    lib.xc_batch_destroy(b)
+    pool.close()
