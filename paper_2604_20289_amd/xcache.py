@@ -522,6 +522,15 @@ class Pool:
             pass
 
 
+_LATER: list = []  # batches whose owner went while their stream was captured
+
+
+def _release_later():
+    """Destroy the batches that could not be then and can be now."""
+    lib = load_library()
+    _LATER[:] = [b for b in _LATER if lib.xc_batch_destroy(b) != XC_OK]
+
+
 class Batch:
     """Rows of a pool's sequences: their norms and rotation, their attention
     (see xc_batch_set, xc_qk_norm_rope, xc_branch_attention)."""
@@ -536,9 +545,13 @@ class Batch:
         self._dtype, self._device = pool.keys.dtype, pool.keys.get_device()
         lib = load_library()
         self._norm_rope, self._attention = lib.xc_qk_norm_rope, lib.xc_branch_attention
+        if _LATER:
+            _release_later()
         self.b = xc_batch_init(pool.p)
 
     def set(self, seqs, new_tokens):
+        if _LATER:
+            _release_later()
         try:
             xc_batch_set(self.b, seqs, new_tokens)
         except XCacheError as e:
@@ -576,12 +589,15 @@ class Batch:
         if self.b:
             xc_batch_destroy(self.b)
             self.b = 0
+        if _LATER:
+            _release_later()
 
     def __del__(self):
         try:
             self.close()
         except Exception:
-            pass
+            if self.b:
+                _LATER.append(self.b)
 
 
 class XCache:

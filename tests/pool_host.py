@@ -15,6 +15,7 @@ from paper_2604_20289_amd import build, xcache
 
 SHIM = r"""
 #include "xc_pool.h"
+#include "xcache.h"
 #include <cstdlib>
 #include <map>
 #include <new>
@@ -29,7 +30,7 @@ struct Block { u64 bytes, used; };
 static std::map<u64, Block>* blocks;
 static std::map<void*, u64>* events;
 static std::vector<int>* calls;
-static int freed_in_use, freed_unknown;
+static int freed_in_use, freed_unknown, launched_on = -1;
 static u64 live_bytes, peak_bytes;
 static AttnArgs last_attention;
 
@@ -52,6 +53,7 @@ static void use(const void* p) {
 static hipError_t launch(int kind) {
   if (counts_down(launch_fails)) return hipErrorLaunchFailure;
   ++launched;
+  launched_on = device;
   calls->push_back(kind);
   return hipSuccess;
 }
@@ -122,7 +124,7 @@ void fake_memory(u64 most) { most_bytes = most; }
 u64 fake_info(int what) {
   const u64 v[] = {live_bytes, peak_bytes, (u64)freed_in_use, (u64)freed_unknown, blocks->size(), (u64)device,
                    (u64)calls->size(), (u64)last_attention.n_slots, (u64)(calls->empty() ? -1 : calls->back()),
-                   (u64)(device_fails >= 0 || new_fails >= 0)};
+                   (u64)(device_fails >= 0 || new_fails >= 0), (u64)launched_on};
   return v[what];
 }
 }
@@ -151,9 +153,10 @@ hipError_t launch_branch_attention(int, const AttnArgs& a, hipStream_t) {
 }
 HandleWindow handle_window(const xc_handle*) { return {}; }
 }  // namespace xc
+extern "C" const char* xc_status_string(xc_status) { return "refused"; }
 """
 INFO = ("live_bytes", "peak_bytes", "freed_in_use", "freed_unknown", "blocks", "device", "launches", "n_slots", "last_launch",
-        "fault_ahead")
+        "fault_ahead", "launched_on")
 
 
 @functools.lru_cache(None)
@@ -227,3 +230,31 @@ def set_batch(b, seqs, new):
 
 def attention(b, width=64, q=ROWS, out=ROWS + (1 << 38), block=0):
     return lib().xc_branch_attention(b, block, q, width, 0.0, out, width)
+
+
+class Tensor:
+    """What the binding asks of a page buffer."""
+
+    class Device:
+        type = "cuda"
+
+        def __init__(self, index):
+            self.index = index
+
+        def __eq__(self, other):
+            return self.index == other.index
+
+    def __init__(self, at, shape, device=0):
+        self.at, self.shape, self.dtype, self.device = at, shape, "torch.bfloat16", Tensor.Device(device)
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.at
+
+    def get_device(self):
+        return self.device.index

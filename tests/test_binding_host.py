@@ -1,0 +1,71 @@
+"""Pool and Batch of the binding over the host side of the cache (tests/pool_host.py), on the CPU."""
+import contextlib
+import gc
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import pool_host as host  # noqa: E402
+from paper_2604_20289_amd import xcache  # noqa: E402
+from paper_2604_20289_amd.xcache import Batch, Pool, XCacheError  # noqa: E402
+
+pytestmark = pytest.mark.skipif(host.shutil.which("g++") is None, reason="no host compiler")
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    out = host.lib()
+    out.xc_status_string.restype = xcache.load_library().xc_status_string.restype
+    out.fake_reset()
+    monkeypatch.setattr(xcache, "_lib", out)
+
+    @contextlib.contextmanager
+    def on(device):
+        before = host.info()["device"]
+        out.fake_set(device.index, 0)
+        yield
+        out.fake_set(before, 0)
+
+    monkeypatch.setattr(torch.cuda, "device", on)
+    yield out
+    gc.collect()
+    out.fake_set(0, 0)
+
+
+def pool(device=0, **kw):
+    shape = (1, 64, 2, 16, 64)
+    return Pool(host.Tensor(host.KEYS, shape, device), host.Tensor(host.VALUES, shape, device), q_heads=2, **kw)
+
+
+def test_a_batch_collected_during_a_capture_is_released_after_it(lib):
+    p = pool()
+    s = p.new()
+    p.extend([s], [5])
+    lost, kept = Batch(p), Batch(p)
+    lost.set([s], [2])
+    kept.set([s], [1])
+    each = host.info()["live_bytes"] // 2
+    lib.fake_set(0, 1)
+    with pytest.raises(XCacheError) as e:  # asked for by name it is refused, and the batch stays
+        kept.close()
+    assert e.value.status == xcache.XC_ERR_STATE and kept.b
+    del lost
+    gc.collect()
+    assert host.info()["live_bytes"] == 2 * each
+    lib.fake_set(0, 0)
+    kept.set([s], [2])
+    assert host.info()["live_bytes"] == each and host.info()["freed_in_use"] == 0
+    kept.close()
+    assert host.info()["live_bytes"] == 0
+    # the last one of all: whatever comes next releases it
+    last = Batch(p)
+    last.set([s], [1])
+    lib.fake_set(0, 1)
+    del last
+    gc.collect()
+    assert host.info()["live_bytes"] > 0
+    lib.fake_set(0, 0)
+    Batch(p)
+    gc.collect()
+    assert host.info()["live_bytes"] == 0 and host.info()["freed_unknown"] == 0
