@@ -467,7 +467,9 @@ class Pool:
         self._head = _ints((0, 0, 0, 0))  # first, tokens, pages (64 bits)
         at = _at(self._head)
         self._heads = at, at + 4, at + 8
-        self.p = xc_pool_init(c, keys, values, stream)
+        import torch
+        with torch.cuda.device(keys.device):  # the pool's device is the current one
+            self.p = xc_pool_init(c, keys, values, stream)
 
     def new(self) -> int:
         return xc_seq_new(self.p)

@@ -69,3 +69,15 @@ def test_a_batch_collected_during_a_capture_is_released_after_it(lib):
     Batch(p)
     gc.collect()
     assert host.info()["live_bytes"] == 0 and host.info()["freed_unknown"] == 0
+
+
+def test_a_pool_is_on_the_device_of_its_buffers(lib):
+    """Another device is current when the pool is made: its work goes to the buffers' device, and the other stays current."""
+    lib.fake_set(0, 0)
+    p = pool(device=3)
+    assert host.info()["device"] == 0
+    s = p.new()
+    p.extend([s], [5])
+    kid, = p.fork(s, 1)
+    p.extend([kid], [1])  # a copy of the shared page
+    assert host.info()["launches"] == 1 and host.info()["launched_on"] == 3 and host.info()["device"] == 0
