@@ -38,7 +38,6 @@ class PageBook {
   int shift() const { return shift_; }
   int live_pages() const { return live_; }
   int live_seqs() const { return used_; }
-  int max_seqs() const { return (int)seqs_.size(); }
   int refs(int page) const { return refs_[page]; }
   bool valid(int s) const { return s >= 0 && s < (int)seqs_.size() && seqs_[s].used; }
   const PageSeq& seq(int s) const { return seqs_[s]; }
@@ -180,13 +179,6 @@ class PageBook {
         if (to[p] >= 0) p = to[p], moved = true;
       if (moved) q.version = ++versions_;
     }
-  }
-
-  // the place (page * page size + row) of token i of sequence s
-  long long place(int s, int i) const {
-    const PageSeq& q = seqs_[s];
-    const long long at = (long long)q.first + i;
-    return ((long long)q.pages[at >> shift_] << shift_) + (at & (page() - 1));
   }
 
  private:

@@ -318,12 +318,6 @@ def xc_pool_info(pool: int) -> dict:
     return dict(zip(("live_pages", "free_pages", "live_seqs"), (x.value for x in v)))
 
 
-def xc_pool_compact(pool: int) -> int:
-    moved = ctypes.c_int32()
-    _check(load_library().xc_pool_compact(pool, ctypes.byref(moved)), "xc_pool_compact")
-    return moved.value
-
-
 def _ints(x) -> array.array:
     return array.array("i", x)  # 32 bits
 
@@ -338,26 +332,8 @@ def xc_seq_new(pool: int) -> int:
     return seq.value
 
 
-def xc_seq_fork(pool: int, src: int, n: int) -> list:
-    out = _ints(bytes(4 * max(n, 0)))
-    _check(load_library().xc_seq_fork(pool, src, n, _at(out)), "xc_seq_fork")
-    return out.tolist()
-
-
-def xc_seq_extend(pool: int, seqs: Sequence[int], tokens: Sequence[int]):
-    if len(seqs) != len(tokens):
-        raise ValueError("one token count per sequence")
-    s, t = _ints(seqs), _ints(tokens)
-    _check(load_library().xc_seq_extend(pool, len(s), _at(s), _at(t)), "xc_seq_extend")
-
-
 def xc_seq_trim(pool: int, seq: int, front: int, back: int):
     _check(load_library().xc_seq_trim(pool, seq, front, back), "xc_seq_trim")
-
-
-def xc_seq_free(pool: int, seqs: Sequence[int]):
-    s = _ints(seqs)
-    _check(load_library().xc_seq_free(pool, len(s), _at(s)), "xc_seq_free")
 
 
 def xc_seq_import(pool: int, seq: int, h: int):
@@ -393,17 +369,6 @@ def xc_batch_set(batch: int, seqs: Sequence[int], new_tokens: Sequence[int]):
         raise ValueError("one token count per sequence")
     s, t = _ints(seqs), _ints(new_tokens)
     _check(load_library().xc_batch_set(batch, len(s), _at(s), _at(t)), "xc_batch_set")
-
-
-def xc_qk_norm_rope(batch: int, block: int, qkv, ld: int, gq, gk, positions, n_axes: int, theta: float, q_out,
-                    q_ld: int):
-    _check(load_library().xc_qk_norm_rope(batch, block, _ptr(qkv), ld, _ptr(gq), _ptr(gk), _ptr(positions), n_axes,
-                                          theta, _ptr(q_out), q_ld), "xc_qk_norm_rope")
-
-
-def xc_branch_attention(batch: int, block: int, q, q_ld: int, scale: float, out, out_ld: int):
-    _check(load_library().xc_branch_attention(batch, block, _ptr(q), q_ld, scale, _ptr(out), out_ld),
-           "xc_branch_attention")
 
 
 def _tensor_dtype(t) -> int:
