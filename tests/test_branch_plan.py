@@ -223,3 +223,13 @@ def test_pieces_of_many_branches_stay_within_their_bound(branches, rows, history
     assert (n_slots > 0) == with_pieces
     first = np.flatnonzero(own[:, 1] > 0)[0] if with_pieces and not shared else 0
     assert int(n_slots) * (branches * rows - int(first)) * heads * (4 * D + 8) <= 4 << 30
+
+
+def test_which_kernels_the_edge_tests_reach():
+    """The shapes of tests/test_gpu_branch_edges.py."""
+    for D in (64, 128):
+        for rows, kv, n in ((90, 256, 3), (90, 256, 1), (70, 256, 1), (257, 256, 1)):
+            assert plan([(rows, 0, 300 + rows, 1000 * i) for i in range(n)], 0, kv_heads=kv, D=D)[4] == 256
+        for rows, n in ((21, 3), (7, 3), (3, 3), (21, 1)):
+            assert plan([(rows, 3, 297 + rows, 1000 * i) for i in range(n)], 128 if n > 1 else 0, kv_heads=1, D=D)[4] == 64
+        assert plan([(90, 3, 297 + 90, 1000 * i) for i in range(3)], 128, kv_heads=256, D=D)[4] == 256
