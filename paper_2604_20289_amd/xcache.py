@@ -563,7 +563,7 @@ class Batch:
         try:
             self.close()
         except Exception:
-            if self.b:
+            if self.b and _LATER is not None:  # (the program may be ending)
                 _LATER.append(self.b)
 
 

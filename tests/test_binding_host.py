@@ -1,6 +1,9 @@
 """Pool and Batch of the binding over the host side of the cache (tests/pool_host.py), on the CPU."""
 import contextlib
 import gc
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -81,3 +84,26 @@ def test_a_pool_is_on_the_device_of_its_buffers(lib):
     kid, = p.fork(s, 1)
     p.extend([kid], [1])  # a copy of the shared page
     assert host.info()["launches"] == 1 and host.info()["launched_on"] == 3 and host.info()["device"] == 0
+
+
+def test_batches_alive_at_the_end_of_the_program_end_quietly():
+    code = """
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import torch, contextlib
+import pool_host as host
+from paper_2604_20289_amd import xcache
+lib = host.lib()
+xcache._lib = lib
+torch.cuda.device = lambda d: contextlib.nullcontext()
+shape = (1, 64, 2, 16, 64)
+p = xcache.Pool(host.Tensor(host.KEYS, shape), host.Tensor(host.VALUES, shape), q_heads=2)
+s = p.new()
+p.extend([s], [5])
+b = xcache.Batch(p)
+b.set([s], [2])
+import builtins
+builtins.held = b  # outlives the module
+""".format(root=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), tests=os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stderr == "", r.stderr
