@@ -224,3 +224,37 @@ def test_an_attention_captured_after_refused_changes_is_right():
             batch.attention(0, q, eager)
             st.synchronize()
             assert torch.equal(out, eager)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_chunk_of_more_pages_than_one_launch_fills(dtype):
+    """15 635 tokens behind nine others, in pages of 16: the second launch begins at an odd token."""
+    import synth
+    from paper_2604_20289_amd.xcache import XC_CACHE_KEYS, XC_CACHE_VALUES, XCache
+    w = synth.workload(0)
+    d = 64 if dtype == "bf16" else 32
+    w = synth.with_model(w, rope=1, kv_window=2, n_heads=2, head_dim=d, hidden=2 * d, mlp_hidden=128, dtype=dtype, n_blocks=2,
+                         groups=(synth.ViewGroup(1, 5, 59, 53),))
+    m = w.model
+    L = m.tokens
+    h = XCache(m, w.gate, synth.make_weights(m), torch.cuda.current_stream().cuda_stream)
+    (e,), (a,) = synth.latent_stream(m, w.stream, 0, 1), synth.action_stream(m, w.stream, 0, 1)
+    x, y = torch.from_numpy(e).cuda(), torch.empty(L, m.hidden, device="cuda")
+    h.forward_chunk(0, synth.timesteps(m)[0], a, x, y)
+    h.kv_update(0.0, a, y)
+    pool = make(BF16 if dtype == "bf16" else F32, blocks=2, pages=1000, kv=2, page=16, d=d)
+    keys, values = pool.keys.clone(), pool.values.clone()
+    s = pool.new()
+    pool.extend([s], [9])
+    pool.import_window(s, h)
+    first, tokens, pages = pool.pages(s)
+    assert (first, tokens, len(pages)) == (0, 9 + L, 978)
+    for kind, buf, old in ((XC_CACHE_KEYS, pool.keys, keys), (XC_CACHE_VALUES, pool.values, values)):
+        for b in range(2):
+            ring = torch.empty(2, 2 * L, d, device="cuda")
+            h.read_cache(kind, 0, b, ring)
+            rows = old[b, :978].transpose(1, 2).reshape(978 * 16, 2, d).clone()  # in order of place
+            rows[9:9 + L] = ring[:, :L].transpose(0, 1).to(buf.dtype)
+            old[b, :978] = rows.view(978, 16, 2, d).transpose(1, 2)
+        assert torch.equal(buf, old)  # the tokens where they belong, everything else as it was
+    h.close()
