@@ -397,8 +397,10 @@ xc_status xc_lds_dma_rate(int32_t row_bytes, void* stream, double* tbytes_per_s)
  *     xc_qk_norm_rope and xc_branch_attention may be captured; such a graph
  *     holds the batch's tables and pieces: it is replayed while its batch is
  *     alive and neither the batch nor its sequences' tables have changed, one
- *     replay or call of one batch at a time.  Two batches share nothing but
- *     the pool.
+ *     replay or call of one batch at a time.  A replay asks for no page's
+ *     sharers: a graph with xc_qk_norm_rope is not replayed while a fork shares
+ *     a page that it writes (outside a graph that is XC_ERR_STATE).  Two batches
+ *     share nothing but the pool.
  *   - Inputs and results of a call do not overlap; rows of one stride may
  *     lie beside each other in one buffer.
  *   - A pool and its batches are used by one thread at a time; a batch may
@@ -461,7 +463,9 @@ xc_status xc_seq_free(xc_pool* pool, int32_t n, const int32_t* seqs);
 
 /* Appends the clean past chunks that the handle's current generation sees
  * (min(n, kv_window - 1) chunks of L tokens, oldest first; every block) to a
- * sequence: a rollout's history becomes one that many branches share.  The
+ * sequence: a rollout's history becomes one that many branches share.  (The way
+ * back is the caller's: a handle's blocks run over its own cache alone, so the
+ * branches' projections, MLPs and modulation come from elsewhere.)  The
  * handle has the pool's dtype, n_blocks, n_heads == kv_heads and head_dim, and
  * is bound to the same stream and device.
  * Errors: XC_ERR_INVALID_ARG, XC_ERR_OOM, XC_ERR_STATE, XC_ERR_HIP (sticky). */
@@ -522,15 +526,19 @@ xc_status xc_qk_norm_rope(xc_batch* batch, int32_t block, const void* qkv, int64
 /* Attention of the batch's rows: softmax(scale q k^T) v over all tokens of the
  * row's sequence in one block (no mask, as in the model), key head h serving
  * query heads h * q_heads / kv_heads and on.  Whole pages that all sequences
- * with rows have in common are read once for the batch where that pays.
+ * with rows begin with are read once for the batch where that pays; pages that
+ * only some of them share are read for each.
  *   q      : device [rows][q_ld], out: device [rows][out_ld], both q_heads *
  *            head_dim columns in the pool's dtype, rows 16-byte aligned, not
  *            overlapping (nor out and the page buffers); NULL where the batch
  *            has no rows.
  *   scale  : positive (a normal number); 0 takes 1 / sqrt(head_dim).
  * Scores, softmax statistics and sums are float32; bf16 pools round the
- * probabilities to bf16 for the product with v.  The same call gives the same
- * bits.  Keys and values outside the sequences are not read.
+ * probabilities to bf16 for the product with v (workgroups of many rows at
+ * head_dim 64 sum the rounded ones).  The same call gives the same bits.  Keys
+ * and values outside the sequences are not read.  NaN and infinities reach the
+ * rows and heads that attend to them alone; an infinite value gives infinity or
+ * NaN in its column.
  * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set or out of date),
  * XC_ERR_HIP (sticky). */
 xc_status xc_branch_attention(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, void* out,

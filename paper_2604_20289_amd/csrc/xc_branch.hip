@@ -17,7 +17,8 @@
 //     the DMA of 8 rows has a wave-uniform 64-bit base.  A wave keeps 64 table
 //     entries in a register and reads them by lane;
 //   * places outside the unit's keys are not read: their lanes fetch the
-//     nearest valid place, and the scores are masked.
+//     nearest valid place, and the scores are masked.  (An infinite value of
+//     that place, times a probability of 0, is NaN where infinity was due.)
 // Two kernels: branch_wide_kernel, 256 rows that share every tile (bound by the
 // matrix cores and the softmax's arithmetic), and branch_few_kernel, up to 64
 // rows whose keys are dealt to four waves (bound by reading the keys).  float32
@@ -175,7 +176,7 @@ __device__ __forceinline__ float half_max(const f32x16& s) {
 }
 
 // p = 2^(scale s - m), rounded to bf16 for the matrix cores (2^-8 each, of
-// either sign); the sum takes them before that rounding.
+// either sign); the sum takes them before that rounding (but see ONES below).
 __device__ __forceinline__ float half_probs(const f32x16& s, float scale, float m, bf16x8 (&p)[2]) {
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -192,8 +193,9 @@ __device__ __forceinline__ float half_probs(const f32x16& s, float scale, float 
 constexpr float kNoMax = -3.402823466e38f;
 
 // The maximum that exponents are taken against moves only when a tile's
-// maximum exceeds it by more than this: p stays <= 2^8 in between, which
-// float sums and bf16 carry.
+// maximum exceeds it by more than this: p stays <= 2^8 in between.  The wide
+// kernel looks at what the exponentials gave instead (see there): p stays below
+// 2^13 at d = 128 and 2^9 at d = 64.  Float sums and bf16 carry any of them.
 constexpr float kMaxSlack = 8.0f, kMaxP = 256.0f;
 
 // 8 waves of 32 rows, all on the same tiles of 64 keys, two waves per SIMD in
@@ -211,8 +213,8 @@ constexpr float kMaxSlack = 8.0f, kMaxP = 256.0f;
 // Bound by the two phases: at d = 128 about 1150 cycles of softmax and 1430 of
 // products, at d = 64 about 940 and 900, where the products alone are 1024
 // and 640; a clock of 1.5 to 1.8 GHz is what the chip's power leaves with all
-// CUs at it.  28080 rows, 21060 keys, 12 heads of 128: 3.0 ms, 1200 TFLOP/s;
-// 6144 rows, 2304 keys, 8 heads of 64: 40 us, 720 TFLOP/s.  The former with
+// CUs at it.  28080 rows, 21060 keys, 12 heads of 128: 2.99 to 3.13 ms from
+// card to card, 1160 to 1210 TFLOP/s; 6144 rows, 2304 keys, 8 heads of 64: 40 us, 720 TFLOP/s.  The former with
 // other choices, at 3440 or 3330 us before the last round of workgroups was
 // filled: the matrix phase without a raised wave priority 3760 us
 // instead of 3440, the softmax raised instead 4010; the softmax not held before
@@ -226,7 +228,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   constexpr int KCG = F::KCG, DT = F::DT, KS = F::KS;
   constexpr int NB = 8 * KCG / kWaves;  // blocks per wave, of a K or a V tile
   // d = 64, where the softmax is the longer phase: its row sums are products
-  // with a row of ones
+  // with a row of ones, and so sums (in float) of the rounded probabilities: 2^-8
+  // more of the result at worst, but the numerator's own roundings where all go
+  // one way cancel
   constexpr int ONES = D == 64;
   constexpr int SLOT = 64 * D * 2;
   // an array per slot: its reads then do not wait for requests into the others
@@ -389,11 +393,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     for (int i = 0; i < PF; ++i) fr[(i0 + i) % PF] = frag(i0 + i, vt, kt);
   };
   // Probabilities of the tile against the maximum so far, which is looked for
-  // only where one of them grew past 2^kMaxSlack (from the first tile's
-  // maximum) - most tiles need none.  Then the tile's own maximum joins in and everything
-  // so far is rescaled.  The limit is checked on the sum or, where there is
-  // none, on the bf16 exponents, whose highest bit stands for 2 and more: the
-  // maximum is taken kMaxSlack higher there.
+  // only where they grew (from the first tile's maximum) - most tiles need none.
+  // Then the tile's own maximum joins in and everything so far is rescaled.  The
+  // limit is checked on a lane's sum of 32, 2^kMaxSlack each (one of them may reach
+  // 2^13), or, where there is none, on the bf16 exponents, whose highest bit
+  // stands for 2 and more: the maximum is taken kMaxSlack higher there (2^9 above it).
   float l_tile = 0.f;
   auto exps = [&]() __attribute__((always_inline)) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};

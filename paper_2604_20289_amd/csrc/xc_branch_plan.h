@@ -83,7 +83,11 @@ inline int cut(int lo, int hi, int n, int i) {
 // waves, 1.3 us alone and 1.85 with every CU busy (the chip's power limits the
 // clock) / 0.9 either way; the few kernel's is 32 KB, 0.86 us alone (38 KB/us
 // through one workgroup's requests; a quarter more with over 32 rows) and 6.0
-// TB/s in all; the float32 kernel's is its products'.
+// TB/s in all; the float32 kernel's is its products'.  Of the latter two fit on
+// a CU at d = 64 and three at 32, but they share the matrix units, and a round
+// of 256 that is not full takes as long as a full one: 1, 2, 3 and 4 rounds of 32
+// tiles take 47, 81, 122 and 158 us (d = 64), 30, 46, 66 and 88 (32), 320
+// workgroups 80 and 46.  So they count as one per CU.
 struct Kernel {
   int rows;
   bool few;
