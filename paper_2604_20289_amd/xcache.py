@@ -494,8 +494,12 @@ _LATER: list = []  # batches whose owner went while their stream was captured
 
 def _release_later():
     """Destroy the batches that could not be then and can be now."""
-    lib = load_library()
-    _LATER[:] = [b for b in _LATER if lib.xc_batch_destroy(b) != XC_OK]
+    # off the list first: a collection in between may come here too
+    batches = _LATER[:]
+    del _LATER[:len(batches)]
+    for b in batches:
+        if load_library().xc_batch_destroy(b) != XC_OK:
+            _LATER.append(b)
 
 
 class Batch:

@@ -107,3 +107,35 @@ builtins.held = b  # outlives the module
 """.format(root=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), tests=os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
     assert r.returncode == 0 and r.stderr == "", r.stderr
+
+
+def test_batches_released_later_are_released_once(lib, monkeypatch):
+    """A collection in the middle of releasing them ends another batch, which comes by the same list."""
+    p = pool()
+    s = p.new()
+    p.extend([s], [5])
+    lost = [Batch(p) for _ in range(4)]
+    extra = [Batch(p)]
+    for b in lost + extra:
+        b.set([s], [1])
+    lib.fake_set(0, 1)
+    lost.clear()
+    del b
+    gc.collect()
+    lib.fake_set(0, 0)
+    seen, destroy = [], lib.xc_batch_destroy
+
+    class Lib:
+        def __getattr__(self, name):
+            return getattr(lib, name)
+
+        def xc_batch_destroy(self, b):
+            seen.append(b)
+            assert seen.count(b) == 1  # (a second time would free it twice)
+            if extra:
+                extra.pop().__del__()
+            return destroy(b)
+
+    monkeypatch.setattr(xcache, "_lib", Lib())
+    xcache._release_later()
+    assert len(seen) == 5 and host.info()["live_bytes"] == 0 and not xcache._LATER
