@@ -60,6 +60,16 @@ class DeviceScope {
   bool changed_ = false;
 };
 
+// Allocations of a batch have nothing to do with a capture of some other stream, whose mode may forbid them to all.
+class OutsideCapture {
+ public:
+  OutsideCapture() { XC_HIP(hipThreadExchangeStreamCaptureMode(&mode_)); }
+  ~OutsideCapture() { (void)hipThreadExchangeStreamCaptureMode(&mode_); }
+
+ private:
+  hipStreamCaptureMode mode_ = hipStreamCaptureModeRelaxed;
+};
+
 xc_status status_of(PageStatus s) {
   return s == PageStatus::ok ? XC_OK : s == PageStatus::full ? XC_ERR_OOM : XC_ERR_INVALID_ARG;
 }
@@ -527,6 +537,7 @@ xc_status xc_batch_destroy(xc_batch* b) {
   if (capturing(b->p->st)) return XC_ERR_STATE;  // waiting would end the capture
   try {
     const DeviceScope scope(b->p->device);
+    const OutsideCapture outside;
     if (b->dev || b->pieces || b->pinned) (void)hipStreamSynchronize(b->p->st);
     if (b->dev) (void)hipFree(b->dev);
     if (b->pieces) (void)hipFree(b->pieces);
@@ -543,6 +554,7 @@ xc_status xc_batch_set(xc_batch* b, int32_t n, const int32_t* seqs, const int32_
   const xc_status s = guarded(*b->p, [&]() -> xc_status {
     if (!b->p->book.distinct(n, seqs)) return XC_ERR_INVALID_ARG;
     if (capturing(b->p->st)) return XC_ERR_STATE;
+    const OutsideCapture outside;
     return set_batch(b, n, seqs, new_tokens);
   });
   if (s == XC_ERR_OOM || s == XC_ERR_HIP) b->set = false, b->rows = 0;  // wherever it failed

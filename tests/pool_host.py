@@ -24,7 +24,7 @@ using namespace xc;
 typedef unsigned long long u64;
 
 // state of the stand-ins
-static int device, capture, device_fails = -1, new_fails = -1, launch_fails = -1;
+static int device, capture, elsewhere, broken, device_fails = -1, new_fails = -1, launch_fails = -1;
 static u64 most_bytes = ~0ull, next_address = 1ull << 44, launched, done;
 struct Block { u64 bytes, used; };
 static std::map<u64, Block>* blocks;
@@ -33,6 +33,14 @@ static std::vector<int>* calls;
 static int freed_in_use, freed_unknown, launched_on = -1;
 static u64 live_bytes, peak_bytes;
 static AttnArgs last_attention;
+
+static hipStreamCaptureMode mode = hipStreamCaptureModeGlobal;
+// while another stream is captured, this thread's mode decides whether allocations are let through or end that capture
+static bool forbidden() {
+  const bool f = elsewhere && mode != hipStreamCaptureModeRelaxed;
+  if (f) ++broken;
+  return f;
+}
 
 static bool counts_down(int& n) { return n >= 0 && n-- == 0; }
 void* operator new(size_t n) {
@@ -64,7 +72,9 @@ hipError_t hipGetDevice(int* d) { return *d = device, hipSuccess; }
 hipError_t hipSetDevice(int d) { return device = d, hipSuccess; }
 hipError_t hipGetLastError() { return hipSuccess; }
 hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t, int) { return *v = 256, hipSuccess; }
+hipError_t hipThreadExchangeStreamCaptureMode(hipStreamCaptureMode* m) { return std::swap(mode, *m), hipSuccess; }
 hipError_t hipMalloc(void** p, size_t n) {
+  if (forbidden()) return hipErrorStreamCaptureUnsupported;
   if (counts_down(device_fails) || live_bytes + n > most_bytes) return hipErrorOutOfMemory;
   const int keep = new_fails;
   new_fails = -1;
@@ -77,6 +87,7 @@ hipError_t hipMalloc(void** p, size_t n) {
   return hipSuccess;
 }
 hipError_t hipFree(void* p) {
+  if (forbidden()) return hipErrorStreamCaptureUnsupported;
   auto it = blocks->find((u64)p);
   if (it == blocks->end()) return ++freed_unknown, hipErrorInvalidValue;
   if (it->second.used > done) ++freed_in_use;
@@ -85,10 +96,11 @@ hipError_t hipFree(void* p) {
   return hipSuccess;
 }
 hipError_t hipHostMalloc(void** p, size_t n, unsigned) {
+  if (forbidden()) return hipErrorStreamCaptureUnsupported;
   if (counts_down(device_fails)) return hipErrorOutOfMemory;
   return (*p = malloc(n)) ? hipSuccess : hipErrorOutOfMemory;
 }
-hipError_t hipHostFree(void* p) { return free(p), hipSuccess; }
+hipError_t hipHostFree(void* p) { return forbidden() ? hipErrorStreamCaptureUnsupported : (free(p), hipSuccess); }
 hipError_t hipEventCreateWithFlags(hipEvent_t* e, unsigned) { return *e = (hipEvent_t)malloc(1), hipSuccess; }
 hipError_t hipEventRecord(hipEvent_t e, hipStream_t) {
   const int keep = new_fails;
@@ -112,19 +124,20 @@ void fake_init() {
   calls->reserve(1 << 16);
 }
 void fake_reset() {
-  device = capture = freed_in_use = freed_unknown = 0;
+  device = capture = elsewhere = broken = freed_in_use = freed_unknown = 0;
   device_fails = new_fails = launch_fails = -1;
   most_bytes = ~0ull;
   peak_bytes = live_bytes;
   calls->clear();
 }
 void fake_set(int dev, int cap) { device = dev, capture = cap; }
+void fake_elsewhere(int on) { elsewhere = on; }
 void fake_faults(int dev, int host, int kernel) { device_fails = dev, new_fails = host, launch_fails = kernel; }
 void fake_memory(u64 most) { most_bytes = most; }
 u64 fake_info(int what) {
   const u64 v[] = {live_bytes, peak_bytes, (u64)freed_in_use, (u64)freed_unknown, blocks->size(), (u64)device,
                    (u64)calls->size(), (u64)last_attention.n_slots, (u64)(calls->empty() ? -1 : calls->back()),
-                   (u64)(device_fails >= 0 || new_fails >= 0), (u64)launched_on};
+                   (u64)(device_fails >= 0 || new_fails >= 0), (u64)launched_on, (u64)broken, (u64)mode};
   return v[what];
 }
 }
@@ -156,7 +169,7 @@ HandleWindow handle_window(const xc_handle*) { return {}; }
 extern "C" const char* xc_status_string(xc_status) { return "refused"; }
 """
 INFO = ("live_bytes", "peak_bytes", "freed_in_use", "freed_unknown", "blocks", "device", "launches", "n_slots", "last_launch",
-        "fault_ahead", "launched_on")
+        "fault_ahead", "launched_on", "broken_captures", "mode")
 
 
 @functools.lru_cache(None)

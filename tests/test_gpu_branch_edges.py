@@ -258,3 +258,35 @@ def test_a_chunk_of_more_pages_than_one_launch_fills(dtype):
             old[b, :978] = rows.view(978, 16, 2, d).transpose(1, 2)
         assert torch.equal(buf, old)  # the tokens where they belong, everything else as it was
     h.close()
+
+
+def test_another_streams_capture_is_left_alone():
+    """While another stream is captured, a pool's calls on its own stream work, allocations among them, and the graph is whole."""
+    own, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(own):
+        pool = make(BF16, pages=400, kv=4, page=16, d=64, seqs=12)
+        parent, seqs = grow(pool, 3000, 0, [(3, 2)] * 8)
+        batch, gone = Batch(pool), Batch(pool)
+        batch.set(seqs[:1], [1])
+        gone.set(seqs[:1], [1])
+        q = torch.randn(16, 4, 64).to(BF16).cuda()
+        out = torch.zeros_like(q)
+    x, y = torch.ones(8, device="cuda"), torch.zeros(8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=other):
+        y.copy_(x * 2)
+        batch.set(seqs, [2] * 8)
+        batch.attention(0, q, out)
+        gone.close()
+        kid, = pool.fork(seqs[0], 1)
+        pool.extend([kid], [1])
+        y.add_(1)
+    for turn in range(3):
+        x.fill_(turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (y == 2 * turn + 1).all()
+    for i, s in enumerate(seqs):
+        want, tol = expected(pool, s, q[2 * i:2 * i + 2], [0, 3])
+        assert ((out[2 * i:2 * i + 2, [0, 3]].double().cpu() - want).abs() <= tol).all()

@@ -174,3 +174,20 @@ def test_columns_of_one_buffer_are_no_overlap():
     assert norms(0, 512, pages // 2, 256) == XC_ERR_INVALID_ARG and attention(0, pages // 2 + 64, 256, 256) == XC_ERR_INVALID_ARG
     lib.xc_batch_destroy(b)
     pool.close()
+
+
+def test_another_streams_capture_is_left_alone():
+    """While some other stream is captured, in the mode that forbids allocations to everybody, a batch grows, is set anew and
+    goes; the thread's mode is what it was."""
+    pool = host.HostPool(n_pages=2000)
+    kids, b, other = _grown(pool), pool.batch(), pool.batch()
+    mode = host.info()["mode"]
+    assert host.set_batch(b, kids[:1], [1]) == XC_OK and host.set_batch(other, kids[:1], [1]) == XC_OK
+    host.lib().fake_elsewhere(1)
+    assert host.set_batch(b, kids, [1] * len(kids)) == XC_OK and host.attention(b) == XC_OK
+    assert host.info()["n_slots"] > 0
+    assert host.lib().xc_batch_destroy(other) == XC_OK and host.lib().xc_batch_destroy(b) == XC_OK
+    assert host.info()["live_bytes"] == 0 and host.info()["freed_unknown"] == 0
+    assert host.info()["broken_captures"] == 0 and host.info()["mode"] == mode
+    host.lib().fake_elsewhere(0)
+    pool.close()
