@@ -544,6 +544,94 @@ xc_status xc_qk_norm_rope(xc_batch* batch, int32_t block, const void* qkv, int64
 xc_status xc_branch_attention(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, void* out,
                               int64_t out_ld);
 
+/* ---- Chunks under a mask, and a cache that stays bounded ----------------
+ *
+ * New tokens that do not all see the same: a history of several chunks or
+ * frames filled in at once, causal by tokens or by frames; a sliding window
+ * whose first tokens stay seen.  And a cache that keeps not the newest tokens
+ * but those that attention uses: xc_chunk_attention gives each row's
+ * log-sum-exp, xc_chunk_weights makes of it the weight that every cached key
+ * got, summed over rows, heads and calls, and xc_chunk_evict keeps the
+ * heaviest.  The usual order:
+ *   xc_seq_extend, xc_chunk_set
+ *   per block: xc_qk_norm_rope, xc_chunk_attention, xc_chunk_weights
+ *   per chunk: xc_chunk_evict
+ *
+ * The conventions of branching rollouts hold.  xc_chunk_set and
+ * xc_chunk_evict change tables and return XC_ERR_STATE while the stream is
+ * being captured; the two others may be captured, under the same conditions
+ * as xc_branch_attention. */
+
+/* Row r (from 0) of the R rows of a sequence of N tokens, its last R, belongs
+ * to group r / group and sees up to the last token of that group, in all
+ *   end = N - R + min(R, (r / group + 1) * group)   (group 0: N)
+ * tokens.  window 0: all of them; else those from max(0, end - window) on and
+ * the sequence's first `sinks`.  Tokens are counted as the sequence has them
+ * (without those dropped or evicted).  Every row sees at least one. */
+typedef struct xc_chunk_mask {
+  int32_t group;   /* 1: causal; the tokens of a frame; 0: no groups */
+  int32_t window;  /* in tokens; 0: no window                        */
+  int32_t sinks;   /* (without a window of no effect)                */
+} xc_chunk_mask;
+
+/* As xc_batch_set, for rows under a mask (NULL: none): the batch then serves
+ * xc_qk_norm_rope, xc_chunk_attention and xc_chunk_weights
+ * (xc_branch_attention has no mask and returns XC_ERR_STATE), until it is set
+ * again or goes out of date.
+ * Errors: those of xc_batch_set; XC_ERR_INVALID_ARG also for a negative field
+ * of the mask. */
+xc_status xc_chunk_set(xc_batch* batch, int32_t n, const int32_t* seqs, const int32_t* new_tokens,
+                       const xc_chunk_mask* mask);
+
+/* Attention of the batch's rows over what each of them sees, otherwise as
+ * xc_branch_attention.
+ *   lse : device float32 [rows][q_heads], the natural logarithm of the row's
+ *         sum of exp(scale q k^T); NULL: not wanted.  Does not overlap q, out
+ *         or the page buffers.
+ * Keys and values that a row does not see do not reach it, whatever they hold;
+ * NaN and infinities that it sees do, as there.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set by xc_chunk_set, or out of
+ * date), XC_ERR_HIP (sticky). */
+xc_status xc_chunk_attention(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, void* out,
+                             int64_t out_ld, float* lse);
+
+/* What the batch's rows give to each token of their sequence in one block:
+ *   weights[i][j] = decay * weights[i][j] + sum exp(scale q k_j^T - lse)
+ * over the rows of the batch's i-th sequence that see its token j and their
+ * query heads, in float32, for every token of every sequence with rows; other
+ * rows and columns of weights are left as they are.
+ *   q, scale : as in xc_chunk_attention, lse: what it gave.
+ *   decay    : 1 adds up, 0 begins anew (weights is not read then); >= 0.
+ *   weights  : device float32 [n of xc_chunk_set][ld], ld at least the tokens of
+ *              the longest sequence; does not overlap q, lse or the page
+ *              buffers.
+ * The same call gives the same bits.  Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE
+ * (as xc_chunk_attention), XC_ERR_HIP (sticky). */
+xc_status xc_chunk_weights(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, const float* lse,
+                           float decay, float* weights, int64_t ld);
+
+/* Shrinks seqs[i] (distinct, any of the pool's) to keep[i] tokens: its first
+ * `sinks`, its last `recent` and of the others the heaviest, the earlier of two
+ * alike (NaN is lighter than any number).  They keep their order and lie in the
+ * sequence's first places, in every block; keys stay as they are, with the
+ * positions that they were rotated to.  A sequence of no more than keep[i]
+ * tokens is left as it is.
+ *   keep    : sinks + recent <= keep[i] for each that shrinks.
+ *   weights : device float32 [n][ld], row i of seqs[i]: those of the kept tokens
+ *             become its first keep[i], the others 0 (up to the tokens it
+ *             had).  NULL where no sequence shrinks.
+ *   kept    : device int32 [n][kept_ld], may be NULL: the numbers, before the call,
+ *             of the tokens kept, ascending.
+ * Pages that only the sequence holds are filled in place; those that others
+ * hold too are replaced by new ones, but for pages of nothing but first
+ * tokens, which do not move; pages left over are released.  The batch lends
+ * its staging memory alone (it need not be set, and its rows play no part);
+ * batches of sequences that shrank are set anew before their next call.
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED (more than 65535 sequences),
+ * XC_ERR_OOM (all or nothing), XC_ERR_STATE, XC_ERR_HIP (sticky). */
+xc_status xc_chunk_evict(xc_batch* batch, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t sinks,
+                         int32_t recent, float* weights, int64_t ld, int32_t* kept, int64_t kept_ld);
+
 #ifdef __cplusplus
 }
 #endif

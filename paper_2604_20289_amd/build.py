@@ -28,8 +28,10 @@ SOURCES = [
     "xc_diag.hip",
     "xc_pages.hip",
     "xc_branch.hip",
+    "xc_chunk.hip",
     "xc_capi.cpp",
     "xc_pool.cpp",
+    "xc_chunk_host.cpp",
 ]
 
 ARCH = "gfx950"

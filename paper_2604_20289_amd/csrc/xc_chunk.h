@@ -1,0 +1,67 @@
+// Chunks of new tokens over the paged cache and what it keeps: the kernels'
+// arguments and launchers.
+#pragma once
+
+#include "xc_chunk_plan.h"
+#include "xc_pool.h"
+
+namespace xc {
+
+// What xc_chunk_set leaves to the calls.
+struct ChunkArgs {
+  const int* tables;
+  const ChunkSeq* seqs;
+  int n_seqs, rows;
+  int q_heads, group;  // group: query heads per key head
+  ChunkMask mask;
+};
+
+struct ChunkAttnArgs {
+  ChunkArgs c;
+  PageBuf buf;
+  const void* q;  // [rows][q_ld]
+  void* out;      // [rows][out_ld]
+  long long q_ld, out_ld;
+  float scale;    // of q . k, in log2 units
+  float* lse;     // [rows][q_heads], may be null
+};
+
+struct ChunkWeightArgs {
+  ChunkArgs c;
+  PageBuf buf;
+  const void* q;  // [rows][q_ld]
+  long long q_ld;
+  float scale;      // of q . k, in log2 units
+  const float* lse;  // [rows][q_heads]
+  float decay;
+  float* weights;  // [sequence][ld]
+  long long ld;
+};
+
+// A sequence that gives tokens up.
+struct EvictSeq {
+  int number;        // row of weights and kept
+  int first, tokens;
+  int keep;          // < tokens; -1: all of them, only listed
+  int from, to;      // its old and new page table begin at tables[from], tables[to]
+  int at;            // its kept tokens' places begin at src[at]
+};
+struct EvictArgs {
+  const EvictSeq* seqs;
+  const int* tables;
+  int* src;  // places (page * page tokens + row) of the kept tokens
+  int n, sinks, recent;
+  float* weights;  // [n][ld]
+  long long ld;
+  int* kept;       // [n][kept_ld], may be null
+  long long kept_ld;
+};
+
+hipError_t launch_chunk_attention(int dtype, const ChunkAttnArgs& a, hipStream_t st);
+// most: tokens of the longest sequence with rows
+hipError_t launch_chunk_weights(int dtype, const ChunkWeightArgs& a, int most, hipStream_t st);
+// whole: the first block; most: of the keeps
+hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes, int most,
+                        hipStream_t st);
+
+}  // namespace xc

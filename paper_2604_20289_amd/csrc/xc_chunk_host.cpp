@@ -1,0 +1,229 @@
+// Host side of chunks under a mask (xc_chunk_* in include/xcache.h): argument
+// validation, what a batch uploads, evictions' tables and the launches.
+#include "xc_pool_state.h"
+
+#include <cmath>
+
+using namespace xc;
+
+namespace {
+
+xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* new_tokens, const ChunkMask& mask) {
+  Pool& p = *b->p;
+  BatchRows r;
+  const xc_status s = batch_rows(p, n, seqs, new_tokens, &r);
+  if (s != XC_OK) return s;
+  const int n_rows = (int)r.seqs.size();
+  std::vector<ChunkSeq> chunk_seqs;
+  std::vector<BatchSeq> batch_seqs;
+  for (int i = 0; i < n_rows; ++i) {
+    const PlanSeq& q = r.seqs[i];
+    chunk_seqs.push_back({r.first_row[i], q.rows, q.first, q.tokens, q.table, r.number[i]});
+    batch_seqs.push_back({r.first_row[i], q.first + q.tokens - q.rows, q.table, {0, 0}});
+  }
+  // uploaded: tables, sequences; written on the device: places, own slots
+  const size_t o_seqs = align256(r.tables.size() * sizeof(int));
+  const size_t o_chunks = o_seqs + align256(batch_seqs.size() * sizeof(BatchSeq));
+  const size_t up = o_chunks + align256(chunk_seqs.size() * sizeof(ChunkSeq));
+  const size_t o_own = up + align256((size_t)r.rows * sizeof(int));
+  const size_t need = o_own + align256((size_t)r.rows * sizeof(OwnSlots));
+  std::vector<int> seq_copy(seqs, seqs + n);
+  if (!staging(b, b->dev, b->dev_bytes, need, up)) return XC_ERR_OOM;
+  if (r.rows > 0) {
+    put(b, 0, r.tables);
+    put(b, o_seqs, batch_seqs);
+    put(b, o_chunks, chunk_seqs);
+    upload(b, b->dev, up);
+    XC_HIP(launch_batch_rows((const int*)b->dev, (const BatchSeq*)(b->dev + o_seqs), n_rows, r.rows, p.book.shift(),
+                             (int*)(b->dev + up), (OwnSlots*)(b->dev + o_own), p.st));
+  }
+  b->attn = {};
+  ChunkArgs& c = b->chunks;
+  c.tables = (const int*)b->dev;
+  c.seqs = (const ChunkSeq*)(b->dev + o_chunks);
+  c.n_seqs = n_rows;
+  c.rows = r.rows;
+  c.q_heads = p.cfg.q_heads;
+  c.group = p.cfg.q_heads / p.cfg.kv_heads;
+  c.mask = mask;
+  b->place = (const int*)(b->dev + up);
+  b->rows = r.rows;
+  b->seqs.swap(seq_copy);
+  b->versions.swap(r.versions);
+  b->written.swap(r.written);
+  b->chunk = b->set = true;
+  return XC_OK;
+}
+
+// 0: not a scale
+float log2_scale(float scale, int head_dim) {
+  const float s = (scale == 0.f ? 1.0f / std::sqrt((float)head_dim) : scale) * 1.4426950408889634f;
+  return scale >= 0.f && std::isnormal(s) ? s : 0.f;
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
+// rows of a caller's buffer of pitch ld that start a row each
+bool stride_ok(long long ld, long long width, int esz) { return ld >= width && ld <= kMaxStride && ld * esz % 16 == 0; }
+
+}  // namespace
+
+extern "C" {
+
+xc_status xc_chunk_set(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* new_tokens, const xc_chunk_mask* mask) {
+  if (!b || n < 0 || (n > 0 && (!seqs || !new_tokens))) return XC_ERR_INVALID_ARG;
+  if (mask && (mask->group < 0 || mask->window < 0 || mask->sinks < 0)) return XC_ERR_INVALID_ARG;
+  ChunkMask m{ChunkMask::kNone, ChunkMask::kNone, 0};
+  if (mask && mask->group > 0) m.group = mask->group;
+  if (mask && mask->window > 0) m.window = mask->window, m.sinks = mask->sinks;
+  const xc_status s = guarded(*b->p, [&]() -> xc_status {
+    if (!b->p->book.distinct(n, seqs)) return XC_ERR_INVALID_ARG;
+    if (capturing(b->p->st)) return XC_ERR_STATE;
+    const OutsideCapture outside;
+    return set_chunk(b, n, seqs, new_tokens, m);
+  });
+  if (s == XC_ERR_OOM || s == XC_ERR_HIP) b->set = false, b->rows = 0;  // wherever it failed
+  return s;
+}
+
+xc_status xc_chunk_attention(xc_batch* b, int32_t block, const void* q, int64_t q_ld, float scale, void* out,
+                             int64_t out_ld, float* lse) {
+  if (!b || (b->rows > 0 && (!q || !out))) return XC_ERR_INVALID_ARG;
+  Pool& p = *b->p;
+  const xc_pool_config& c = p.cfg;
+  const long long width = (long long)c.q_heads * c.head_dim;
+  if (block < 0 || block >= c.n_blocks || !stride_ok(q_ld, width, p.esz) || !stride_ok(out_ld, width, p.esz) ||
+      !aligned16(q) || !aligned16(out) || !aligned4(lse))
+    return XC_ERR_INVALID_ARG;
+  const float s = log2_scale(scale, c.head_dim);
+  if (s == 0.f) return XC_ERR_INVALID_ARG;
+  return guarded(p, [&]() -> xc_status {
+    if (!b->current() || !b->chunk) return XC_ERR_STATE;
+    const Rows in = rows_at(q, b->rows, q_ld, width, p.esz), to = rows_at(out, b->rows, out_ld, width, p.esz),
+               sums = rows_at(lse, lse ? b->rows : 0, c.q_heads, c.q_heads, 4);
+    if (overlap(in, to) || overlap(in, sums) || overlap(to, sums) || p.holds(out, to.extent) || p.holds(lse, sums.extent))
+      return XC_ERR_INVALID_ARG;
+    if (b->rows == 0) return XC_OK;
+    ChunkAttnArgs a{};
+    a.c = b->chunks;
+    a.buf = p.block(block);
+    a.q = q;
+    a.q_ld = q_ld;
+    a.out = out;
+    a.out_ld = out_ld;
+    a.scale = s;
+    a.lse = lse;
+    XC_HIP(launch_chunk_attention(c.dtype, a, p.st));
+    return XC_OK;
+  });
+}
+
+xc_status xc_chunk_weights(xc_batch* b, int32_t block, const void* q, int64_t q_ld, float scale, const float* lse,
+                           float decay, float* weights, int64_t ld) {
+  if (!b || (b->rows > 0 && (!q || !lse || !weights))) return XC_ERR_INVALID_ARG;
+  Pool& p = *b->p;
+  const xc_pool_config& c = p.cfg;
+  const long long width = (long long)c.q_heads * c.head_dim;
+  if (block < 0 || block >= c.n_blocks || !stride_ok(q_ld, width, p.esz) || !aligned16(q) || !aligned4(lse) ||
+      !aligned4(weights) || ld < 0 || ld > kMaxStride || !(decay >= 0.f) || !std::isfinite(decay))
+    return XC_ERR_INVALID_ARG;
+  const float s = log2_scale(scale, c.head_dim);
+  if (s == 0.f) return XC_ERR_INVALID_ARG;
+  return guarded(p, [&]() -> xc_status {
+    if (!b->current() || !b->chunk) return XC_ERR_STATE;
+    if (b->rows == 0) return XC_OK;
+    int most = 0;
+    for (int seq : b->seqs) most = std::max(most, p.book.seq(seq).tokens);
+    if (ld < most) return XC_ERR_INVALID_ARG;
+    const Rows in = rows_at(q, b->rows, q_ld, width, p.esz), sums = rows_at(lse, b->rows, c.q_heads, c.q_heads, 4),
+               to = rows_at(weights, (long long)b->seqs.size(), ld, most, 4);
+    if (overlap(in, to) || overlap(sums, to) || p.holds(weights, to.extent)) return XC_ERR_INVALID_ARG;
+    ChunkWeightArgs a{};
+    a.c = b->chunks;
+    a.buf = p.block(block);
+    a.q = q;
+    a.q_ld = q_ld;
+    a.scale = s;
+    a.lse = lse;
+    a.decay = decay;
+    a.weights = weights;
+    a.ld = ld;
+    XC_HIP(launch_chunk_weights(c.dtype, a, most, p.st));
+    return XC_OK;
+  });
+}
+
+xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t sinks, int32_t recent,
+                         float* weights, int64_t ld, int32_t* kept, int64_t kept_ld) {
+  if (!b || n < 0 || (n > 0 && (!seqs || !keep)) || sinks < 0 || recent < 0 || !aligned4(weights) || !aligned4(kept) ||
+      ld < 0 || ld > kMaxStride || kept_ld < 0 || kept_ld > kMaxStride)
+    return XC_ERR_INVALID_ARG;
+  Pool& p = *b->p;
+  return guarded(p, [&]() -> xc_status {
+    if (!p.book.distinct(n, seqs)) return XC_ERR_INVALID_ARG;
+    if (capturing(p.st)) return XC_ERR_STATE;
+    const OutsideCapture outside;
+    std::vector<EvictSeq> list;
+    std::vector<int> tables;
+    int most_tokens = 0, most_listed = 0, most_kept = 0;
+    long long places = 0;
+    for (int i = 0; i < n; ++i) {
+      const PageSeq& q = p.book.seq(seqs[i]);
+      if (keep[i] < 0) return XC_ERR_INVALID_ARG;
+      const bool less = keep[i] < q.tokens;
+      if (less && (long long)sinks + recent > keep[i]) return XC_ERR_INVALID_ARG;
+      if (q.tokens == 0) continue;
+      most_listed = std::max(most_listed, std::min(keep[i], q.tokens));
+      if (less) {
+        most_tokens = std::max(most_tokens, q.tokens);
+        most_kept = std::max(most_kept, keep[i]);
+        if (places + keep[i] > kMaxPlaces) return XC_ERR_UNSUPPORTED;
+        list.push_back({i, q.first, q.tokens, keep[i], (int)tables.size(), 0, (int)places});
+        tables.insert(tables.end(), q.pages.begin(), q.pages.end());
+        places += keep[i];
+      } else if (kept) {
+        list.push_back({i, q.first, q.tokens, -1, 0, 0, 0});
+      }
+    }
+    if (most_tokens > 0 && (!weights || ld < most_tokens)) return XC_ERR_INVALID_ARG;
+    if (kept && kept_ld < most_listed) return XC_ERR_INVALID_ARG;
+    const Rows w = rows_at(weights, most_tokens ? n : 0, ld, most_tokens, 4),
+               k = rows_at(kept, kept ? n : 0, kept_ld, most_listed, 4);
+    if (overlap(w, k) || p.holds(weights, w.extent) || p.holds(kept, k.extent)) return XC_ERR_INVALID_ARG;
+    if (list.empty()) return XC_OK;
+    if (list.size() > 65535) return XC_ERR_UNSUPPORTED;
+    // room for twice the tables: the new ones are no longer
+    const size_t o_tables = align256(list.size() * sizeof(EvictSeq));
+    const size_t up_most = o_tables + align256(2 * tables.size() * sizeof(int));
+    const size_t need = up_most + align256((size_t)places * sizeof(int));
+    tables.reserve(2 * tables.size());
+    if (!staging(b, b->evict, b->evict_bytes, need, up_most)) return XC_ERR_OOM;
+    std::vector<std::vector<int>> next;
+    const PageStatus s = p.book.evict(n, seqs, keep, sinks, &next);
+    if (s != PageStatus::ok) return status_of(s);
+    committed([&] {
+      for (EvictSeq& e : list) {
+        e.to = (int)tables.size();
+        if (e.keep >= 0) tables.insert(tables.end(), next[e.number].begin(), next[e.number].end());
+      }
+      put(b, 0, list);
+      put(b, o_tables, tables);
+      upload(b, b->evict, up_most);
+      EvictArgs a{};
+      a.seqs = (const EvictSeq*)b->evict;
+      a.tables = (const int*)(b->evict + o_tables);
+      a.src = (int*)(b->evict + up_most);
+      a.n = (int)list.size();
+      a.sinks = sinks;
+      a.recent = recent;
+      a.weights = weights;
+      a.ld = ld;
+      a.kept = kept;
+      a.kept_ld = kept_ld;
+      XC_HIP(launch_evict(a, p.block(0), p.esz, p.cfg.n_blocks, p.block_elems() * p.esz, most_kept, p.st));
+    });
+    return XC_OK;
+  });
+}
+
+}  // extern "C"

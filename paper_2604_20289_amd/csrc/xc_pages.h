@@ -139,6 +139,47 @@ class PageBook {
     return PageStatus::ok;
   }
 
+  // seqs[i] keeps keep[i] of its tokens (as many or more: unchanged) in its first places; which ones is no matter
+  // here.  A place lies in the page it had where nobody else holds that page or its tokens are the first `sinks`, which
+  // do not move; other pages are replaced.  What is shared is settled before the call; new pages are none that it gives
+  // up.  All or nothing; tables receives the new tables.
+  PageStatus evict(int n, const int32_t* seqs, const int32_t* keep, int sinks, std::vector<std::vector<int>>* tables) {
+    if (n < 0 || sinks < 0 || !distinct(n, seqs)) return PageStatus::invalid;
+    auto places = [&](int i) { return (long long)seqs_[seqs[i]].first + keep[i]; };
+    auto moves = [&](int i, size_t j) {
+      const PageSeq& q = seqs_[seqs[i]];
+      return refs_[q.pages[j]] > 1 && ((long long)j + 1) << shift_ > (long long)q.first + sinks;
+    };
+    long long need = 0;
+    std::vector<std::vector<int>> next(n);
+    for (int i = 0; i < n; ++i) {
+      const PageSeq& q = seqs_[seqs[i]];
+      if (keep[i] < 0) return PageStatus::invalid;
+      if (keep[i] >= q.tokens) continue;
+      const size_t used = keep[i] ? (size_t)((places(i) + page() - 1) >> shift_) : 0;
+      next[i].assign(q.pages.begin(), q.pages.begin() + used);
+      for (size_t j = 0; j < used; ++j)
+        if (moves(i, j)) next[i][j] = -1, ++need;
+    }
+    if (need > n_pages() - live_) return PageStatus::full;
+    std::vector<std::vector<int>> copy(next);
+    tables->swap(copy);  // from here on nothing allocates
+    for (int i = 0; i < n; ++i)
+      for (size_t j = 0; j < next[i].size(); ++j)
+        if (next[i][j] < 0) next[i][j] = (*tables)[i][j] = take_page();
+    for (int i = 0; i < n; ++i) {
+      PageSeq& q = seqs_[seqs[i]];
+      if (keep[i] >= q.tokens) continue;
+      for (size_t j = 0; j < q.pages.size(); ++j)
+        if (j >= next[i].size() || next[i][j] != q.pages[j]) release(q.pages[j]);
+      q.pages.swap(next[i]);
+      q.tokens = keep[i];
+      if (keep[i] == 0) q.first = 0;
+      q.version = ++versions_;
+    }
+    return PageStatus::ok;
+  }
+
   PageStatus free(int n, const int32_t* seqs) {
     if (n < 0 || !distinct(n, seqs)) return PageStatus::invalid;
     for (int i = 0; i < n; ++i) {

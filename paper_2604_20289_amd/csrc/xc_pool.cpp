@@ -6,203 +6,20 @@
 // its pieces; and the pieces themselves.  Tables go up from pinned memory on
 // the pool's stream.  A buffer that became too small goes once the work before
 // is done (a graph captured before is not replayed after a new xc_batch_set).
-#include <hip/hip_runtime.h>
+#include "xc_pool_state.h"
 
 #include <cmath>
-#include <cstring>
-#include <memory>
-#include <new>
-#include <vector>
-
-#include "xc_internal.h"
-#include "xc_pool.h"
-#include "xcache.h"
 
 using namespace xc;
 
 namespace {
 
-// places (page * page tokens + row) are 32-bit numbers with room for a tile
-constexpr long long kMaxPlaces = 1ll << 30;
-constexpr int kMaxRows = 1 << 24;
 constexpr int kMaxHeads = 1024;
-constexpr long long kMaxStride = 1ll << 36;  // a row stride; keeps extents in 64 bits
-
-struct Fail {
-  xc_status s;
-};
-
-#define XC_HIP(call)                                                              \
-  do {                                                                            \
-    const hipError_t e_ = (call);                                                 \
-    if (e_ != hipSuccess) {                                                       \
-      (void)hipGetLastError();                                                    \
-      throw Fail{e_ == hipErrorOutOfMemory ? XC_ERR_OOM : XC_ERR_HIP};            \
-    }                                                                             \
-  } while (0)
-
-// The pool's device for the length of a call.
-class DeviceScope {
- public:
-  explicit DeviceScope(int device) {
-    XC_HIP(hipGetDevice(&before_));
-    if (before_ != device) {
-      XC_HIP(hipSetDevice(device));
-      changed_ = true;
-    }
-  }
-  ~DeviceScope() {
-    if (changed_) (void)hipSetDevice(before_);
-  }
-
- private:
-  int before_ = 0;
-  bool changed_ = false;
-};
-
-// Allocations of a batch have nothing to do with a capture of some other stream, whose mode may forbid them to all.
-class OutsideCapture {
- public:
-  OutsideCapture() { XC_HIP(hipThreadExchangeStreamCaptureMode(&mode_)); }
-  ~OutsideCapture() { (void)hipThreadExchangeStreamCaptureMode(&mode_); }
-
- private:
-  hipStreamCaptureMode mode_ = hipStreamCaptureModeRelaxed;
-};
-
-xc_status status_of(PageStatus s) {
-  return s == PageStatus::ok ? XC_OK : s == PageStatus::full ? XC_ERR_OOM : XC_ERR_INVALID_ARG;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-bool overlap(const void* a, size_t an, const void* b, size_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + bn && y < x + an;
-}
-
-struct Pool {
-  Pool(const xc_pool_config& c, int shift) : cfg(c), book(c.n_pages, shift, c.max_seqs) {}
-  xc_pool_config cfg;
-  PageBook book;
-  char *keys = nullptr, *values = nullptr;
-  hipStream_t st = nullptr;
-  int device = 0, cus = 256, esz = 4;
-  bool sticky = false;
-  RopeFreqs freqs{};     // of (theta, axes): the same in every call of a model
-  double theta = 0.0;
-
-  long long block_elems() const {
-    return ((long long)cfg.n_pages << book.shift()) * cfg.kv_heads * cfg.head_dim;
-  }
-  // whether bytes lie in the page buffers
-  bool holds(const void* x, size_t n) const {
-    const size_t bytes = (size_t)block_elems() * cfg.n_blocks * esz;
-    return n > 0 && (overlap(x, n, keys, bytes) || overlap(x, n, values, bytes));
-  }
-  PageBuf block(int b) const {
-    const long long o = b * block_elems() * esz;
-    return {keys + o, values + o, book.shift(), cfg.kv_heads, cfg.head_dim};
-  }
-};
-
-// Tables change on the host while the call is made: inside a capture the
-// replayed work and they would part.
-bool capturing(hipStream_t st) {
-  hipStreamCaptureStatus s = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(st, &s) != hipSuccess) {
-    (void)hipGetLastError();
-    return true;
-  }
-  return s != hipStreamCaptureStatusNone;
-}
 
 void copy_pages(Pool& p, const std::vector<PageCopy>& copies) {
   for (size_t i = 0; i < copies.size(); i += kCopyBatch)
     XC_HIP(launch_page_copies(copies.data() + i, (int)std::min<size_t>(kCopyBatch, copies.size() - i), p.block(0), p.esz,
                               p.cfg.n_blocks, p.block_elems() * p.esz, p.st));
-}
-
-}  // namespace
-
-struct xc_pool {
-  std::shared_ptr<Pool> p;
-};
-
-struct xc_batch {
-  std::shared_ptr<Pool> p;
-  // what xc_batch_set left
-  bool set = false;
-  std::vector<int> seqs;
-  std::vector<uint64_t> versions;
-  std::vector<int> written;  // pages that hold rows of the batch
-  AttnArgs attn{};           // the plan's part of the arguments
-  const int* place = nullptr;
-  int rows = 0;
-  // buffers
-  char* dev = nullptr;
-  size_t dev_bytes = 0;
-  char* pieces = nullptr;
-  size_t piece_bytes = 0;
-  char* pinned = nullptr;
-  size_t pinned_bytes = 0;
-  hipEvent_t uploaded = nullptr;
-  bool upload_pending = false;
-
-  // the tables are still those of its sequences
-  bool current() const {
-    if (!set) return false;
-    for (size_t i = 0; i < seqs.size(); ++i)
-      if (!p->book.valid(seqs[i]) || p->book.seq(seqs[i]).version != versions[i]) return false;
-    return true;
-  }
-};
-
-namespace {
-
-// Runs f with the pool's device current; failures of HIP stick to the pool.
-template <typename F>
-xc_status guarded(Pool& p, F&& f) {
-  if (p.sticky) return XC_ERR_HIP;
-  try {
-    const DeviceScope scope(p.device);
-    return f();
-  } catch (const Fail& e) {
-    if (e.s == XC_ERR_HIP) p.sticky = true;
-    return e.s;
-  } catch (const std::bad_alloc&) {
-    return XC_ERR_OOM;
-  }
-}
-
-// ... of a call that changes tables before it launches: a launch that fails
-// leaves tables and pages apart, whatever the reason
-template <typename F>
-void committed(F&& f) {
-  try {
-    f();
-  } catch (...) {
-    throw Fail{XC_ERR_HIP};
-  }
-}
-
-size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-
-// A caller's [rows][ld], `width` elements of each row in use; all in bytes.
-struct Rows {
-  uintptr_t at;
-  size_t pitch, width, extent;  // extent: to the end of the last row
-};
-Rows rows_at(const void* p, long long rows, long long ld, long long width, int esz) {
-  return {reinterpret_cast<uintptr_t>(p), (size_t)ld * esz, (size_t)width * esz,
-          rows > 0 ? (size_t)((rows - 1) * ld + width) * esz : 0};
-}
-// Rows of one stride may lie beside each other in a buffer; others are told apart by where they begin and end.
-bool overlap(const Rows& a, const Rows& b) {
-  if (a.at >= b.at + b.extent || b.at >= a.at + a.extent) return false;
-  if (a.pitch != b.pitch) return true;
-  const size_t from = b.at >= a.at ? (b.at - a.at) % a.pitch : (a.pitch - (a.at - b.at) % a.pitch) % a.pitch;
-  return from < a.width || from + b.width > a.pitch;
 }
 
 RopeFreqs rope_freqs(int d, int axes, double theta) {
@@ -218,77 +35,19 @@ RopeFreqs rope_freqs(int d, int axes, double theta) {
   return f;
 }
 
-// Device memory of at least `need` bytes at buf, its contents lost; false: there is none.  Work before may still use the
-// smaller buffer, and is waited for.
-bool enlarge(Pool& p, char*& buf, size_t& have, size_t need, size_t reserve) {
-  if (need <= have) return true;
-  if (buf) {
-    XC_HIP(hipStreamSynchronize(p.st));
-    char* old = buf;
-    buf = nullptr;
-    have = 0;
-    XC_HIP(hipFree(old));
-  }
-  void* d = nullptr;
-  const hipError_t e = hipMalloc(&d, need + reserve);
-  if (e == hipErrorOutOfMemory) return (void)hipGetLastError(), false;
-  XC_HIP(e);
-  buf = (char*)d;
-  have = need + reserve;
-  return true;
-}
-
 xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* new_tokens) {
   Pool& p = *b->p;
-  const PageBook& book = p.book;
-  const int shift = book.shift();
-  long long rows = 0;
-  for (int i = 0; i < n; ++i) {
-    if (new_tokens[i] < 0 || new_tokens[i] > book.seq(seqs[i]).tokens) return XC_ERR_INVALID_ARG;
-    rows += new_tokens[i];
-  }
-  if (rows > kMaxRows) return XC_ERR_UNSUPPORTED;
-
-  // whole pages that every sequence with rows begins with
-  const PageSeq* head = nullptr;
-  size_t shared = 0, with_rows = 0;
-  for (int i = 0; i < n; ++i) {
-    if (new_tokens[i] == 0) continue;
-    const PageSeq& q = book.seq(seqs[i]);
-    const size_t whole = (size_t)(((long long)q.first + q.tokens) >> shift);
-    if (with_rows++ == 0) {
-      head = &q;
-      shared = whole;
-      continue;
-    }
-    if (q.first != head->first) shared = 0;
-    shared = std::min(shared, whole);
-    size_t same = 0;
-    while (same < shared && q.pages[same] == head->pages[same]) ++same;
-    shared = same;
-  }
-  if (with_rows < 2) shared = 0;
-
-  std::vector<PlanSeq> plan_seqs;
+  const int shift = p.book.shift();
+  BatchRows r;
+  const xc_status s = batch_rows(p, n, seqs, new_tokens, &r);
+  if (s != XC_OK) return s;
+  const std::vector<PlanSeq>& plan_seqs = r.seqs;
+  const std::vector<int>& tables = r.tables;
+  const long long rows = r.rows;
   std::vector<BatchSeq> batch_seqs;
-  std::vector<int> tables, written, first_row;
-  std::vector<uint64_t> versions(n);
-  int row0 = 0;
-  for (int i = 0; i < n; ++i) {
-    const PageSeq& q = book.seq(seqs[i]);
-    versions[i] = q.version;
-    if (new_tokens[i] == 0) continue;
-    const int at = q.first + q.tokens - new_tokens[i];
-    plan_seqs.push_back({new_tokens[i], q.first, q.tokens, (int)tables.size()});
-    first_row.push_back(row0);
-    tables.insert(tables.end(), q.pages.begin(), q.pages.end());
-    written.insert(written.end(), q.pages.begin() + (at >> shift), q.pages.end());
-    row0 += new_tokens[i];
-  }
-  if (tables.size() > (size_t)kMaxPlaces) return XC_ERR_UNSUPPORTED;
   const int group = p.cfg.q_heads / p.cfg.kv_heads;
   const PlanShape shape{group, p.cfg.kv_heads, p.cfg.head_dim, p.esz, p.cus};
-  AttnPlan plan = plan_attention(plan_seqs, (int)(shared << shift), shape);
+  AttnPlan plan = plan_attention(plan_seqs, r.shared_end, shape);
   auto launches = [&] {  // a launch takes fewer than 2^32 threads
     const long long threads = std::max(((long long)plan.units.size() * p.cfg.kv_heads + kXcds * kXcds) * 512,
                                        plan.n_slots ? rows * p.cfg.q_heads * (p.cfg.head_dim / 4) : 0);
@@ -300,12 +59,12 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   auto stats_at = [&] { return align256(stat_rows() * p.cfg.head_dim * sizeof(float)); };
   const size_t piece_need = plan.n_slots ? stats_at() + stat_rows() * sizeof(float2) : 0;
   if (!enlarge(p, b->pieces, b->piece_bytes, piece_need, piece_need / 4)) {
-    plan = plan_attention(plan_seqs, (int)(shared << shift), shape, 0);  // no memory: without pieces
+    plan = plan_attention(plan_seqs, r.shared_end, shape, 0);  // no memory: without pieces
     if (!launches()) return XC_ERR_OOM;
   }
   for (const PlanPart& part : plan.parts) {
     const PlanSeq& q = plan_seqs[part.seq];
-    const int at = q.first + q.tokens - q.rows + (part.tok0 - first_row[part.seq]);
+    const int at = q.first + q.tokens - q.rows + (part.tok0 - r.first_row[part.seq]);
     batch_seqs.push_back({part.tok0, at, q.table, part.own});
   }
 
@@ -317,27 +76,12 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const size_t need = o_own + align256(rows * sizeof(OwnSlots));
   std::vector<int> seq_copy(seqs, seqs + n);
 
-  if (!enlarge(p, b->dev, b->dev_bytes, need, need / 2)) return XC_ERR_OOM;
-  if (b->upload_pending) {  // the staging memory is being read
-    XC_HIP(hipEventSynchronize(b->uploaded));
-    b->upload_pending = false;
-  }
-  if (up > b->pinned_bytes) {
-    void* d = nullptr;
-    XC_HIP(hipHostMalloc(&d, up + up / 2, hipHostMallocDefault));
-    if (b->pinned) (void)hipHostFree(b->pinned);
-    b->pinned = (char*)d;
-    b->pinned_bytes = up + up / 2;
-  }
-  if (!b->uploaded) XC_HIP(hipEventCreateWithFlags(&b->uploaded, hipEventDisableTiming));
-
+  if (!staging(b, b->dev, b->dev_bytes, need, up)) return XC_ERR_OOM;
   if (rows > 0) {
-    std::memcpy(b->pinned, tables.data(), tables.size() * sizeof(int));
-    std::memcpy(b->pinned + o_seqs, batch_seqs.data(), batch_seqs.size() * sizeof(BatchSeq));
-    std::memcpy(b->pinned + o_units, plan.units.data(), plan.units.size() * sizeof(AttnUnit));
-    XC_HIP(hipMemcpyAsync(b->dev, b->pinned, up, hipMemcpyHostToDevice, p.st));
-    XC_HIP(hipEventRecord(b->uploaded, p.st));
-    b->upload_pending = true;
+    put(b, 0, tables);
+    put(b, o_seqs, batch_seqs);
+    put(b, o_units, plan.units);
+    upload(b, b->dev, up);
     XC_HIP(launch_batch_rows((const int*)b->dev, (const BatchSeq*)(b->dev + o_seqs), (int)batch_seqs.size(), (int)rows,
                              shift, (int*)(b->dev + up), (OwnSlots*)(b->dev + o_own), p.st));
   }
@@ -361,8 +105,9 @@ xc_status set_batch(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   b->place = (const int*)(b->dev + up);
   b->rows = (int)rows;
   b->seqs.swap(seq_copy);
-  b->versions.swap(versions);
-  b->written.swap(written);
+  b->versions.swap(r.versions);
+  b->written.swap(r.written);
+  b->chunk = false;
   b->set = true;
   return XC_OK;
 }
@@ -538,9 +283,10 @@ xc_status xc_batch_destroy(xc_batch* b) {
   try {
     const DeviceScope scope(b->p->device);
     const OutsideCapture outside;
-    if (b->dev || b->pieces || b->pinned) (void)hipStreamSynchronize(b->p->st);
+    if (b->dev || b->pieces || b->evict || b->pinned) (void)hipStreamSynchronize(b->p->st);
     if (b->dev) (void)hipFree(b->dev);
     if (b->pieces) (void)hipFree(b->pieces);
+    if (b->evict) (void)hipFree(b->evict);
     if (b->pinned) (void)hipHostFree(b->pinned);
     if (b->uploaded) (void)hipEventDestroy(b->uploaded);
   } catch (const Fail&) {
@@ -612,7 +358,7 @@ xc_status xc_branch_attention(xc_batch* b, int32_t block, const void* q, int64_t
   const float log2_scale = (scale == 0.f ? 1.0f / std::sqrt((float)c.head_dim) : scale) * 1.4426950408889634f;
   if (!(scale >= 0.f) || !std::isnormal(log2_scale)) return XC_ERR_INVALID_ARG;
   return guarded(p, [&]() -> xc_status {
-    if (!b->current()) return XC_ERR_STATE;
+    if (!b->current() || b->chunk) return XC_ERR_STATE;
     const Rows in = rows_at(q, b->rows, q_ld, width, p.esz), to = rows_at(out, b->rows, out_ld, width, p.esz);
     if (overlap(in, to) || p.holds(out, to.extent)) return XC_ERR_INVALID_ARG;
     if (b->rows == 0) return XC_OK;

@@ -41,7 +41,8 @@ EXPORTED = ["xc_status_string", "xc_init", "xc_forward_chunk", "xc_forward_chunk
             "xc_mfma_rate", "xc_lds_dma_rate",
             "xc_pool_init", "xc_pool_destroy", "xc_pool_info", "xc_pool_compact", "xc_seq_new", "xc_seq_fork",
             "xc_seq_extend", "xc_seq_trim", "xc_seq_free", "xc_seq_import", "xc_seq_pages", "xc_batch_init",
-            "xc_batch_destroy", "xc_batch_set", "xc_qk_norm_rope", "xc_branch_attention"]
+            "xc_batch_destroy", "xc_batch_set", "xc_qk_norm_rope", "xc_branch_attention",
+            "xc_chunk_set", "xc_chunk_attention", "xc_chunk_weights", "xc_chunk_evict"]
 
 
 class ViewGroupC(ctypes.Structure):
@@ -77,6 +78,10 @@ class StatsC(ctypes.Structure):
 class PoolConfigC(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_blocks", "q_heads", "kv_heads", "head_dim", "dtype", "page_tokens",
                                               "n_pages", "max_seqs")]
+
+
+class ChunkMaskC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("group", "window", "sinks")]
 
 
 class XCacheError(RuntimeError):
@@ -134,6 +139,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "xc_batch_set": (i32, [vp, i32, vp, vp]),
         "xc_qk_norm_rope": (i32, [vp, i32, vp, i64, vp, vp, vp, i32, ctypes.c_double, vp, i64]),
         "xc_branch_attention": (i32, [vp, i32, vp, i64, f32, vp, i64]),
+        "xc_chunk_set": (i32, [vp, i32, vp, vp, P(ChunkMaskC)]),
+        "xc_chunk_attention": (i32, [vp, i32, vp, i64, f32, vp, i64, vp]),
+        "xc_chunk_weights": (i32, [vp, i32, vp, i64, f32, vp, f32, vp, i64]),
+        "xc_chunk_evict": (i32, [vp, i32, vp, vp, i32, i32, vp, i64, vp, i64]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -371,6 +380,14 @@ def xc_batch_set(batch: int, seqs: Sequence[int], new_tokens: Sequence[int]):
     _check(load_library().xc_batch_set(batch, len(s), _at(s), _at(t)), "xc_batch_set")
 
 
+def xc_chunk_set(batch: int, seqs: Sequence[int], new_tokens: Sequence[int], mask: Optional[ChunkMaskC] = None):
+    if len(seqs) != len(new_tokens):
+        raise ValueError("one token count per sequence")
+    s, t = _ints(seqs), _ints(new_tokens)
+    _check(load_library().xc_chunk_set(batch, len(s), _at(s), _at(t), ctypes.byref(mask) if mask else None),
+           "xc_chunk_set")
+
+
 def _tensor_dtype(t) -> int:
     """XC_F32 or XC_BF16 of a tensor."""
     name = str(t.dtype)
@@ -406,6 +423,18 @@ def _rows(t, what: str, rows: int, width: int, dtype, device: int) -> int:
     if stride[-1] != 1 or (n == 3 and shape[1] > 1 and stride[1] != shape[2]):
         raise ValueError(f"{what} must have dense rows")
     return stride[0] if rows > 1 else width
+
+
+def _table(t, what: str, rows: int, cols: int, dtype: str, device: int) -> int:
+    """The row stride of [rows, at least cols] with dense rows."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] < cols:
+        raise ValueError(f"{what} must hold {rows} rows of at least {cols}, not {tuple(shape)}")
+    if not _is(t, dtype) or t.get_device() != device:
+        raise ValueError(f"{what} must be {dtype} on GPU {device}")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have dense rows")
+    return t.stride(0) if rows > 1 else shape[1]
 
 
 class Pool:
@@ -470,6 +499,11 @@ class Pool:
             return xc_seq_pages(self.p, seq)
         return head[0], head[1], np.frombuffer(table, np.int32, head[2])
 
+    def tokens(self, seq: int) -> int:
+        """Tokens of a sequence."""
+        _check(self._pages(self.p, seq, None, self._heads[1], None, 0, None), "xc_seq_pages")
+        return self._head[1]
+
     def import_window(self, seq: int, xcache: "XCache"):
         """Append the past chunks of a rollout's window (xc_seq_import)."""
         xc_seq_import(self.p, seq, xcache.h)
@@ -504,11 +538,14 @@ def _release_later():
 
 class Batch:
     """Rows of a pool's sequences: their norms and rotation, their attention
-    (see xc_batch_set, xc_qk_norm_rope, xc_branch_attention)."""
+    (see xc_batch_set, xc_qk_norm_rope, xc_branch_attention), under a mask too, with
+    the weight it gives to each key and the eviction of light ones (see
+    xc_chunk_set, xc_chunk_attention, xc_chunk_weights, xc_chunk_evict)."""
 
     def __init__(self, pool: Pool):
         self.b = 0
         self.pool, self.rows = pool, 0  # the buffers live as long as the batch
+        self._n = self._most = 0  # sequences, tokens of the longest (set_chunk)
         c = pool.config
         self._q_width = c.q_heads * c.head_dim
         self._width = self._q_width + 2 * c.kv_heads * c.head_dim
@@ -530,6 +567,19 @@ class Batch:
                 self.rows = 0
             raise
         self.rows = sum(new_tokens)
+
+    def set_chunk(self, seqs, new_tokens, group: int = 1, window: int = 0, sinks: int = 0):
+        """The rows under a mask (xc_chunk_mask): causal unless ``group`` says otherwise."""
+        if _LATER:
+            _release_later()
+        try:
+            xc_chunk_set(self.b, seqs, new_tokens, ChunkMaskC(group, window, sinks))
+        except XCacheError as e:
+            if e.status in (XC_ERR_OOM, XC_ERR_HIP):  # the batch has no rows then
+                self.rows = 0
+            raise
+        self.rows, self._n = sum(new_tokens), len(seqs)
+        self._most = max(map(self.pool.tokens, seqs), default=0)
 
     def qk_norm_rope(self, block: int, qkv, gq, gk, positions, theta: float, q_out):
         """``qkv`` [rows, (q_heads + 2 kv_heads) head_dim], ``q_out`` [rows, q_heads (x) head_dim],
@@ -555,6 +605,45 @@ class Batch:
         q_ld = _rows(q, "q", self.rows, self._q_width, self._dtype, self._device)
         out_ld = _rows(out, "out", self.rows, self._q_width, self._dtype, self._device)
         _check(self._attention(self.b, block, q.data_ptr(), q_ld, scale, out.data_ptr(), out_ld), "xc_branch_attention")
+
+    def _lse(self, lse) -> int:
+        shape = (self.rows, self._q_width // self._head_dim)
+        if lse.shape != shape or not lse.is_contiguous() or lse.get_device() != self._device or not _is(lse, "float32"):
+            raise ValueError(f"lse must be float32 {list(shape)} on GPU {self._device}")
+        return lse.data_ptr()
+
+    def chunk_attention(self, block: int, q, out, lse=None, scale: float = 0.0):
+        """``q`` and ``out`` [rows, q_heads (x) head_dim], ``lse`` float32 [rows, q_heads] or None."""
+        q_ld = _rows(q, "q", self.rows, self._q_width, self._dtype, self._device)
+        out_ld = _rows(out, "out", self.rows, self._q_width, self._dtype, self._device)
+        _check(load_library().xc_chunk_attention(self.b, block, q.data_ptr(), q_ld, scale, out.data_ptr(), out_ld,
+                                                 None if lse is None else self._lse(lse)), "xc_chunk_attention")
+
+    def chunk_weights(self, block: int, q, lse, weights, decay: float = 1.0, scale: float = 0.0):
+        """``q`` [rows, q_heads (x) head_dim], ``lse`` float32 [rows, q_heads], ``weights`` float32 [sequences of
+        set_chunk, at least their most tokens]."""
+        q_ld = _rows(q, "q", self.rows, self._q_width, self._dtype, self._device)
+        ld = _table(weights, "weights", self._n, self._most, "float32", self._device)
+        _check(load_library().xc_chunk_weights(self.b, block, q.data_ptr(), q_ld, scale, self._lse(lse), decay,
+                                               weights.data_ptr(), ld), "xc_chunk_weights")
+
+    def evict(self, seqs, keep, weights, kept=None, sinks: int = 0, recent: int = 0):
+        """``weights`` float32 [len(seqs), at least their most tokens], ``kept`` int32 [len(seqs), at least the most
+        kept] or None."""
+        s, k = _ints(seqs), _ints(keep)
+        if len(s) != len(k):
+            raise ValueError("one number to keep per sequence")
+        tokens = [self.pool.tokens(x) for x in s]
+        ld = kept_ld = 0
+        w = at = None
+        if weights is not None:
+            most = max((t for t, n in zip(tokens, k) if n < t), default=0)
+            ld, w = _table(weights, "weights", len(s), most, "float32", self._device), weights.data_ptr()
+        if kept is not None:
+            most = max(map(min, tokens, k), default=0)
+            kept_ld, at = _table(kept, "kept", len(s), most, "int32", self._device), kept.data_ptr()
+        _check(load_library().xc_chunk_evict(self.b, len(s), _at(s), _at(k), sinks, recent, w, ld, at, kept_ld),
+               "xc_chunk_evict")
 
     def close(self):
         if self.b:
