@@ -76,18 +76,103 @@ __device__ __forceinline__ float partner_sum(float x) {
 
 // Where a query row's results go.
 struct RowOut {
-  long long out, piece, stat;
+  long long out, piece, stat, lse;
 };
 __device__ __forceinline__ RowOut row_out(const AttnArgs& a, const AttnUnit& un, int h, int r) {
   const int t = un.tok0 + r / a.group, qh = h * a.group + r % a.group;
   RowOut o;
   o.out = (long long)t * a.out_ld + qh * a.buf.D;
+  o.lse = (long long)t * a.q_heads + qh;
   o.stat = ((long long)un.slot * a.piece_rows + t - a.piece_row0) * a.q_heads + qh;
   o.piece = o.stat * a.buf.D;
   return o;
 }
 
-// The page table of a unit, 64 entries at a time: entry e0 + lane.
+// The kernels' units with and without a mask.
+template <bool CHUNK>
+__device__ __forceinline__ auto unit_of(const AttnArgs& a, int u) {
+  if constexpr (CHUNK) return a.chunk_units[u];
+  else return a.units[u];
+}
+// Tiles of `keys` places (64 or 32) of a unit, and where one begins.
+template <bool CHUNK, typename U>
+__device__ __forceinline__ int unit_tiles(const U& un, int keys) {
+  int places = un.hi - (un.lo & ~15);
+  if constexpr (CHUNK) places -= un.skip;
+  return (places + keys - 1) / keys;
+}
+template <bool CHUNK, typename U>
+__device__ __forceinline__ int tile_place(const U& un, int j, int keys) {
+  int at = (un.lo & ~15) + j * keys;
+  if constexpr (CHUNK) at += j * keys >= un.skip_at * 64 ? un.skip : 0;
+  return at;
+}
+// Whether some row of the unit does not see all of a tile.
+template <bool CHUNK, typename U>
+__device__ __forceinline__ bool tile_masked(const U& un, int j, int keys) {
+  if constexpr (CHUNK) {
+    const int at = tile_place<CHUNK>(un, j, keys);
+    return at < un.all_lo || at + keys > un.all_hi;
+  }
+  return false;
+}
+// What a query row sees of a unit's places.
+struct Limits {
+  int begin, lo;
+  unsigned window, sinks;  // places from begin on, from lo on
+  __device__ __forceinline__ bool sees(int at) const { return (unsigned)(at - begin) < window || (unsigned)(at - lo) < sinks; }
+};
+template <bool CHUNK, typename U>
+__device__ __forceinline__ Limits limits_of(const AttnArgs& a, const U& un, int r) {
+  if constexpr (CHUNK) {
+    if (un.seq >= 0) {
+      const ChunkSeq q = a.chunk_seqs[un.seq];
+      const Seen w = seen(q, a.mask, un.tok0 + r / a.group - q.row0);
+      const int begin = max(w.begin, un.lo), end = min(w.end, un.hi);
+      return {begin, un.lo, (unsigned)max(0, end - begin), (unsigned)max(0, min(w.sink_end, un.hi) - un.lo)};
+    }
+  }
+  return {un.lo, un.lo, (unsigned)(un.hi - un.lo), 0u};
+}
+__device__ __forceinline__ void mask_row(f32x16& s, int at0, int hi, const Limits& lim) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (!lim.sees(at0 + key_of_row(0, (i >> 2) * 8 + hi * 4 + (i & 3)))) s[i] = -INFINITY;
+}
+
+// An infinite or NaN value that some rows see and others do not: times the
+// probability 0 of the latter it would be NaN.  So a masked tile's V is looked
+// through in LDS, such numbers become 0 there, and where there were any the rows
+// that see one get NaN in its column once the unit's results are written.
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+__device__ __forceinline__ unsigned not_finite(unsigned x) {  // the bits of 16 bytes' numbers that are not
+  if (sizeof(T) == 4) return (x & 0x7fffffffu) >= 0x7f800000u ? ~0u : 0u;
+  return (((x & 0x7fff7fffu) + 0x00800080u & 0x80008000u) >> 15) * 0xffffu;
+}
+// blocks of 1 KB, `step` apart; whether there were any
+template <typename T, int N>
+__device__ __forceinline__ bool clean_blocks(char* tile, int step, int lane) {
+  unsigned any = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u32x4* at = reinterpret_cast<u32x4*>(tile + i * step + lane * 16);
+    u32x4 x = *at;
+    unsigned bits = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const unsigned m = not_finite<T>(x[e]);
+      bits |= m;
+      x[e] &= ~m;
+    }
+    if (bits != 0) *at = x;
+    any |= bits;
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  return __builtin_amdgcn_ballot_w64(any != 0) != 0;
+}
+
+// The page table of a unit, 64 entries at a time// The page table of a unit, 64 entries at a time: entry e0 + lane.
 struct TableWindow {
   const int* table;
   int e0, e_last, entries, shift, lane;
@@ -153,6 +238,34 @@ __device__ __forceinline__ int k_block_row(int rg, int lane) {
 __device__ __forceinline__ unsigned k_block_col(int rg, int cg, int lane) { return (cg * 8 + ((lane & 7) ^ (lane >> 3) ^ (rg & 1))) * 16; }
 __device__ __forceinline__ int v_block_row(int rg, int lane) { return rg * 8 + (lane >> 3); }
 __device__ __forceinline__ unsigned v_block_col(int cg, int lane) { return (cg * 8 + ((lane & 7) ^ (((lane >> 4) & 1) << 2))) * 16; }
+
+// Rows [r0, r1) of a unit, written before: NaN where they see a value that is
+// not finite in a tile that not all rows see.  A wave, a lane per column or two.
+template <typename T>
+__device__ __forceinline__ void spoil_rows(const AttnArgs& a, const ChunkUnit& un, int h, int keys, int r0, int r1) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  const int D = a.buf.D, shift = a.buf.shift, lane = threadIdx.x & 63, tiles = unit_tiles<true>(un, keys);
+  const T* values = reinterpret_cast<const T*>(a.buf.values);
+  for (int j = 0; j < tiles; ++j) {
+    if (!tile_masked<true>(un, j, keys)) continue;
+    const int at0 = tile_place<true>(un, j, keys);
+    for (int at = max(at0, un.lo); at < min(at0 + keys, un.hi); ++at) {
+      const long long page = a.tables[un.table + (at >> shift)];
+      for (int d = lane; d < D; d += 64) {
+        const float v = (float)values[(((page * a.buf.kv_heads + h) << shift) + (at & ((1 << shift) - 1))) * D + d];
+        if (fabsf(v) < INFINITY) continue;
+        for (int r = r0; r < r1; ++r) {
+          if (!limits_of<true>(a, un, r).sees(at)) continue;
+          const RowOut o = row_out(a, un, h, r);
+          if (un.slot < 0) reinterpret_cast<T*>(a.out)[o.out + d] = (T)NAN;
+          else a.pieces[o.piece + d] = NAN;
+        }
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
 
 // The address of a unit's query row r, head dims hi * 8 on.
 __device__ __forceinline__ const bf16* query_row(const AttnArgs& a, const AttnUnit& un, int h, int r, int hi) {
@@ -222,7 +335,7 @@ constexpr float kMaxSlack = 8.0f, kMaxP = 256.0f;
 // for the latter).  One wave of 64 rows per SIMD, its softmax between its own
 // products, halves the LDS reads but has nothing to hide the requests' address
 // arithmetic behind: 3650 instead of 3310 (47 instead of 43).
-template <int D>
+template <int D, bool CHUNK>
 __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a) {
   using F = Frags<D>;
   constexpr int KCG = F::KCG, DT = F::DT, KS = F::KS;
@@ -231,7 +344,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   // with a row of ones, and so sums (in float) of the rounded probabilities: 2^-8
   // more of the result at worst, but the numerator's own roundings where all go
   // one way cancel
-  constexpr int ONES = D == 64;
+  // (no sums of rounded ones where their logarithm is asked for)
+  constexpr int ONES = D == 64 && !CHUNK;
   constexpr int SLOT = 64 * D * 2;
   // an array per slot: its reads then do not wait for requests into the others
   // (K's come after V's in LDS, in order of name: a transposing read's offset
@@ -244,13 +358,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   __shared__ __attribute__((aligned(1024))) char sV1[SLOT];
   __shared__ __attribute__((aligned(1024))) char sV2[SLOT];
   __shared__ __attribute__((aligned(1024))) char sV3[SLOT];
+  __shared__ __attribute__((aligned(16))) int bad[kWaves];  // CHUNK: of each wave's blocks, whether one was cleaned
   int u, h;
   if (!xcd_pair(blockIdx.x, a.n_units, a.n_long, a.buf.kv_heads, u, h)) return;
-  const AttnUnit un = a.units[u];
+  const auto un = unit_of<CHUNK>(a, u);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hi = lane >> 5, lo = lane & 31;
   const int rows = un.tokens * a.group;
-  const int base = un.lo & ~15, n = (un.hi - base + 63) >> 6, last = un.hi - 1;
+  const int base = un.lo & ~15, n = unit_tiles<CHUNK>(un, 64), last = un.hi - 1;
   const bool live = wave * 32 < rows, later = wave >= kWaves / 2;
   const int in_page = (1 << a.buf.shift) - 1;
   const long long head_bytes = (long long)D * 2 << a.buf.shift, page_bytes = head_bytes * a.buf.kv_heads;
@@ -278,7 +393,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   // half a request: K (first) or V of block i of tile j; j0: the unit's first tile
   auto fetch = [&](int j, int i, bool is_v, char* dst, bool j0 = false) __attribute__((always_inline)) {
     if (!is_v) {
-      const int g0 = min(base + min(j, n - 1) * 64 + (wave + kWaves * i) / KCG / 2 * 16, last & ~15);
+      const int g0 = min(tile_place<CHUNK>(un, min(j, n - 1), 64) + (wave + kWaves * i) / KCG / 2 * 16, last & ~15);
       const int page = __builtin_amdgcn_readlane(win.entries, (g0 >> a.buf.shift) - win.e0);
       group_at = ((long long)((unsigned)page * page_kb) << 10) + (g0 & in_page) * (D * 2);
       group_rows = min(15, last - g0);
@@ -289,7 +404,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     dma16((is_v ? Vh : Kh) + group_at, row * (D * 2) + (is_v ? v_col[i] : k_col[i]), dst + (wave + kWaves * i) * 1024);
   };
   auto cover = [&](int j) __attribute__((always_inline)) {
-    const int at0 = base + min(j, n - 1) * 64;
+    const int at0 = tile_place<CHUNK>(un, min(j, n - 1), 64);
     win.cover(max(at0, un.lo), min(at0 + 63, last));
   };
   auto request = [&](int j, char* kd, char* vd, bool j0 = false) __attribute__((always_inline)) {
@@ -300,6 +415,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
       fetch(j, i, true, vd, j0);
     }
   };
+  // the blocks of V of a masked tile that this wave has fetched
+  auto look = [&](int j, char* vt) __attribute__((always_inline)) {
+    if (tile_masked<CHUNK>(un, j, 64) && clean_blocks<bf16, NB>(vt + wave * 1024, kWaves * 1024, lane)) {
+      if (lane == 0) bad[wave] = 1;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  };
+  if (CHUNK && lane == 0) bad[wave] = 0;
   // What S of the first tile needs is asked for first and waited for alone (36
   // tiles, d = 128: 64 us instead of 65).
 #pragma unroll
@@ -321,23 +444,26 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     // waves without rows only stage tiles, between the same barriers
     XC_WAIT_VM(0);
     tile_barrier();
+    if (CHUNK) look(0, sV0);
     tile_barrier();
     if (later) tile_barrier();
-    auto stage = [&](int j, char* kd, char* vd) __attribute__((always_inline)) {
+    auto stage = [&](int j, char* vn, char* kd, char* vd) __attribute__((always_inline)) {
+      if (CHUNK && later) look(j + 1, vn);
       if (!later) XC_WAIT_VM(2 * NB);
       tile_barrier();
+      if (CHUNK && !later) look(j + 1, vn);
       request(j + 3, kd, vd);
       if (later) XC_WAIT_VM(2 * NB);
       tile_barrier();
     };
     for (int j = 0; j < n - 1; j += 4) {
-      stage(j, tK3, sV3);
+      stage(j, sV1, tK3, sV3);
       if (j + 1 >= n - 1) break;
-      stage(j + 1, tK0, sV0);
+      stage(j + 1, sV2, tK0, sV0);
       if (j + 2 >= n - 1) break;
-      stage(j + 2, tK1, sV1);
+      stage(j + 2, sV3, tK1, sV1);
       if (j + 3 >= n - 1) break;
-      stage(j + 3, tK2, sV2);
+      stage(j + 3, sV0, tK2, sV2);
     }
     if (!later) tile_barrier();
     return;
@@ -353,6 +479,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (bf16)1.0f;
   const F f(lane);
+  const Limits lim = limits_of<CHUNK>(a, un, min(wave * 32 + lo, rows - 1));
   // The matrix phase as a fixed sequence: 4 (DT + ONES) products P V, then 2 KS
   // products K Q^T, one fragment each, read PF products ahead (an LDS read
   // takes longer than the one product that the compiler would read ahead).
@@ -439,8 +566,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   };
   // only a unit's first and last tiles reach outside its keys
   auto mask = [&](int j) __attribute__((always_inline)) {
-    mask_half(s[0], base + j * 64, hi, un.lo, last);
-    mask_half(s[1], base + j * 64 + 32, hi, un.lo, last);
+    if (CHUNK) {
+      const int at = tile_place<CHUNK>(un, j, 64);
+      mask_row(s[0], at, hi, lim);
+      mask_row(s[1], at + 32, hi, lim);
+    } else {
+      mask_half(s[0], base + j * 64, hi, un.lo, last);
+      mask_half(s[1], base + j * 64 + 32, hi, un.lo, last);
+    }
   };
 
   XC_WAIT_VM(5 * NB);  // the first K, the queries
@@ -449,23 +582,29 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   tile_barrier();
   lead(NPV, sV0, tK0);
   products(NPV, NPV + NQK, sV0, tK0, nothing);
-  if (un.lo != base && n > 1) mask(0);
+  if (CHUNK ? tile_masked<CHUNK>(un, 0, 64) : un.lo != base && n > 1) mask(0);
   // (keys that are yet to be masked are copies of valid ones)
   m_run = fmaxf(kNoMax, partner_max(fmaxf(half_max(s[0]), half_max(s[1]))) * a.scale + (ONES ? kMaxSlack : 0.f));
   XC_WAIT_VM(4 * NB);  // the first V
+  if (CHUNK) look(0, sV0);
   tile_barrier();
   if (later) {
     XC_WAIT_VM(2 * NB);  // the second tile
     tile_barrier();
   }
-  // tile j: its V, the next K, and the slots of tile j + 3
-  auto iter = [&](int j, const char* vt, const char* kn, char* kd, char* vd) __attribute__((always_inline)) {
+  // tile j: its V, the next K, the next V, and the slots of tile j + 3
+  auto iter = [&](int j, const char* vt, const char* kn, char* vn, char* kd, char* vd) __attribute__((always_inline)) {
+    // V of tile j + 1 is looked through while the first half's products of tile j and the second half's softmax of
+    // it run: by then both halves' requests have landed, and the first fragments are read a phase later
+    if (CHUNK && later) look(j + 1, vn);
+    if (CHUNK && j > 0 && tile_masked<CHUNK>(un, j, 64)) mask(j);
     softmax();
     // ... all of it here: without this the compiler sinks it behind the barrier, to P's use
     asm volatile("" : "+v"(p[0][0]), "+v"(p[0][1]), "+v"(p[1][0]), "+v"(p[1][1]), "+v"(l_run));
     lead(0, vt, kn);  // V has been there for a phase at least
     if (!later) XC_WAIT_VM(2 * NB);  // all but tile j + 2
     tile_barrier();
+    if (CHUNK && !later) look(j + 1, vn);
     cover(j + 3);
     __builtin_amdgcn_s_setprio(1);
     products(0, NPV + NQK, vt, kn, [&](int i) __attribute__((always_inline)) {
@@ -477,29 +616,31 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
     tile_barrier();
   };
   for (int j = 0; j < n - 1; j += 4) {
-    iter(j, sV0, tK1, tK3, sV3);
+    iter(j, sV0, tK1, sV1, tK3, sV3);
     if (j + 1 >= n - 1) break;
-    iter(j + 1, sV1, tK2, tK0, sV0);
+    iter(j + 1, sV1, tK2, sV2, tK0, sV0);
     if (j + 2 >= n - 1) break;
-    iter(j + 2, sV2, tK3, tK1, sV1);
+    iter(j + 2, sV2, tK3, sV3, tK1, sV1);
     if (j + 3 >= n - 1) break;
-    iter(j + 3, sV3, tK0, tK2, sV2);
+    iter(j + 3, sV3, tK0, sV0, tK2, sV2);
   }
   if (!later) tile_barrier();
   {
     const int slot = (n - 1) & 3;
     const char* vt = slot == 0 ? sV0 : slot == 1 ? sV1 : slot == 2 ? sV2 : sV3;
-    mask(n - 1);
+    if (!CHUNK || (n > 1 && tile_masked<CHUNK>(un, n - 1, 64))) mask(n - 1);
     softmax();
     lead(0, vt, nullptr);
     products(0, NPV, vt, nullptr, nothing);
   }
   const int r = wave * 32 + lo;
   const float l = ONES ? oacc[DT][0] : partner_sum(l_run);
-  if (r >= rows) return;
   const RowOut o = row_out(a, un, h, r);
-  if (un.slot < 0) {
+  if (r >= rows) {
+    // (not a row)
+  } else if (un.slot < 0) {
     const float inv = 1.0f / l;
+    if (CHUNK && a.lse != nullptr && hi == 0) a.lse[o.lse] = log_sum(m_run, l);
     bf16* row = reinterpret_cast<bf16*>(a.out) + o.out;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -522,6 +663,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
         *reinterpret_cast<f32x4*>(row + dt * 32 + g * 8 + hi * 4) = v;
       }
     if (hi == 0) a.stats[o.stat] = make_float2(m_run, l);
+  }
+  if constexpr (CHUNK) {
+    const u32x4 *b = reinterpret_cast<const u32x4*>(bad), x = b[0] | b[1];
+    if (__builtin_amdgcn_readfirstlane(x[0] | x[1] | x[2] | x[3]) != 0)
+      spoil_rows<bf16>(a, un, h, 64, wave * 32, min(wave * 32 + 32, rows));
   }
 }
 
@@ -546,8 +692,8 @@ struct FewShape {
   static constexpr int TILE = KEYS * D * 2;           // bytes, 8 KB
   static constexpr int LOADS = TILE / 1024;
 };
-template <int D, int G>
-__device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, int h, char* sK, char* sV, char* sQ) {
+template <int D, int G, bool CHUNK, typename U>
+__device__ __forceinline__ void few_body(const AttnArgs& a, const U& un, int h, char* sK, char* sV, char* sQ) {
   using F = Frags<D>;
   using S = FewShape<D>;
   constexpr int KCG = F::KCG, DT = F::DT, KS = F::KS, HT = S::HT;
@@ -555,7 +701,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
   const int hi = lane >> 5, lo = lane & 31;
   const int rows = un.tokens * a.group;
   const int base = un.lo & ~15, last = un.hi - 1;
-  const int tiles = (un.hi - base + S::KEYS - 1) / S::KEYS;
+  const int tiles = unit_tiles<CHUNK>(un, S::KEYS);
   const int n = (tiles - wave + 3) >> 2;  // this wave's: wave, wave + 4, ..
   const int in_page = (1 << a.buf.shift) - 1;
   const long long head_bytes = (long long)D * 2 << a.buf.shift, page_bytes = head_bytes * a.buf.kv_heads;
@@ -582,7 +728,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
   char* vt = sV + wave * S::TILE;
   // tile i of this wave, of K (is_k) or V
   auto request = [&](int i, bool is_k) __attribute__((always_inline)) {
-    const int at0 = base + (wave + 4 * i) * S::KEYS;
+    const int at0 = tile_place<CHUNK>(un, wave + 4 * i, S::KEYS);
 #pragma unroll
     for (int rg = 0; rg < 4 * HT; ++rg) {
       const int at = min(max(at0 + (is_k ? k_block_row(rg, lane) : v_block_row(rg, lane)), un.lo), last);
@@ -594,7 +740,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
     }
   };
   auto cover = [&](int i) __attribute__((always_inline)) {
-    const int at0 = base + (wave + 4 * i) * S::KEYS;
+    const int at0 = tile_place<CHUNK>(un, wave + 4 * i, S::KEYS);
     win.cover(max(at0, un.lo), min(at0 + S::KEYS - 1, last));
   };
   if (n > 0) {
@@ -621,6 +767,10 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
       for (int r = 0; r < 16; ++r) oacc[g][i][r] = 0.f;
   }
   const F f(lane);
+  Limits lim[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) lim[g] = limits_of<CHUNK>(a, un, min(g * 32 + lo, rows - 1));
+  int spoiled = 0;
   for (int i = 0; i < n; ++i) {
     XC_WAIT_VM(S::LOADS);  // K has landed, V may be on its way
     asm volatile("" ::: "memory");
@@ -651,10 +801,17 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
       request(i + 1, true);
     }
     const int tile = wave + 4 * i;
+    const bool masked = tile_masked<CHUNK>(un, tile, S::KEYS);
+    const int at = tile_place<CHUNK>(un, tile, S::KEYS);
     bf16x8 p[G][HT][2];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      if (tile == 0 || tile == tiles - 1) {
+      if (CHUNK) {
+        if (masked) {
+#pragma unroll
+          for (int mt = 0; mt < HT; ++mt) mask_row(s[g][mt], at + mt * 32, hi, lim[g]);
+        }
+      } else if (tile == 0 || tile == tiles - 1) {
 #pragma unroll
         for (int mt = 0; mt < HT; ++mt) mask_half(s[g][mt], base + tile * S::KEYS + mt * 32, hi, un.lo, last);
       }
@@ -676,6 +833,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
     }
     if (more) { XC_WAIT_VM(S::LOADS); } else { XC_WAIT_VM(0); }
     asm volatile("" ::: "memory");
+    if (CHUNK && masked && clean_blocks<bf16, S::LOADS>(vt, 1024, lane)) spoiled = 1;
 #pragma unroll
     for (int kv = 0; kv < 2 * HT; ++kv)
 #pragma unroll
@@ -698,6 +856,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
   constexpr int LPR = D / 4;  // 16-byte chunks, or lanes, per row
   static_assert(2 * 32 * D * 4 <= 4 * S::TILE, "two partial results per array");
   float2* stats = reinterpret_cast<float2*>(sQ);
+  int* spoils = reinterpret_cast<int*>(sQ + 2048);
   auto part = [&](int w, int r, int c) __attribute__((always_inline)) {
     return reinterpret_cast<f32x4*>(w < 2 ? sK : sV) + ((w & 1) * 32 + r) * LPR + (c ^ (r & (LPR - 1)));
   };
@@ -707,6 +866,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
     {
       const float l = partner_sum(l_run[g]);
       if (hi == 0) stats[wave * 32 + lo] = make_float2(m_run[g], l);
+      if (CHUNK && lane == 0) spoils[wave] = spoiled;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -734,6 +894,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
       const RowOut ro = row_out(a, un, h, g * 32 + r);
       if (un.slot < 0) {
         const float inv = 1.0f / l;
+        if (CHUNK && a.lse != nullptr && c == 0) a.lse[ro.lse] = log_sum(m, l);
         bf16x4 v;
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = (bf16)(o[k] * inv);
@@ -744,8 +905,12 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const AttnUnit& un, 
       }
     }
   }
+  if constexpr (CHUNK) {
+    if (spoils[0] | spoils[1] | spoils[2] | spoils[3])
+      spoil_rows<bf16>(a, un, h, S::KEYS, wave * (G * 8), min((wave + 1) * (G * 8), rows));
+  }
 }
-template <int D>
+template <int D, bool CHUNK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void branch_few_kernel(AttnArgs a) {
   // arrays of their own: reads of one then do not wait for requests into another
   __shared__ __attribute__((aligned(1024))) char sK[4 * FewShape<D>::TILE];
@@ -754,9 +919,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // units outermost, the long ones first: each key is read by one workgroup
   // (or two in a row), so what counts is that the CUs finish together
   const int u = blockIdx.x / a.buf.kv_heads, h = blockIdx.x - u * a.buf.kv_heads;
-  const AttnUnit un = a.units[u];
-  if (un.tokens * a.group > 32) few_body<D, 2>(a, un, h, sK, sV, sQ);
-  else few_body<D, 1>(a, un, h, sK, sV, sQ);
+  const auto un = unit_of<CHUNK>(a, u);
+  if (un.tokens * a.group > 32) few_body<D, 2, CHUNK>(a, un, h, sK, sV, sQ);
+  else few_body<D, 1, CHUNK>(a, un, h, sK, sV, sQ);
 }
 
 // float32: as branch_few_kernel, four waves with all of up to 32 rows on 32-key
@@ -771,19 +936,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // model's 3 x 64 rows and 128 keys, where these take 5.1.
 // Row r, chunk c of a tile sits at c ^ f(r): rows at one chunk (K) and one row's
 // chunks beside those of the row 4 below (V) meet different banks.
-template <int D>
+template <int D, bool CHUNK>
 __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
   constexpr int DT = D / 32, CH = D / 4, TILE = 32 * D * 4, LOADS = TILE / 1024, RPB = 64 / CH;  // rows per 1 KB block
   __shared__ __attribute__((aligned(1024))) char sK[4 * TILE];
   __shared__ __attribute__((aligned(1024))) char sV[4 * TILE];
   __shared__ float2 stats[4][32];
+  __shared__ int spoils[4];  // CHUNK: of each wave, whether it cleaned a tile
   const int u = blockIdx.x / a.buf.kv_heads, h = blockIdx.x - u * a.buf.kv_heads;
-  const AttnUnit un = a.units[u];
+  const auto un = unit_of<CHUNK>(a, u);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hi = lane >> 5, lo = lane & 31;
   const int rows = un.tokens * a.group;
   const int base = un.lo & ~15, last = un.hi - 1;
-  const int tiles = (un.hi - base + 31) >> 5;
+  const int tiles = unit_tiles<CHUNK>(un, 32);
   const int n = (tiles - wave + 3) >> 2;
   const int in_page = (1 << a.buf.shift) - 1;
   const long long head_bytes = (long long)D * 4 << a.buf.shift, page_bytes = head_bytes * a.buf.kv_heads;
@@ -796,7 +962,7 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     return c ^ (CH >= 16 ? (r & 7) ^ ((r & 4) << 1) : r & 7);
   };
   auto request = [&](int i, const char* src, char* dst) __attribute__((always_inline)) {
-    const int at0 = base + (wave + 4 * i) * 32;
+    const int at0 = tile_place<CHUNK>(un, wave + 4 * i, 32);
 #pragma unroll
     for (int b = 0; b < LOADS; ++b) {
       const int row = b * RPB + lane / CH, g0 = at0 + (b * RPB & 16);
@@ -806,7 +972,7 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     }
   };
   auto cover = [&](int i) __attribute__((always_inline)) {
-    const int at0 = base + (wave + 4 * i) * 32;
+    const int at0 = tile_place<CHUNK>(un, wave + 4 * i, 32);
     win.cover(max(at0, un.lo), min(at0 + 31, last));
   };
   f32x4 qf[D / 8];
@@ -830,6 +996,8 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
   float m_run = kNoMax, l_run = 0.f;
+  const Limits lim = limits_of<CHUNK>(a, un, min(lo, rows - 1));
+  int spoiled = 0;
   for (int i = 0; i < n; ++i) {
     XC_WAIT_VM(LOADS);  // K has landed, V may be on its way
     asm volatile("" ::: "memory");
@@ -854,7 +1022,16 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
       request(i + 1, Kh, kt);
     }
     const int tile = wave + 4 * i;
-    if (tile == 0 || tile == tiles - 1) {  // only these reach outside the unit's keys
+    const bool masked = tile_masked<CHUNK>(un, tile, 32);
+    const int place = tile_place<CHUNK>(un, tile, 32);
+    auto sees = [&](int r) __attribute__((always_inline)) { return lim.sees(place + (r >> 2) * 8 + hi * 4 + (r & 3)); };
+    if (CHUNK) {
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!sees(r)) s[r] = -INFINITY;
+      }
+    } else if (tile == 0 || tile == tiles - 1) {  // only these reach outside the unit's keys
       const int at0 = base + tile * 32;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -879,15 +1056,15 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     }
     if (more) { XC_WAIT_VM(LOADS); } else { XC_WAIT_VM(0); }
     asm volatile("" ::: "memory");
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
+    auto value = [&](int r, int dt) __attribute__((always_inline)) {
       const int key = (r >> 2) * 8 + hi * 4 + (r & 3);
+      return *reinterpret_cast<const float*>(vt + key * (D * 4) + swz(key, dt * 8 + (lo >> 2)) * 16 + (lo & 3) * 4);
+    };
+    if (CHUNK && masked && clean_blocks<float, LOADS>(vt, 1024, lane)) spoiled = 1;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const float v = *reinterpret_cast<const float*>(vt + key * (D * 4) + swz(key, dt * 8 + (lo >> 2)) * 16 + (lo & 3) * 4);
-        oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], oacc[dt], 0, 0, 0);
-      }
-    }
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(r, dt), s[r], oacc[dt], 0, 0, 0);
     if (more) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this V has been read
       request(i + 1, Vh, vt);
@@ -900,6 +1077,7 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
   {
     const float l = partner_sum(l_run);
     if (hi == 0) stats[wave][lo] = make_float2(m_run, l);
+    if (CHUNK && lane == 0) spoils[wave] = spoiled;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -927,11 +1105,15 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     const RowOut ro = row_out(a, un, h, r);
     if (un.slot < 0) {
       const float inv = 1.0f / l;
+      if (CHUNK && a.lse != nullptr && c == 0) a.lse[ro.lse] = log_sum(m, l);
       *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + ro.out + c * 4) = o * inv;
     } else {
       *reinterpret_cast<f32x4*>(a.pieces + ro.piece + c * 4) = o;
       if (c == 0) a.stats[ro.stat] = make_float2(m, l);
     }
+  }
+  if constexpr (CHUNK) {
+    if (spoils[0] | spoils[1] | spoils[2] | spoils[3]) spoil_rows<float>(a, un, h, 32, wave * 8, min(wave * 8 + 8, rows));
   }
 }
 
@@ -997,6 +1179,7 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(AttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
   if (g != 0) return;
+  if (a.lse != nullptr && d0 == 0) a.lse[(long long)t * a.q_heads + i % a.q_heads] = log_sum(m, den);
   T* out = reinterpret_cast<T*>(a.out) + t * a.out_ld + (i % a.q_heads) * D + d0;
   const float inv = 1.0f / den;
 #pragma unroll
@@ -1041,6 +1224,7 @@ __global__ __launch_bounds__(256) void branch_merge_few_kernel(AttnArgs a) {
       acc += w * o[k];
     }
   const float inv = 1.0f / den;
+  if (a.lse != nullptr && d0 == 0) a.lse[(long long)t * a.q_heads + i % a.q_heads] = log_sum(m, den);
   typedef T vec __attribute__((ext_vector_type(4)));
   vec v;
 #pragma unroll
@@ -1057,19 +1241,25 @@ hipError_t launch_branch_attention(int dtype, const AttnArgs& a, hipStream_t st)
   const int total = a.n_units * a.buf.kv_heads, D = a.buf.D;
   if (total == 0) return hipSuccess;
   const unsigned grid = (unsigned)xcd_grid(a.n_units, a.buf.kv_heads);
-  if (dtype == 1) {
-    if (a.few) {
-      if (D == 128) branch_few_kernel<128><<<total, 256, 0, st>>>(a);
-      else branch_few_kernel<64><<<total, 256, 0, st>>>(a);
-    } else {
-      if (D == 128) branch_wide_kernel<128><<<grid, 64 * kWaves, 0, st>>>(a);
-      else branch_wide_kernel<64><<<grid, 64 * kWaves, 0, st>>>(a);
-    }
-  } else {
-    if (D == 128) branch_f32_kernel<128><<<total, 256, 0, st>>>(a);
-    else if (D == 64) branch_f32_kernel<64><<<total, 256, 0, st>>>(a);
-    else branch_f32_kernel<32><<<total, 256, 0, st>>>(a);
-  }
+#define XC_BRANCH(CHUNK)                                                             \
+  do {                                                                               \
+    if (dtype == 1) {                                                                \
+      if (a.few) {                                                                   \
+        if (D == 128) branch_few_kernel<128, CHUNK><<<total, 256, 0, st>>>(a);       \
+        else branch_few_kernel<64, CHUNK><<<total, 256, 0, st>>>(a);                 \
+      } else {                                                                       \
+        if (D == 128) branch_wide_kernel<128, CHUNK><<<grid, 64 * kWaves, 0, st>>>(a); \
+        else branch_wide_kernel<64, CHUNK><<<grid, 64 * kWaves, 0, st>>>(a);         \
+      }                                                                              \
+    } else {                                                                         \
+      if (D == 128) branch_f32_kernel<128, CHUNK><<<total, 256, 0, st>>>(a);         \
+      else if (D == 64) branch_f32_kernel<64, CHUNK><<<total, 256, 0, st>>>(a);      \
+      else branch_f32_kernel<32, CHUNK><<<total, 256, 0, st>>>(a);                   \
+    }                                                                                \
+  } while (0)
+  if (a.chunk_units != nullptr) XC_BRANCH(true);
+  else XC_BRANCH(false);
+#undef XC_BRANCH
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_slots == 0) return e;
   // a wave per (row, head), or one of its lane groups where few pieces join.

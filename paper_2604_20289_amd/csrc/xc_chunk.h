@@ -16,16 +16,6 @@ struct ChunkArgs {
   ChunkMask mask;
 };
 
-struct ChunkAttnArgs {
-  ChunkArgs c;
-  PageBuf buf;
-  const void* q;  // [rows][q_ld]
-  void* out;      // [rows][out_ld]
-  long long q_ld, out_ld;
-  float scale;    // of q . k, in log2 units
-  float* lse;     // [rows][q_heads], may be null
-};
-
 struct ChunkWeightArgs {
   ChunkArgs c;
   PageBuf buf;
@@ -57,7 +47,6 @@ struct EvictArgs {
   long long kept_ld;
 };
 
-hipError_t launch_chunk_attention(int dtype, const ChunkAttnArgs& a, hipStream_t st);
 // most: tokens of the longest sequence with rows
 hipError_t launch_chunk_weights(int dtype, const ChunkWeightArgs& a, int most, hipStream_t st);
 // whole: the first block; most: of the keeps

@@ -1,5 +1,6 @@
-// Kernels of chunks under a mask: attention with its log-sum-exp, the weight
-// that it gives to cached keys, and the eviction of the light ones.
+// Kernels of chunks under a mask besides their attention (which is that of
+// branches, xc_branch.hip): the weight that it gives to cached keys, and the
+// eviction of the light ones.
 #include "xc_chunk.h"
 
 #include "xc_internal.h"
@@ -12,72 +13,7 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-// The sequence of a batch row: the last with row0 <= row.
-__device__ __forceinline__ ChunkSeq seq_of(const ChunkArgs& c, int row) {
-  int lo = 0, hi = c.n_seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (c.seqs[mid].row0 <= row) lo = mid;
-    else hi = mid;
-  }
-  return c.seqs[lo];
-}
-
 __device__ __forceinline__ bool sees(const Seen& w, int at) { return at < w.end && (at >= w.begin || at < w.sink_end); }
-
-__device__ __forceinline__ float wave_max(float v) {
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
-// A wave per (row, query head): 64 keys at a time, one a lane, with a running
-// maximum and sum; then a lane per head dim (or two of them).
-template <typename T, int D>
-__global__ __launch_bounds__(64) void chunk_attention_kernel(ChunkAttnArgs a) {
-  const int row = blockIdx.x, qh = blockIdx.y, lane = threadIdx.x;
-  const ChunkSeq s = seq_of(a.c, row);
-  const Seen w = seen(s, a.c.mask, row - s.row0);
-  const int h = qh / a.c.group, kv = a.buf.kv_heads, shift = a.buf.shift, in_page = (1 << shift) - 1;
-  const T* q = reinterpret_cast<const T*>(a.q) + row * a.q_ld + (long long)qh * D;
-  auto at_of = [&](const void* buf, int place) {
-    const long long page = a.c.tables[s.table + (place >> shift)];
-    return reinterpret_cast<const T*>(buf) + (((page * kv + h) << shift) + (place & in_page)) * D;
-  };
-  constexpr int DL = (D + 63) / 64;
-  float o[DL], m = -INFINITY, l = 0.f;
-  for (int i = 0; i < DL; ++i) o[i] = 0.f;
-  for (int at0 = s.first; at0 < w.end; at0 += 64) {
-    if (at0 >= w.sink_end && at0 + 63 < w.begin) continue;
-    const int at = at0 + lane;
-    float x = -INFINITY;
-    if (sees(w, at)) {
-      const T* k = at_of(a.buf.keys, at);
-      x = 0.f;
-      for (int d = 0; d < D; ++d) x += (float)q[d] * (float)k[d];
-      x *= a.scale;
-    }
-    const float mx = fmaxf(m, wave_max(x)), alpha = m == mx ? 1.f : exp2f(m - mx);
-    const float p = x == -INFINITY ? 0.f : exp2f(x - mx);
-    m = mx;
-    l = l * alpha + wave_sum(p);
-    for (int i = 0; i < DL; ++i) o[i] *= alpha;
-    for (int j = 0; j < 64; ++j) {
-      const float pj = __shfl(p, j, 64);
-      if (!sees(w, at0 + j)) continue;
-      const T* v = at_of(a.buf.values, at0 + j);
-      for (int i = 0; i < DL; ++i)
-        if (i * 64 + lane < D) o[i] += pj * (float)v[i * 64 + lane];
-    }
-  }
-  T* out = reinterpret_cast<T*>(a.out) + row * a.out_ld + (long long)qh * D;
-  for (int i = 0; i < DL; ++i)
-    if (i * 64 + lane < D) out[i * 64 + lane] = (T)(o[i] / l);
-  if (a.lse && lane == 0) a.lse[(long long)row * a.c.q_heads + qh] = (m + log2f(l)) * 0.6931471805599453f;
-}
 
 // A lane per key of a sequence, which keeps the key's row of one head at a time
 // and meets all rows' queries.
@@ -282,21 +218,6 @@ __global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a, char* keys
 }
 
 }  // namespace
-
-hipError_t launch_chunk_attention(int dtype, const ChunkAttnArgs& a, hipStream_t st) {
-  const dim3 grid(a.c.rows, a.c.q_heads);
-#define XC_ATTN(T, DD) chunk_attention_kernel<T, DD><<<grid, 64, 0, st>>>(a)
-  if (dtype == 1) {
-    if (a.buf.D == 128) XC_ATTN(bf16, 128);
-    else XC_ATTN(bf16, 64);
-  } else {
-    if (a.buf.D == 128) XC_ATTN(float, 128);
-    else if (a.buf.D == 64) XC_ATTN(float, 64);
-    else XC_ATTN(float, 32);
-  }
-#undef XC_ATTN
-  return hipGetLastError();
-}
 
 hipError_t launch_chunk_weights(int dtype, const ChunkWeightArgs& a, int most, hipStream_t st) {
   const dim3 grid((most + 63) / 64, a.c.n_seqs);

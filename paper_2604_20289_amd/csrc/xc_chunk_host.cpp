@@ -13,38 +13,79 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   BatchRows r;
   const xc_status s = batch_rows(p, n, seqs, new_tokens, &r);
   if (s != XC_OK) return s;
-  const int n_rows = (int)r.seqs.size();
+  const int n_rows = (int)r.seqs.size(), shift = p.book.shift();
   std::vector<ChunkSeq> chunk_seqs;
-  std::vector<BatchSeq> batch_seqs;
   for (int i = 0; i < n_rows; ++i) {
     const PlanSeq& q = r.seqs[i];
     chunk_seqs.push_back({r.first_row[i], q.rows, q.first, q.tokens, q.table, r.number[i]});
-    batch_seqs.push_back({r.first_row[i], q.first + q.tokens - q.rows, q.table, {0, 0}});
   }
-  // uploaded: tables, sequences; written on the device: places, own slots
+  const int group = p.cfg.q_heads / p.cfg.kv_heads;
+  const PlanShape shape{group, p.cfg.kv_heads, p.cfg.head_dim, p.esz, p.cus};
+  ChunkPlan plan = plan_chunk(chunk_seqs, mask, r.shared_end, shape);
+  const long long rows = r.rows;
+  auto launches = [&] {  // a launch takes fewer than 2^32 threads
+    const long long threads = std::max(((long long)plan.units.size() * p.cfg.kv_heads + kXcds * kXcds) * 512,
+                                       plan.n_slots ? rows * p.cfg.q_heads * (p.cfg.head_dim / 4) : 0);
+    return threads >> 32 == 0;
+  };
+  if (!launches()) return XC_ERR_UNSUPPORTED;
+  // pieces [slot][row][head][D], then their statistics
+  auto stat_rows = [&] { return (size_t)plan.n_slots * (rows - plan.piece_row0) * p.cfg.q_heads; };
+  auto stats_at = [&] { return align256(stat_rows() * p.cfg.head_dim * sizeof(float)); };
+  const size_t piece_need = plan.n_slots ? stats_at() + stat_rows() * sizeof(float2) : 0;
+  if (!enlarge(p, b->pieces, b->piece_bytes, piece_need, piece_need / 4)) {
+    plan = plan_chunk(chunk_seqs, mask, r.shared_end, shape, 0);  // no memory: without pieces
+    if (!launches()) return XC_ERR_OOM;
+  }
+  std::vector<BatchSeq> batch_seqs;
+  for (const PlanPart& part : plan.parts) {
+    const ChunkSeq& q = chunk_seqs[part.seq];
+    batch_seqs.push_back({part.tok0, q.first + q.tokens - q.rows + (part.tok0 - q.row0), q.table, part.own});
+  }
+  // uploaded: tables, sequences, units; written on the device: places, own slots
   const size_t o_seqs = align256(r.tables.size() * sizeof(int));
   const size_t o_chunks = o_seqs + align256(batch_seqs.size() * sizeof(BatchSeq));
-  const size_t up = o_chunks + align256(chunk_seqs.size() * sizeof(ChunkSeq));
-  const size_t o_own = up + align256((size_t)r.rows * sizeof(int));
-  const size_t need = o_own + align256((size_t)r.rows * sizeof(OwnSlots));
+  const size_t o_units = o_chunks + align256(chunk_seqs.size() * sizeof(ChunkSeq));
+  const size_t up = o_units + align256(plan.units.size() * sizeof(ChunkUnit));
+  const size_t o_own = up + align256(rows * sizeof(int));
+  const size_t need = o_own + align256(rows * sizeof(OwnSlots));
   std::vector<int> seq_copy(seqs, seqs + n);
   if (!staging(b, b->dev, b->dev_bytes, need, up)) return XC_ERR_OOM;
-  if (r.rows > 0) {
+  if (rows > 0) {
     put(b, 0, r.tables);
     put(b, o_seqs, batch_seqs);
     put(b, o_chunks, chunk_seqs);
+    put(b, o_units, plan.units);
     upload(b, b->dev, up);
-    XC_HIP(launch_batch_rows((const int*)b->dev, (const BatchSeq*)(b->dev + o_seqs), n_rows, r.rows, p.book.shift(),
+    XC_HIP(launch_batch_rows((const int*)b->dev, (const BatchSeq*)(b->dev + o_seqs), (int)batch_seqs.size(), r.rows, shift,
                              (int*)(b->dev + up), (OwnSlots*)(b->dev + o_own), p.st));
   }
-  b->attn = {};
+  AttnArgs& a = b->attn;
+  a = {};
+  a.tables = (const int*)b->dev;
+  a.chunk_units = (const ChunkUnit*)(b->dev + o_units);
+  a.chunk_seqs = (const ChunkSeq*)(b->dev + o_chunks);
+  a.mask = mask;
+  a.n_units = (int)plan.units.size();
+  a.n_long = long_units(plan.units);
+  a.group = group;
+  a.pieces = (float*)b->pieces;
+  a.stats = (float2*)(b->pieces + stats_at());
+  a.own = (const OwnSlots*)(b->dev + o_own);
+  a.shared_slots = plan.shared_slots;
+  a.rows = r.rows;
+  a.q_heads = p.cfg.q_heads;
+  a.n_slots = plan.n_slots;
+  a.piece_row0 = plan.piece_row0;
+  a.piece_rows = r.rows - plan.piece_row0;
+  a.few = plan.few;
   ChunkArgs& c = b->chunks;
-  c.tables = (const int*)b->dev;
-  c.seqs = (const ChunkSeq*)(b->dev + o_chunks);
+  c.tables = a.tables;
+  c.seqs = a.chunk_seqs;
   c.n_seqs = n_rows;
   c.rows = r.rows;
   c.q_heads = p.cfg.q_heads;
-  c.group = p.cfg.q_heads / p.cfg.kv_heads;
+  c.group = group;
   c.mask = mask;
   b->place = (const int*)(b->dev + up);
   b->rows = r.rows;
@@ -104,8 +145,7 @@ xc_status xc_chunk_attention(xc_batch* b, int32_t block, const void* q, int64_t 
     if (overlap(in, to) || overlap(in, sums) || overlap(to, sums) || p.holds(out, to.extent) || p.holds(lse, sums.extent))
       return XC_ERR_INVALID_ARG;
     if (b->rows == 0) return XC_OK;
-    ChunkAttnArgs a{};
-    a.c = b->chunks;
+    AttnArgs a = b->attn;
     a.buf = p.block(block);
     a.q = q;
     a.q_ld = q_ld;
@@ -113,7 +153,7 @@ xc_status xc_chunk_attention(xc_batch* b, int32_t block, const void* q, int64_t 
     a.out_ld = out_ld;
     a.scale = s;
     a.lse = lse;
-    XC_HIP(launch_chunk_attention(c.dtype, a, p.st));
+    XC_HIP(launch_branch_attention(c.dtype, a, p.st));
     return XC_OK;
   });
 }

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "xc_branch_plan.h"
+#include "xc_chunk_plan.h"
 #include "xc_pages.h"
 
 struct xc_handle;
@@ -91,6 +92,11 @@ struct AttnArgs {
   int piece_row0, piece_rows;  // the rows that have pieces: from piece_row0 to the last
   int n_slots;              // 0: no row has pieces
   int few;                  // bf16: units of at most kFewRows query rows, for branch_few_kernel
+  // rows under a mask: units of their own in the place of `units`, else null
+  const ChunkUnit* chunk_units;
+  const ChunkSeq* chunk_seqs;
+  ChunkMask mask;
+  float* lse;               // [rows][q_heads] log-sum-exps, may be null
 };
 
 

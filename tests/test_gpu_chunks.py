@@ -196,3 +196,94 @@ def test_evictions_of_every_length(n):
     pool.extend([s], [n])
     w = torch.rand(1, n, generator=torch.Generator().manual_seed(n)).cuda()
     evict_check(pool, Batch(pool), [s], [n // 2], 0, n // 8, w)
+
+
+# ---------------------------------------------------------------- numbers that are not finite
+
+# type, key heads, head dim, rows: with 256 heads the kernel of 256-row workgroups, with one or two those of 64 and 32
+KERNELS = [(BF16, 256, 64, 300), (BF16, 256, 128, 300), (BF16, 1, 64, 21), (BF16, 2, 128, 50), (F32, 1, 32, 21), (F32, 2, 64, 90),
+           (F32, 1, 128, 40)]
+
+
+@pytest.mark.parametrize("dtype,kv,d,rows", KERNELS)
+@pytest.mark.parametrize("what,bad", [("key", math.nan), ("key", math.inf), ("value", math.nan), ("value", -math.inf)])
+@pytest.mark.parametrize("mask", [(1, 0, 0), (4, 40, 3), (1, 1, 0)])
+def test_what_a_row_does_not_see_does_not_reach_it(mask, what, bad, dtype, kv, d, rows):
+    """Numbers that are not finite in the middle of the new tokens, in the last one and, where there is a window that hides it, in
+    an old one.  A row that sees a value has it in its column alone, and none that does not is touched."""
+    before = 70
+    tokens = before + rows
+    pool = make(dtype, pages=2 * (-(-(tokens + 3) // 16) + 1), kv=kv, page=16, d=d, seqs=3)
+    s = pool.new()
+    pool.extend([s], [tokens + 3])
+    pool.trim(s, front=3)
+    g = torch.Generator().manual_seed(11)
+    k, v = torch.randn(2, tokens, kv, d, generator=g)
+    head, dim, at = kv // 2, d // 3, [20] * bool(mask[1]) + [before + rows // 2, tokens - 1]
+    (k if what == "key" else v)[at, head, dim] = bad
+    write(pool, s, k, v)
+    batch = Batch(pool)
+    batch.set_chunk([s], [rows], *mask)
+    q = torch.randn(rows, kv, d, generator=g).to(dtype).cuda()
+    out, lse = torch.empty_like(q), torch.empty(rows, kv, device="cuda")
+    batch.chunk_attention(0, q, out, lse=lse)
+    w = torch.zeros(1, tokens, device="cuda")
+    batch.chunk_weights(0, q, lse, w, decay=0.0)
+    heads = sorted({0, head, kv - 1})
+    k, v = (ref.gather(b, 0, pool.pages(s)) for b in (pool.keys, pool.values))
+    see = chunk.sees(tokens, rows, *mask)
+    hit = see[:, at].any(1)
+    assert not hit.all()
+    k0, v0 = (torch.where(torch.isfinite(x), x, torch.zeros_like(x)) for x in (k, v))
+    want, tol, want_lse, lse_tol = chunk.attention(q[:, heads].double().cpu(), k0[:, heads], v0[:, heads], d ** -0.5, see, dtype,
+                                                   p_eps(dtype))
+    got, got_lse = out.double().cpu()[:, heads], lse.double().cpu()[:, heads]
+    i = heads.index(head)
+    fine = torch.ones(want.shape, dtype=torch.bool)
+    if what == "key":
+        fine[hit, i] = False
+    else:
+        fine[hit, i, dim] = False
+    assert ((got - want).abs() <= tol)[fine].all()
+    assert torch.isfinite(out.double().cpu()[:, [h for h in range(kv) if h != head]]).all()
+    if what == "value":
+        assert not torch.isfinite(got[hit, i, dim]).any()
+        assert ((got_lse - want_lse).abs() <= lse_tol).all()
+        total, tol = chunk.weights(q.double().cpu(), k, d ** -0.5, see, lse.double().cpu())
+        assert ((w[0].double().cpu() - total).abs() <= tol + 1e-30).all()
+    else:
+        rows_ok = torch.ones(rows, dtype=torch.bool)
+        rows_ok[hit] = False
+        assert ((got_lse - want_lse).abs() <= lse_tol)[rows_ok].all()
+        # tokens that only untouched rows see have finite weights
+        only = ~(see & hit[:, None]).any(0) & see.any(0)
+        assert torch.isfinite(w[0].cpu()[only]).all()
+
+
+@pytest.mark.parametrize("dtype,kv,d,rows", KERNELS)
+def test_scores_of_any_size_under_a_mask(dtype, kv, d, rows):
+    """Scores hundreds of log2 units apart in rising and falling order, the largest of them hidden from most rows, and keys
+    whose product with every query overflows to -infinity."""
+    before = 60
+    tokens = before + rows
+    pool = make(dtype, pages=-(-tokens // 16) + 1, kv=kv, page=16, d=d, seqs=2)
+    s = pool.new()
+    pool.extend([s], [tokens])
+    g = torch.Generator().manual_seed(12)
+    only = sorted({0, kv // 2, kv - 1})
+    batch = Batch(pool)
+    for order in ("up", "down"):
+        ramp = torch.linspace(-60, 60, tokens)
+        ramp = ramp if order == "up" else ramp.flip(0)
+        k = ramp[:, None, None].expand(tokens, kv, d) + 0.5 * torch.randn(tokens, kv, d, generator=g)
+        write(pool, s, k, torch.randn(tokens, kv, d, generator=g))
+        for mask in ((1, 0, 0), (5, 30, 2)):
+            batch.set_chunk([s], [rows], *mask)
+            q = torch.ones(rows, kv, d).to(dtype).cuda()
+            out, lse = torch.empty_like(q), torch.empty(rows, kv, device="cuda")
+            batch.chunk_attention(0, q, out, lse=lse, scale=0.3)
+            kk, vv = (ref.gather(b, 0, pool.pages(s))[:, only] for b in (pool.keys, pool.values))
+            want, tol, want_lse, lse_tol = chunk.attention(q[:, only].double().cpu(), kk, vv, 0.3, chunk.sees(tokens, rows, *mask),
+                                                           dtype, p_eps(dtype))
+            assert ((out[:, only].double().cpu() - want).abs() <= tol).all()
+            assert ((lse[:, only].double().cpu() - want_lse).abs() <= lse_tol).all()
