@@ -110,17 +110,18 @@ __device__ __forceinline__ int tile_place(const U& un, int j, int keys) {
 // Whether some row of the unit does not see all of a tile.
 template <bool CHUNK, typename U>
 __device__ __forceinline__ bool tile_masked(const U& un, int j, int keys) {
-  if constexpr (CHUNK) {
-    const int at = tile_place<CHUNK>(un, j, keys);
-    return at < un.all_lo || at + keys > un.all_hi;
-  }
+  if constexpr (CHUNK) return (unsigned)((keys == 64 ? j : j >> 1) - un.free_lo) >= (unsigned)un.free_n;
   return false;
 }
-// What a query row sees of a unit's places.
+// What a query row sees of a unit's places: [begin, end) and [lo, sink_end).
 struct Limits {
-  int begin, lo;
-  unsigned window, sinks;  // places from begin on, from lo on
-  __device__ __forceinline__ bool sees(int at) const { return (unsigned)(at - begin) < window || (unsigned)(at - lo) < sinks; }
+  int begin, end, lo, sink_end;
+  __device__ __forceinline__ bool sees(int at) const { return (at >= begin && at < end) || (at >= lo && at < sink_end); }
+  // of 32 places from `at` on, a bit each
+  __device__ __forceinline__ unsigned bits(int at) const {
+    auto below = [](int n) __attribute__((always_inline)) { return n <= 0 ? 0u : ~0u >> (32 - min(n, 32)); };
+    return (below(end - at) & ~below(begin - at)) | (below(sink_end - at) & ~below(lo - at));
+  }
 };
 template <bool CHUNK, typename U>
 __device__ __forceinline__ Limits limits_of(const AttnArgs& a, const U& un, int r) {
@@ -128,16 +129,25 @@ __device__ __forceinline__ Limits limits_of(const AttnArgs& a, const U& un, int 
     if (un.seq >= 0) {
       const ChunkSeq q = a.chunk_seqs[un.seq];
       const Seen w = seen(q, a.mask, un.tok0 + r / a.group - q.row0);
-      const int begin = max(w.begin, un.lo), end = min(w.end, un.hi);
-      return {begin, un.lo, (unsigned)max(0, end - begin), (unsigned)max(0, min(w.sink_end, un.hi) - un.lo)};
+      return {max(w.begin, un.lo), min(w.end, un.hi), un.lo, min(w.sink_end, un.hi)};
     }
+    return {max(un.from, un.lo), un.hi, un.lo, min(un.sink_end, un.hi)};
   }
-  return {un.lo, un.lo, (unsigned)(un.hi - un.lo), 0u};
+  return {un.lo, un.hi, un.lo, un.lo};
 }
-__device__ __forceinline__ void mask_row(f32x16& s, int at0, int hi, const Limits& lim) {
+// Scores of a half tile at `at` that the row does not see: -infinity.  Bits
+// and not comparisons: these would want a pair of scalar registers each.
+// KEY: the place of a score among its half wave's 16.
+template <typename Key>
+__device__ __forceinline__ void mask_row(f32x16& s, unsigned bits, Key key) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (!lim.sees(at0 + key_of_row(0, (i >> 2) * 8 + hi * 4 + (i & 3)))) s[i] = -INFINITY;
+  for (int i = 0; i < 16; ++i) {
+    const unsigned keep = (unsigned)((int)(bits << (31 - key(i))) >> 31);
+    s[i] = __uint_as_float((__float_as_uint(s[i]) & keep) | (0xff800000u & ~keep));
+  }
+}
+__device__ __forceinline__ void mask_row(f32x16& s, int at, int hi, const Limits& lim) {
+  mask_row(s, lim.bits(at) >> (hi * 8), [](int i) { return key_of_row(0, (i >> 2) * 8 + (i & 3)); });
 }
 
 // An infinite or NaN value that some rows see and others do not: times the
@@ -241,9 +251,14 @@ __device__ __forceinline__ unsigned v_block_col(int cg, int lane) { return (cg *
 
 // Rows [r0, r1) of a unit, written before: NaN where they see a value that is
 // not finite in a tile that not all rows see.  A wave, a lane per column or two.
+// (Its arguments are loaded here: held in registers from the start they would crowd out the loop's.)
 template <typename T>
-__device__ __forceinline__ void spoil_rows(const AttnArgs& a, const ChunkUnit& un, int h, int keys, int r0, int r1) {
+__device__ __forceinline__ void spoil_rows(int u, int h, int keys, int r0, int r1) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  const void* args = (const void*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(args));
+  const AttnArgs& a = *reinterpret_cast<const AttnArgs*>(args);
+  const ChunkUnit un = a.chunk_units[u];
   const int D = a.buf.D, shift = a.buf.shift, lane = threadIdx.x & 63, tiles = unit_tiles<true>(un, keys);
   const T* values = reinterpret_cast<const T*>(a.buf.values);
   for (int j = 0; j < tiles; ++j) {
@@ -667,7 +682,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void branch_wide_kernel(AttnArgs a)
   if constexpr (CHUNK) {
     const u32x4 *b = reinterpret_cast<const u32x4*>(bad), x = b[0] | b[1];
     if (__builtin_amdgcn_readfirstlane(x[0] | x[1] | x[2] | x[3]) != 0)
-      spoil_rows<bf16>(a, un, h, 64, wave * 32, min(wave * 32 + 32, rows));
+      spoil_rows<bf16>(u, h, 64, wave * 32, min(wave * 32 + 32, rows));
   }
 }
 
@@ -693,7 +708,7 @@ struct FewShape {
   static constexpr int LOADS = TILE / 1024;
 };
 template <int D, int G, bool CHUNK, typename U>
-__device__ __forceinline__ void few_body(const AttnArgs& a, const U& un, int h, char* sK, char* sV, char* sQ) {
+__device__ __forceinline__ void few_body(const AttnArgs& a, const U& un, int u, int h, char* sK, char* sV, char* sQ) {
   using F = Frags<D>;
   using S = FewShape<D>;
   constexpr int KCG = F::KCG, DT = F::DT, KS = F::KS, HT = S::HT;
@@ -907,7 +922,7 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const U& un, int h, 
   }
   if constexpr (CHUNK) {
     if (spoils[0] | spoils[1] | spoils[2] | spoils[3])
-      spoil_rows<bf16>(a, un, h, S::KEYS, wave * (G * 8), min((wave + 1) * (G * 8), rows));
+      spoil_rows<bf16>(u, h, S::KEYS, wave * (G * 8), min((wave + 1) * (G * 8), rows));
   }
 }
 template <int D, bool CHUNK>
@@ -920,8 +935,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // (or two in a row), so what counts is that the CUs finish together
   const int u = blockIdx.x / a.buf.kv_heads, h = blockIdx.x - u * a.buf.kv_heads;
   const auto un = unit_of<CHUNK>(a, u);
-  if (un.tokens * a.group > 32) few_body<D, 2, CHUNK>(a, un, h, sK, sV, sQ);
-  else few_body<D, 1, CHUNK>(a, un, h, sK, sV, sQ);
+  if (un.tokens * a.group > 32) few_body<D, 2, CHUNK>(a, un, u, h, sK, sV, sQ);
+  else few_body<D, 1, CHUNK>(a, un, u, h, sK, sV, sQ);
 }
 
 // float32: as branch_few_kernel, four waves with all of up to 32 rows on 32-key
@@ -1024,13 +1039,8 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     const int tile = wave + 4 * i;
     const bool masked = tile_masked<CHUNK>(un, tile, 32);
     const int place = tile_place<CHUNK>(un, tile, 32);
-    auto sees = [&](int r) __attribute__((always_inline)) { return lim.sees(place + (r >> 2) * 8 + hi * 4 + (r & 3)); };
     if (CHUNK) {
-      if (masked) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!sees(r)) s[r] = -INFINITY;
-      }
+      if (masked) mask_row(s, lim.bits(place) >> (hi * 4), [](int i) { return (i >> 2) * 8 + (i & 3); });
     } else if (tile == 0 || tile == tiles - 1) {  // only these reach outside the unit's keys
       const int at0 = base + tile * 32;
 #pragma unroll
@@ -1113,7 +1123,7 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     }
   }
   if constexpr (CHUNK) {
-    if (spoils[0] | spoils[1] | spoils[2] | spoils[3]) spoil_rows<float>(a, un, h, 32, wave * 8, min(wave * 8 + 8, rows));
+    if (spoils[0] | spoils[1] | spoils[2] | spoils[3]) spoil_rows<float>(u, h, 32, wave * 8, min(wave * 8 + 8, rows));
   }
 }
 

@@ -43,10 +43,11 @@ constexpr Seen seen(const ChunkSeq& q, const ChunkMask& m, int r) {
 // lo rounded down to 16 on, `skip` places left out before tile skip_at (between
 // the first tokens and a window).
 struct ChunkUnit : AttnUnit {
-  int seq;             // sequence of its rows; -1: a shared history, of which every row sees all
+  int seq;             // sequence of its rows; -1: a shared history, of which every row sees [lo, sink_end) and from
+  int from, sink_end;  // place `from` on
   int tiles;
   int skip_at, skip;
-  int all_lo, all_hi;  // every row sees every place of them
+  int free_lo, free_n;  // of the tiles from free_lo on, every row sees all of free_n
 };
 
 struct ChunkPlan {
@@ -60,26 +61,68 @@ struct ChunkPlan {
 
 namespace plan_detail {
 
-// The tiles of rows [r0, r1) of a sequence, from place `from` on (0: all they see).
+// Tiles over places [lo, hi); those from free_lo to free_hi hide nothing from any row.
 struct TileRun {
-  int lo, hi, tiles, skip_at, skip, all_lo, all_hi;
+  int lo, hi, tiles = 0, skip_at = 0, skip = 0, free_lo = 0, free_hi = 0;
   int at(int j) const { return (lo & ~15) + 64 * j + (j >= skip_at ? skip : 0); }
+  // every row sees places [all_lo, all_hi), and before them and behind them there is no tile of which all rows see all
+  void free_between(int all_lo, int all_hi) {
+    tiles = std::max(0, (int)cdiv(hi - skip - (lo & ~15), 64));
+    const int main = (lo & ~15) + skip;  // where tile 0 would be without the places left out
+    free_lo = std::max(skip_at, (int)cdiv(std::max(0, all_lo - main), 64));
+    free_hi = std::max(free_lo, std::min(tiles, (std::max(main, all_hi) - main) / 64));
+  }
 };
+// ... of what rows [r0, r1) of a sequence see, from place `from` on (0: all)
 inline TileRun tile_run(const ChunkSeq& q, const ChunkMask& m, int r0, int r1, int from) {
   const Seen a = seen(q, m, r0), b = seen(q, m, r1 - 1);
-  TileRun t{std::max(q.first, from), b.end, 0, 0, 0, 0, 0};
-  t.all_lo = std::max(t.lo, b.begin);
-  t.all_hi = a.end;
-  const int gap_lo = b.sink_end > t.lo ? (t.lo & ~15) + 64 * tiles_of(t.lo, b.sink_end) : t.lo & ~15, gap_hi = a.begin & ~15;
+  TileRun t{std::max(q.first, from), b.end};
+  const int base = t.lo & ~15, sink_tiles = tiles_of(t.lo, b.sink_end), gap_lo = base + 64 * sink_tiles, gap_hi = a.begin & ~15;
+  const int all_lo = std::max(t.lo, b.begin);
   if (gap_hi > gap_lo) {
-    if (b.sink_end > t.lo) t.skip_at = (gap_lo - (t.lo & ~15)) / 64, t.skip = gap_hi - gap_lo;
+    if (sink_tiles > 0) t.skip_at = sink_tiles, t.skip = gap_hi - gap_lo;
     else t.lo = a.begin;
   }
-  t.tiles = std::max(0, (int)cdiv(t.hi - t.skip - (t.lo & ~15), 64));
+  t.free_between(all_lo, a.end);
   return t;
 }
 
 }  // namespace plan_detail
+
+// What every row of a batch sees of the places up to shared_end, whose pages
+// are the same in all its sequences: [first, sink_end) and [from, to).
+struct SharedRun {
+  int first, sink_end, from, to;
+  bool any() const { return to > from; }
+  plan_detail::TileRun run() const {
+    plan_detail::TileRun t{sink_end > first || from == first ? first : from, to};
+    if (sink_end > first) {
+      const int sink_tiles = plan_detail::tiles_of(first, sink_end), gap_lo = (first & ~15) + 64 * sink_tiles;
+      if (from > gap_lo) t.skip_at = sink_tiles, t.skip = from - gap_lo;
+    }
+    t.free_between(from, to);
+    return t;
+  }
+};
+inline SharedRun shared_run(const std::vector<ChunkSeq>& seqs, const ChunkMask& mask, int shared_end) {
+  SharedRun s{0, 0, 0, 0};
+  if (seqs.size() < 2 || shared_end == 0) return s;
+  const bool window = mask.window != ChunkMask::kNone;
+  s.first = s.from = s.sink_end = seqs[0].first;
+  s.to = shared_end;
+  int begin = shared_end;
+  for (const ChunkSeq& q : seqs) {
+    const Seen a = seen(q, mask, 0), b = seen(q, mask, q.rows - 1);
+    s.from = std::max(s.from, b.begin);
+    s.to = std::min(s.to, a.end);
+    begin = std::min(begin, a.begin);
+    if (window) s.sink_end = std::max(s.sink_end, b.sink_end);
+  }
+  s.to &= ~15;
+  if (s.from > s.first) s.from = (s.from + 15) & ~15;
+  if (window && begin < s.sink_end) s.to = 0;  // windows that reach into the first tokens
+  return s;
+}
 
 // As plan_attention, for rows under a mask: the same kernels with the same
 // times, blocks of rows of unequal length.  shared_end: the place up to which
@@ -89,16 +132,22 @@ inline ChunkPlan plan_chunk(const std::vector<ChunkSeq>& seqs, const ChunkMask& 
   using namespace plan_detail;
   ChunkPlan best;
   long long rows = 0;
-  int wholly = shared_end;  // what every row sees of the shared places
-  for (const ChunkSeq& q : seqs) rows += q.rows, wholly = std::min(wholly, seen(q, mask, 0).end);
+  for (const ChunkSeq& q : seqs) rows += q.rows;
   if (rows == 0) return best;
-  wholly &= ~15;
-  if (mask.window != ChunkMask::kNone || seqs.size() < 2 || wholly <= seqs[0].first) wholly = 0;
+  const SharedRun shared = shared_run(seqs, mask, shared_end);
+  const TileRun shared_tiles = shared.run();
+  // what rows [r0, r1) of a sequence see besides a shared history: before it and behind it
+  auto before = [&](const ChunkSeq& q, int r0, int r1) {
+    TileRun t{seen(q, mask, r0).begin, shared.from};
+    if (t.hi > t.lo) t.free_between(seen(q, mask, r1 - 1).begin, shared.from);
+    return t;
+  };
+  auto behind = [&](const ChunkSeq& q, int r0, int r1) { return tile_run(q, mask, r0, r1, shared.to); };
   const double row_bytes = (double)sh.kv_heads * sh.group * (sh.D * 4 + 8);
 
   struct Like {
     int tiles;  // of the longest
-    bool tall;
+    bool tall, front;
     long long blocks = 0;
   };
   auto slots_of = [](int tiles, int c) { return tiles ? (int)cdiv(tiles, c) : 0; };
@@ -118,30 +167,39 @@ inline ChunkPlan plan_chunk(const std::vector<ChunkSeq>& seqs, const ChunkMask& 
     if (k.few && have && most_rows > 64 * kper) continue;  // (whole chunks: many workgroups to price, and never the cheaper)
     const long long places = (long long)k.per_cu * sh.cus;
     for (const bool packed : {false, true}) {
-      if (packed && wholly == 0) break;
-      const int from = packed ? wholly : 0;
+      if (packed && !shared.any()) break;
       std::vector<Like> likes;
       std::vector<int> like_of;  // of the blocks
       std::unordered_map<uint64_t, int> known;
-      double keys = packed ? wholly - seqs[0].first : 0;
-      int longest = 0;
+      double keys = packed ? shared_tiles.tiles * 64 : 0;
+      int longest = packed ? shared_tiles.tiles : 0;
+      auto count = [&](const TileRun& t, bool tall, bool front) {
+        const uint64_t key = (uint64_t)scale_of(t.tiles) << 2 | (tall ? 2 : 0) | (front ? 1 : 0);
+        const int at = known.emplace(key, (int)likes.size()).first->second;
+        if (at == (int)likes.size()) likes.push_back({t.tiles, tall, front});
+        likes[at].tiles = std::max(likes[at].tiles, t.tiles);
+        ++likes[at].blocks;
+        longest = std::max(longest, t.tiles);
+        return at;
+      };
       for (const ChunkSeq& q : seqs) {
-        int seq_keys = 0;
+        int seq_tiles = 0;
         for (int r = 0; r < q.rows; r += kper) {
           const int r1 = std::min(q.rows, r + kper);
-          const TileRun t = tile_run(q, mask, r, r1, from);
           const bool tall = (r1 - r) * sh.group > 32;
-          const int at = known.emplace((uint64_t)scale_of(t.tiles) << 1 | (tall ? 1 : 0), (int)likes.size()).first->second;
-          if (at == (int)likes.size()) likes.push_back({t.tiles, tall});
-          likes[at].tiles = std::max(likes[at].tiles, t.tiles);
-          ++likes[at].blocks;
-          like_of.push_back(at);
-          longest = std::max(longest, t.tiles);
-          seq_keys = std::max(seq_keys, t.tiles * 64);
+          const TileRun t = packed ? behind(q, r, r1) : tile_run(q, mask, r, r1, 0);
+          int tiles = t.tiles;
+          like_of.push_back(count(t, tall, false));
+          if (packed && shared.from > shared.first) {
+            const TileRun f = before(q, r, r1);
+            count(f, tall, true);
+            tiles += f.tiles;
+          }
+          seq_tiles = std::max(seq_tiles, tiles);
         }
-        keys += seq_keys;
+        keys += seq_tiles * 64;
       }
-      const int together = packed ? tiles_of(seqs[0].first, wholly) : 0;
+      const int together = packed ? shared_tiles.tiles : 0;
       const long long blocks = (long long)like_of.size(), shared_blocks = packed ? cdiv(rows, kper) : 0;
       Work w;
       auto add = [&](long long n, int tiles, bool tall, int c) {
@@ -160,15 +218,16 @@ inline ChunkPlan plan_chunk(const std::vector<ChunkSeq>& seqs, const ChunkMask& 
       };
       for (size_t i = 0; i <= kNumCuts + 1; ++i) {
         // past the list: as many pieces as the slots hold, one
-        const int c = i < kNumCuts ? kCuts[i] : i == kNumCuts ? (int)cdiv(std::max(longest, together), kPlanMaxSlots - 6) : kWhole;
-        if (c != kWhole && (c == 0 || c >= std::max(longest, together))) continue;  // kWhole is the same
+        const int c = i < kNumCuts ? kCuts[i] : i == kNumCuts ? (int)cdiv(longest, kPlanMaxSlots / 3 - 2) : kWhole;
+        if (c != kWhole && (c == 0 || c >= longest)) continue;  // kWhole is the same
         long long groups = shared_blocks * slots_of(together, c);
-        int most = 0;
+        int most_of[2] = {0, 0};
         for (const Like& l : likes) {
-          most = std::max(most, slots_of(l.tiles, c));
+          most_of[l.front] = std::max(most_of[l.front], slots_of(l.tiles, c));
           groups += l.blocks * slots_of(l.tiles, c);
         }
         if (c != kWhole && groups * sh.kv_heads > 8 * places) continue;  // rounds enough with longer pieces
+        const int most = most_of[0] + most_of[1];
         const int slots = packed ? slots_of(together, c) + most : most > 1 ? most : 0;
         const double bytes = slots * row_bytes * rows;
         if (slots > kPlanMaxSlots || bytes > (double)max_piece_bytes) continue;
@@ -179,22 +238,21 @@ inline ChunkPlan plan_chunk(const std::vector<ChunkSeq>& seqs, const ChunkMask& 
       // the last blocks of rows, those past the last full round, in pieces
       const long long over = blocks * sh.kv_heads % places;
       if (packed || blocks * sh.kv_heads <= places || over == 0) continue;
-      for (int more = 0; more < 2; ++more)
+      for (long long tail : {cdiv(over, sh.kv_heads), cdiv(over, sh.kv_heads) + 1, blocks / 2, blocks * 3 / 4}) {
+        if (tail >= blocks || tail == 0) continue;
+        std::vector<long long> cut(likes.size());
+        for (long long i = blocks - tail; i < blocks; ++i) ++cut[like_of[i]];
         for (int pieces : {2, 3, 4, 6, 8}) {
-          const long long tail = cdiv(over, sh.kv_heads) + more;
-          if (tail >= blocks) continue;
           const double bytes = (double)pieces * tail * kper * row_bytes;
           if (bytes > (double)max_piece_bytes) continue;
-          std::vector<long long> whole;
-          for (const Like& l : likes) whole.push_back(l.blocks);
-          for (long long i = blocks - tail; i < blocks; ++i) {
-            const Like& l = likes[like_of[i]];
-            --whole[like_of[i]];
-            add(1, l.tiles, l.tall, (int)std::max(1ll, cdiv(l.tiles, pieces)));
+          for (size_t i = 0; i < likes.size(); ++i) {
+            const Like& l = likes[i];
+            add(cut[i], l.tiles, l.tall, (int)std::max(1ll, cdiv(l.tiles, pieces)));
+            add(l.blocks - cut[i], l.tiles, l.tall, kWhole);
           }
-          for (size_t i = 0; i < likes.size(); ++i) add(whole[i], likes[i].tiles, likes[i].tall, kWhole);
           take(time() + kMergeUs + bytes / kPieceBytesPerUs, kWhole, (int)tail, pieces);
         }
+      }
     }
   }
 
@@ -207,17 +265,18 @@ inline ChunkPlan plan_chunk(const std::vector<ChunkSeq>& seqs, const ChunkMask& 
       u.lo = i == 0 ? t.lo : t.at(j0);
       u.hi = i == n - 1 ? t.hi : t.at(j1 - 1) + 64;
       u.slot = direct && n == 1 ? -1 : slot0 + i;
+      if (seq < 0) u.from = shared.from, u.sink_end = shared.sink_end;
       if (t.skip > 0 && t.skip_at > j0 && t.skip_at < j1) u.skip_at = t.skip_at - j0, u.skip = t.skip;
-      u.all_lo = t.all_lo, u.all_hi = t.all_hi;
+      u.free_lo = std::min(std::max(t.free_lo - j0, 0), u.tiles);
+      u.free_n = std::max(0, std::min(t.free_hi - j0, u.tiles) - u.free_lo);
       best.units.push_back(u);
     }
     return n;
   };
   if (best_packed) {
-    TileRun t{seqs[0].first, wholly, tiles_of(seqs[0].first, wholly), 0, 0, seqs[0].first, wholly};
     int n = 0;
     for (long long r = 0; r < rows; r += per)
-      n = emit(t, -1, seqs[0].table, (int)r, (int)std::min<long long>(per, rows - r), 0, false, best_c);
+      n = emit(shared_tiles, -1, seqs[0].table, (int)r, (int)std::min<long long>(per, rows - r), 0, false, best_c);
     best.shared_slots = best.n_slots = n;
   }
   long long blocks = 0, block = 0;
@@ -227,9 +286,12 @@ inline ChunkPlan plan_chunk(const std::vector<ChunkSeq>& seqs, const ChunkMask& 
     const ChunkSeq& q = seqs[i];
     for (int r = 0; r < q.rows; r += per, ++block) {
       const int r1 = std::min(q.rows, r + per);
-      const TileRun t = tile_run(q, mask, r, r1, best_packed ? wholly : 0);
+      const TileRun t = best_packed ? behind(q, r, r1) : tile_run(q, mask, r, r1, 0);
       const int c = block >= blocks - best_tail ? (int)std::max(1ll, cdiv(t.tiles, best_pieces)) : best_c;
-      const int n = emit(t, (int)i, q.table, q.row0 + r, r1 - r, best.shared_slots, !best_packed, c);
+      int n = 0;
+      if (best_packed && shared.from > shared.first)
+        n = emit(before(q, r, r1), (int)i, q.table, q.row0 + r, r1 - r, best.shared_slots, false, c);
+      n += emit(t, (int)i, q.table, q.row0 + r, r1 - r, best.shared_slots + n, !best_packed, c);
       const OwnSlots own{best.shared_slots, !best_packed && n == 1 ? 0 : n};
       if (!best.parts.empty() && best.parts.back().seq == (int)i && best.parts.back().own.n == own.n)
         best.parts.back().rows += r1 - r;
