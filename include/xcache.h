@@ -606,7 +606,8 @@ xc_status xc_chunk_attention(xc_batch* batch, int32_t block, const void* q, int6
  *              the longest sequence; does not overlap q, lse or the page
  *              buffers.
  * The same call gives the same bits.  Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE
- * (as xc_chunk_attention), XC_ERR_HIP (sticky). */
+ * (as xc_chunk_attention), XC_ERR_UNSUPPORTED (rows of q of 256 MiB or more
+ * apart), XC_ERR_HIP (sticky). */
 xc_status xc_chunk_weights(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, const float* lse,
                            float decay, float* weights, int64_t ld);
 

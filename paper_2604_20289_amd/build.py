@@ -28,10 +28,11 @@ SOURCES = [
     "xc_diag.hip",
     "xc_pages.hip",
     "xc_branch.hip",
-    "xc_chunk.hip",
+    "xc_weights.hip",
+    "xc_evict.hip",
     "xc_capi.cpp",
     "xc_pool.cpp",
-    "xc_chunk_host.cpp",
+    "xc_chunk.cpp",
 ]
 
 ARCH = "gfx950"

@@ -42,11 +42,26 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     const ChunkSeq& q = chunk_seqs[part.seq];
     batch_seqs.push_back({part.tok0, q.first + q.tokens - q.rows + (part.tok0 - q.row0), q.table, part.own});
   }
+  // the sums of weights: where all sequences have few rows, or with partial sums
+  int groups = 0;
+  const std::vector<WeightRun> runs = plan_weight_runs(chunk_seqs, r.shared_end, shape, &groups);
+  const bool few = p.esz == 2 && !runs.empty();
+  WeightPlan sums;
+  if (!few) sums = plan_weights(chunk_seqs, mask, shape);
+  const size_t part_need =
+      (size_t)sums.parts * p.cfg.kv_heads * (p.esz == 2 ? kWeightKeys : kWeightKeysF32) * sizeof(float);
+  if ((((long long)sums.units.size() + kXcds) * p.cfg.kv_heads + kXcds * kXcds) * 256 >> 32 || (long long)groups * 256 >> 32 ||
+      (long long)sums.tiles.size() * 256 >> 32)
+    return XC_ERR_UNSUPPORTED;
+  if (!enlarge(p, b->parts, b->part_bytes, part_need, part_need / 4)) return XC_ERR_OOM;
   // uploaded: tables, sequences, units; written on the device: places, own slots
   const size_t o_seqs = align256(r.tables.size() * sizeof(int));
   const size_t o_chunks = o_seqs + align256(batch_seqs.size() * sizeof(BatchSeq));
   const size_t o_units = o_chunks + align256(chunk_seqs.size() * sizeof(ChunkSeq));
-  const size_t up = o_units + align256(plan.units.size() * sizeof(ChunkUnit));
+  const size_t o_runs = o_units + align256(plan.units.size() * sizeof(ChunkUnit));
+  const size_t o_sums = o_runs + align256((few ? runs.size() : 0) * sizeof(WeightRun));
+  const size_t o_tiles = o_sums + align256(sums.units.size() * sizeof(WeightUnit));
+  const size_t up = o_tiles + align256(sums.tiles.size() * sizeof(WeightTile));
   const size_t o_own = up + align256(rows * sizeof(int));
   const size_t need = o_own + align256(rows * sizeof(OwnSlots));
   std::vector<int> seq_copy(seqs, seqs + n);
@@ -56,6 +71,9 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     put(b, o_seqs, batch_seqs);
     put(b, o_chunks, chunk_seqs);
     put(b, o_units, plan.units);
+    if (few) put(b, o_runs, runs);
+    put(b, o_sums, sums.units);
+    put(b, o_tiles, sums.tiles);
     upload(b, b->dev, up);
     XC_HIP(launch_batch_rows((const int*)b->dev, (const BatchSeq*)(b->dev + o_seqs), (int)batch_seqs.size(), r.rows, shift,
                              (int*)(b->dev + up), (OwnSlots*)(b->dev + o_own), p.st));
@@ -79,14 +97,23 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   a.piece_row0 = plan.piece_row0;
   a.piece_rows = r.rows - plan.piece_row0;
   a.few = plan.few;
-  ChunkArgs& c = b->chunks;
-  c.tables = a.tables;
-  c.seqs = a.chunk_seqs;
-  c.n_seqs = n_rows;
-  c.rows = r.rows;
-  c.q_heads = p.cfg.q_heads;
-  c.group = group;
-  c.mask = mask;
+  WeightArgs& w = b->weights;
+  w = {};
+  w.tables = a.tables;
+  w.seqs = a.chunk_seqs;
+  w.mask = mask;
+  w.q_heads = p.cfg.q_heads;
+  w.group = group;
+  w.by_group = group == 1 ? 0 : (unsigned)(((1ull << 32) + group - 1) / group);
+  w.units = (const WeightUnit*)(b->dev + o_sums);
+  w.tiles = (const WeightTile*)(b->dev + o_tiles);
+  w.n_units = (int)sums.units.size();
+  w.n_long = long_units(sums.units);
+  w.n_tiles = (int)sums.tiles.size();
+  w.parts = (float*)b->parts;
+  w.runs = (const WeightRun*)(b->dev + o_runs);
+  w.n_runs = few ? (int)runs.size() : 0;
+  w.n_groups = few ? groups : 0;
   b->place = (const int*)(b->dev + up);
   b->rows = r.rows;
   b->seqs.swap(seq_copy);
@@ -171,6 +198,7 @@ xc_status xc_chunk_weights(xc_batch* b, int32_t block, const void* q, int64_t q_
   if (s == 0.f) return XC_ERR_INVALID_ARG;
   return guarded(p, [&]() -> xc_status {
     if (!b->current() || !b->chunk) return XC_ERR_STATE;
+    if (q_ld * p.esz >> 28) return XC_ERR_UNSUPPORTED;  // 8 rows within 32 bits
     if (b->rows == 0) return XC_OK;
     int most = 0;
     for (int seq : b->seqs) most = std::max(most, p.book.seq(seq).tokens);
@@ -178,8 +206,7 @@ xc_status xc_chunk_weights(xc_batch* b, int32_t block, const void* q, int64_t q_
     const Rows in = rows_at(q, b->rows, q_ld, width, p.esz), sums = rows_at(lse, b->rows, c.q_heads, c.q_heads, 4),
                to = rows_at(weights, (long long)b->seqs.size(), ld, most, 4);
     if (overlap(in, to) || overlap(sums, to) || p.holds(weights, to.extent)) return XC_ERR_INVALID_ARG;
-    ChunkWeightArgs a{};
-    a.c = b->chunks;
+    WeightArgs a = b->weights;
     a.buf = p.block(block);
     a.q = q;
     a.q_ld = q_ld;
@@ -188,7 +215,7 @@ xc_status xc_chunk_weights(xc_batch* b, int32_t block, const void* q, int64_t q_
     a.decay = decay;
     a.weights = weights;
     a.ld = ld;
-    XC_HIP(launch_chunk_weights(c.dtype, a, most, p.st));
+    XC_HIP(launch_weights(c.dtype, a, p.st));
     return XC_OK;
   });
 }

@@ -7,24 +7,27 @@
 
 namespace xc {
 
-// What xc_chunk_set leaves to the calls.
-struct ChunkArgs {
+// What xc_chunk_set leaves to the sums of weights: units and tiles, or, where
+// all sequences have few rows, runs.
+struct WeightArgs {
+  PageBuf buf;
   const int* tables;
   const ChunkSeq* seqs;
-  int n_seqs, rows;
-  int q_heads, group;  // group: query heads per key head
   ChunkMask mask;
-};
-
-struct ChunkWeightArgs {
-  ChunkArgs c;
-  PageBuf buf;
-  const void* q;  // [rows][q_ld]
+  int q_heads, group;  // group: query heads per key head
+  unsigned by_group;   // 2^32 / group rounded up, 0 for 1: r / group is the high half of r * by_group
+  const WeightUnit* units;
+  const WeightTile* tiles;
+  int n_units, n_long, n_tiles;
+  float* parts;        // [part][key head][kWeightKeys] (float32 pools: kWeightKeysF32)
+  const WeightRun* runs;
+  int n_runs, n_groups;
+  const void* q;       // [rows][q_ld]
   long long q_ld;
-  float scale;      // of q . k, in log2 units
-  const float* lse;  // [rows][q_heads]
+  float scale;         // of q . k, in log2 units
+  const float* lse;    // [rows][q_heads]
   float decay;
-  float* weights;  // [sequence][ld]
+  float* weights;      // [sequence][ld]
   long long ld;
 };
 
@@ -47,8 +50,7 @@ struct EvictArgs {
   long long kept_ld;
 };
 
-// most: tokens of the longest sequence with rows
-hipError_t launch_chunk_weights(int dtype, const ChunkWeightArgs& a, int most, hipStream_t st);
+hipError_t launch_weights(int dtype, const WeightArgs& a, hipStream_t st);
 // whole: the first block; most: of the keeps
 hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes, int most,
                         hipStream_t st);

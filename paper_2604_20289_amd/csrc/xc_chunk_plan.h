@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <utility>
 #include <vector>
 
 #include "xc_branch_plan.h"
@@ -309,6 +310,168 @@ inline ChunkPlan plan_chunk(const std::vector<ChunkSeq>& seqs, const ChunkMask& 
 inline int long_units(const std::vector<ChunkUnit>& units) {  // sorted
   int n = 0;
   while (n < (int)units.size() && units[n].tiles > units[0].tiles / 2) ++n;
+  return n;
+}
+
+// ---- the weights of keys
+
+struct RowRange {
+  int begin, end;
+};
+// Rows of the sequence that see some, and that see all, of its places [k0, k1):
+// both runs of rows, since what a row sees of the places past the first tokens
+// moves on with it.
+constexpr RowRange rows_seeing_some(const ChunkSeq& q, const ChunkMask& m, int k0, int k1) {
+  const long long old = q.first + (long long)q.tokens - q.rows, g = m.group < q.rows ? m.group : q.rows;
+  const long long x = k0 - old, y = k1 - old + m.window;  // r sees some: groups_end > x, groups_end < y
+  RowRange r{0, q.rows};
+  if (x >= q.rows) r.begin = q.rows;
+  else if (x >= 0) r.begin = (int)(x / g * g);
+  if (k0 - q.first >= m.sinks && y <= q.rows) {
+    const long long n = (y + g - 1) / g - 1;
+    r.end = n > 0 ? (int)(n * g) : 0;
+  }
+  if (r.end > q.rows) r.end = q.rows;
+  if (r.end < r.begin) r.end = r.begin;
+  return r;
+}
+constexpr RowRange rows_seeing_all(const ChunkSeq& q, const ChunkMask& m, int k0, int k1) {
+  const long long old = q.first + (long long)q.tokens - q.rows, g = m.group < q.rows ? m.group : q.rows;
+  const long long x = k1 - old, y = k0 - old + m.window;  // r sees all: groups_end >= x, groups_end <= y
+  RowRange r{0, q.rows};
+  if (x > q.rows) r.begin = q.rows;
+  else if (x > 0) r.begin = (int)(((x + g - 1) / g - 1) * g);
+  if (k1 - q.first > m.sinks && y < q.rows) r.end = y >= g ? (int)(y / g * g) : 0;
+  if (r.end < r.begin) r.end = r.begin;
+  return r;
+}
+
+// Keys of a workgroup, query rows of a stage of its queries.
+constexpr int kWeightKeys = 256, kWeightKeysF32 = 128, kWeightRows = 64, kWeightRowsF32 = 32;
+// A workgroup's share: what rows [r0, r1) of a sequence give to the keys at
+// places [lo, hi); its sums are partial sums number `part`.
+struct WeightUnit {
+  int seq, lo, hi, r0, r1, part;
+};
+// Keys whose partial sums are joined: numbers part .. part + parts - 1.
+struct WeightTile {
+  int seq, lo, hi, part, parts;
+};
+struct WeightPlan {
+  std::vector<WeightUnit> units;  // the long ones first
+  std::vector<WeightTile> tiles;  // all keys
+  int parts = 0;
+};
+
+// Few rows: the keys of a run of places and the query rows of sequences
+// seq0 .. seq0 + n_seqs - 1, at most kWeightFew of them, which all have these
+// places.  Its workgroups begin at number `group0`.
+constexpr int kWeightFew = 64;
+struct WeightRun {
+  int seq0, n_seqs, lo, hi, group0;
+};
+// Key tiles of a wave of the kernel of few rows, waves that share the heads of
+// one, keys of a workgroup.
+constexpr int few_keys(int D) { return D == 128 ? 32 : 64; }
+constexpr int few_head_waves(int kv_heads) { return kv_heads >= 4 ? 4 : kv_heads >= 2 ? 2 : 1; }
+constexpr int few_group_keys(int D, int kv_heads) { return few_keys(D) * 4 / few_head_waves(kv_heads); }
+
+// The runs of a batch whose sequences all have few rows; empty: not all do.  A
+// shared history is read once for as many sequences as fit.
+inline std::vector<WeightRun> plan_weight_runs(const std::vector<ChunkSeq>& seqs, int shared_end, const PlanShape& sh,
+                                               int* groups) {
+  std::vector<WeightRun> runs;
+  *groups = 0;
+  for (const ChunkSeq& q : seqs)
+    if ((long long)q.rows * sh.group > kWeightFew) return runs;
+  const int keys = few_group_keys(sh.D, sh.kv_heads);
+  auto add = [&](int seq0, int n, int lo, int hi) {
+    if (hi <= lo) return;
+    runs.push_back({seq0, n, lo, hi, *groups});
+    *groups += (int)plan_detail::cdiv(hi - (lo & ~15), keys);
+  };
+  for (size_t i = 0; shared_end > 0 && i < seqs.size();) {
+    size_t j = i;
+    int rows = 0;
+    while (j < seqs.size() && rows + seqs[j].rows * sh.group <= kWeightFew) rows += seqs[j++].rows * sh.group;
+    add((int)i, (int)(j - i), seqs[i].first, shared_end);
+    i = j;
+  }
+  for (size_t i = 0; i < seqs.size(); ++i)
+    add((int)i, 1, std::max(seqs[i].first, shared_end), seqs[i].first + seqs[i].tokens);
+  return runs;
+}
+
+// Rows in runs of about as many stages as give every place several workgroups:
+// the time of each is that of its stages and a start.  Measured: PLACEHOLDER
+inline WeightPlan plan_weights(const std::vector<ChunkSeq>& seqs, const ChunkMask& mask, const PlanShape& sh) {
+  using namespace plan_detail;
+  const bool f32 = sh.elem == 4;
+  const int keys = f32 ? kWeightKeysF32 : kWeightKeys, per = f32 ? kWeightRowsF32 : kWeightRows;
+  WeightPlan plan;
+  struct Rows {
+    RowRange r;
+    int stages;
+  };
+  std::vector<Rows> rows;
+  std::vector<std::pair<int, long long>> kinds;  // stages, tiles
+  std::unordered_map<int, int> known;
+  int longest = 0;
+  for (size_t i = 0; i < seqs.size(); ++i) {
+    const ChunkSeq& q = seqs[i];
+    for (int k = 0; k < q.tokens; k += keys) {
+      const int lo = q.first + k, hi = q.first + std::min(q.tokens, k + keys);
+      const RowRange r = rows_seeing_some(q, mask, lo, hi);
+      const int stages = (int)cdiv((long long)(r.end - r.begin) * sh.group, per);
+      plan.tiles.push_back({(int)i, lo, hi, 0, 0});
+      rows.push_back({r, stages});
+      longest = std::max(longest, stages);
+      if (stages == 0) continue;
+      const int at = known.emplace(scale_of(stages), (int)kinds.size()).first->second;
+      if (at == (int)kinds.size()) kinds.push_back({stages, 0});
+      kinds[at].first = std::max(kinds[at].first, stages);
+      ++kinds[at].second;
+    }
+  }
+  const int per_cu = 2;
+  const double stage_us = f32 ? 0.031 * sh.D : sh.D == 128 ? 0.55 : 0.4, start_us = 4.0;
+  const long long places = (long long)per_cu * sh.cus;
+  double best_us = 0;
+  int best_c = 1;
+  static const int kCuts[] = {1, 2, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 512, 1024, 4096, 16384, 65536};
+  Work w;
+  bool have = false;
+  for (int c : kCuts) {
+    long long groups = 0;
+    for (const auto& k : kinds) groups += k.second * cdiv(k.first, c);
+    if (groups * sh.kv_heads > 16 * places && c < longest) continue;  // rounds enough with longer runs
+    for (const auto& k : kinds) {
+      const long long n = cdiv(k.first, c);
+      w.add(k.second * n * sh.kv_heads, (double)k.first / n * stage_us + start_us);
+    }
+    const double us = w.us(places, 0.5 * places) + (double)groups * sh.kv_heads * keys * 8 / kPieceBytesPerUs;
+    w.kinds.clear();
+    if (!have || us < best_us) have = true, best_us = us, best_c = c;
+    if (c >= longest) break;
+  }
+  for (size_t i = 0; i < plan.tiles.size(); ++i) {
+    WeightTile& t = plan.tiles[i];
+    const int n = (int)cdiv(rows[i].stages, best_c), tokens = rows[i].r.end - rows[i].r.begin;
+    t.part = plan.parts;
+    for (int j = 0; j < n; ++j) {
+      const int a = (int)((long long)tokens * j / n), b = (int)((long long)tokens * (j + 1) / n);
+      if (a == b) continue;
+      plan.units.push_back({t.seq, t.lo, t.hi, rows[i].r.begin + a, rows[i].r.begin + b, plan.parts++});
+    }
+    t.parts = plan.parts - t.part;
+  }
+  std::stable_sort(plan.units.begin(), plan.units.end(),
+                   [](const WeightUnit& x, const WeightUnit& y) { return x.r1 - x.r0 > y.r1 - y.r0; });
+  return plan;
+}
+inline int long_units(const std::vector<WeightUnit>& units) {  // sorted
+  int n = 0;
+  while (n < (int)units.size() && units[n].r1 - units[n].r0 > (units[0].r1 - units[0].r0) / 2) ++n;
   return n;
 }
 

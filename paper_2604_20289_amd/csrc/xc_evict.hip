@@ -1,6 +1,5 @@
-// Kernels of chunks under a mask besides their attention (which is that of
-// branches, xc_branch.hip): the weight that it gives to cached keys, and the
-// eviction of the light ones.
+// Evictions: which tokens a sequence keeps, and their keys and values moved
+// to its first places.
 #include "xc_chunk.h"
 
 #include "xc_internal.h"
@@ -12,40 +11,6 @@ namespace xc {
 namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ bool sees(const Seen& w, int at) { return at < w.end && (at >= w.begin || at < w.sink_end); }
-
-// A lane per key of a sequence, which keeps the key's row of one head at a time
-// and meets all rows' queries.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void chunk_weights_kernel(ChunkWeightArgs a) {
-  const ChunkSeq s = a.c.seqs[blockIdx.y];
-  const int j = blockIdx.x * 64 + threadIdx.x;
-  if (j >= s.tokens) return;
-  const int at = s.first + j, kv = a.buf.kv_heads, shift = a.buf.shift;
-  const long long page = a.c.tables[s.table + (at >> shift)];
-  float sum = 0.f;
-  for (int h = 0; h < kv; ++h) {
-    const T* kp = reinterpret_cast<const T*>(a.buf.keys) + (((page * kv + h) << shift) + (at & ((1 << shift) - 1))) * D;
-    float k[D];
-    for (int d = 0; d < D; ++d) k[d] = (float)kp[d];
-    for (int r = 0; r < s.rows; ++r) {
-      const Seen w = seen(s, a.c.mask, r);
-      if (!sees(w, at)) continue;
-      for (int g = 0; g < a.c.group; ++g) {
-        const int qh = h * a.c.group + g;
-        const T* q = reinterpret_cast<const T*>(a.q) + (s.row0 + r) * a.q_ld + (long long)qh * D;
-        float x = 0.f;
-        for (int d = 0; d < D; ++d) x += (float)q[d] * k[d];
-        sum += exp2f(x * a.scale - a.lse[(long long)(s.row0 + r) * a.c.q_heads + qh] * 1.4426950408889634f);
-      }
-    }
-  }
-  float* to = a.weights + s.number * a.ld + j;
-  *to = a.decay == 0.f ? sum : *to * a.decay + sum;
-}
-
-// ---------------------------------------------------------------- eviction
 
 // Order of the weights as whole numbers: NaN below everything, -0 as +0.
 __device__ __forceinline__ unsigned order_of(float w) {
@@ -218,21 +183,6 @@ __global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a, char* keys
 }
 
 }  // namespace
-
-hipError_t launch_chunk_weights(int dtype, const ChunkWeightArgs& a, int most, hipStream_t st) {
-  const dim3 grid((most + 63) / 64, a.c.n_seqs);
-#define XC_WEIGHTS(T, DD) chunk_weights_kernel<T, DD><<<grid, 64, 0, st>>>(a)
-  if (dtype == 1) {
-    if (a.buf.D == 128) XC_WEIGHTS(bf16, 128);
-    else XC_WEIGHTS(bf16, 64);
-  } else {
-    if (a.buf.D == 128) XC_WEIGHTS(float, 128);
-    else if (a.buf.D == 64) XC_WEIGHTS(float, 64);
-    else XC_WEIGHTS(float, 32);
-  }
-#undef XC_WEIGHTS
-  return hipGetLastError();
-}
 
 hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes, int most,
                         hipStream_t st) {

@@ -127,12 +127,14 @@ struct xc_batch {
   xc::AttnArgs attn{};       // the plan's part of the arguments
   const int* place = nullptr;
   int rows = 0;
-  xc::ChunkArgs chunks{};  // of a chunk batch
+  xc::WeightArgs weights{};  // of a chunk batch
   // buffers
   char* dev = nullptr;
   size_t dev_bytes = 0;
   char* pieces = nullptr;
   size_t piece_bytes = 0;
+  char* parts = nullptr;  // partial sums of weights
+  size_t part_bytes = 0;
   char* evict = nullptr;  // an eviction's tables and choices
   size_t evict_bytes = 0;
   char* pinned = nullptr;

@@ -1,0 +1,555 @@
+// The weight that the rows of a batch give to each token of their sequences:
+// w_j = decay w_j + sum over rows and heads of exp(scale q k_j - lse).
+//
+// S^T = K Q^T on the matrix cores, as in the attention, but a wave keeps its
+// keys' operand in registers and the queries go by: every sum over rows is a
+// lane's own until the end.  Nothing is added by atomics, and every sum has a
+// fixed order.  exp2(x - hi) f, with lse log2(e) = hi + lo rounded apart and f =
+// 2^-lo, keeps what the product with log2(e) would lose of a large lse.
+//
+// Two kinds of workgroup.  Many rows: weights_kernel (float32:
+// weights_f32_kernel), 256 (128) keys of one head against a run of rows, whose
+// partial sums weights_join_kernel adds up.  Few rows: weights_few_kernel, all
+// heads of a few keys, read once for all sequences that have them.
+#include "xc_chunk.h"
+
+#include "xc_internal.h"
+#include "xc_tiles.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+namespace xc {
+
+namespace {
+
+// exp(x ln 2 - lse) = exp2(x - hi) * f
+struct Term {
+  float hi, f;
+};
+__device__ __forceinline__ Term term_of(float lse) {
+  constexpr float kLog2e = 1.44269502162933349609375f, kRest = 1.925963033500e-8f;
+  const float hi = lse * kLog2e, lo = __builtin_fmaf(lse, kLog2e, -hi) + lse * kRest;
+  return {hi, lo == lo ? __builtin_amdgcn_exp2f(-lo) : 1.f};  // (infinite or NaN: hi says it)
+}
+
+// (nothing, where it is no row)
+__device__ __forceinline__ Limits limits_of(const ChunkSeq& q, const ChunkMask& m, int r, bool row) {
+  const Seen w = seen(q, m, r);
+  return {w.begin, row ? w.end : w.begin, q.first, row ? w.sink_end : q.first};
+}
+
+// Element i of a lane's 16 scores: the key's place among the 32 of its half
+// tile, less 4 in the upper half wave.
+__device__ __forceinline__ int key_of(int i) { return (i >> 2) * 8 + (i & 3); }
+
+__device__ __forceinline__ unsigned keep_bit(unsigned bits, int at) { return (unsigned)((int)(bits << (31 - at)) >> 31); }
+
+// 4 bytes per lane, global -> LDS
+__device__ __forceinline__ void dma4(const char* base, unsigned off, char* lds) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), (short)0, -1, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 4, (int)off, 0, 0, 0);
+}
+
+// A unit's query rows: query row i is query head i % group of the unit's token i / group.
+struct QueryRows {
+  int n, group;
+  unsigned by_group;
+  __device__ __forceinline__ int token(int i) const { return (int)__umulhi((unsigned)i, by_group) + (group == 1 ? i : 0); }
+  __device__ __forceinline__ int clamped(int i) const { return min(i, n - 1); }
+};
+
+// Sum over the 32 lanes of a half wave of 16 numbers each: lane l (of 16) of the
+// lower (upper) row of 16 lanes gets number l (8 + l), l < 8.
+__device__ __forceinline__ float fold(const f32x16& v, int lane) {
+  float x[8], out = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
+    x[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    auto add = [&](auto ctrl) __attribute__((always_inline)) {
+      x[i] += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x[i]), decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    add(std::integral_constant<int, 0xB1>{});   // lane ^ 1
+    add(std::integral_constant<int, 0x4E>{});   // lane ^ 2
+    add(std::integral_constant<int, 0x141>{});  // the two quads of 8 lanes
+    add(std::integral_constant<int, 0x140>{});  // the two halves of a row of 16
+    if ((lane & 15) == i) out = x[i];
+  }
+  return out;
+}
+
+// 4 waves of 64 keys.  The queries come by in stages of 64 rows, one on its
+// way; products of one tile of 32 rows and exponentials of the one before
+// alternate, two to four of these to a product.  Two workgroups per CU.
+template <int D>
+__global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
+  using F = Frags<D>;
+  constexpr int KCG = F::KCG, KS = F::KS, SLOT = 64 * D * 2, NB = 2 * KCG;  // blocks of a stage per wave
+  // an array per slot: its reads then do not wait for requests into the others
+  __shared__ __attribute__((aligned(1024))) char s0[SLOT];
+  __shared__ __attribute__((aligned(1024))) char s1[SLOT];
+  __shared__ __attribute__((aligned(256))) char l0[4 * 256];
+  __shared__ __attribute__((aligned(256))) char l1[4 * 256];
+  int u, h;
+  if (!xcd_pair(blockIdx.x, a.n_units, a.n_long, a.buf.kv_heads, u, h)) return;
+  const WeightUnit un = a.units[u];
+  const ChunkSeq sq = a.seqs[un.seq];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hi = lane >> 5, lo = lane & 31;
+  const QueryRows rows{(un.r1 - un.r0) * a.group, a.group, a.by_group};
+  const int n = (rows.n + 63) >> 6;
+  const long long ld = a.q_ld * 2;
+  const char* q = reinterpret_cast<const char*>(a.q) + (long long)(sq.row0 + un.r0) * ld + (long long)h * a.group * D * 2;
+  const char* lse = reinterpret_cast<const char*>(a.lse + (long long)(sq.row0 + un.r0) * a.q_heads + h * a.group);
+
+  auto request = [&](int s, char* slot, char* terms) __attribute__((always_inline)) {
+    const int at = s * 64;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int B = wave + 4 * i, rg = B / KCG, cg = B % KCG;
+      const int t0 = rows.token(rows.clamped(at + rg * 8));
+      const int r = rows.clamped(at + rg * 8 + ((lane >> 3) ^ (rg & 1))), t = rows.token(r);
+      dma16(q + t0 * ld, (unsigned)(t - t0) * (unsigned)ld + (r - t * a.group) * (D * 2) + k_block_col(rg, cg, lane), slot + B * 1024);
+    }
+    const int t0 = rows.token(rows.clamped(at)), r = rows.clamped(at + lane), t = rows.token(r);
+    dma4(lse + (long long)t0 * a.q_heads * 4, ((t - t0) * a.q_heads + r - t * a.group) * 4, terms + wave * 256);
+  };
+  request(0, s0, l0);
+
+  const int k0 = un.lo + wave * 64;
+  bf16x8 kf[2][KS];
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt) {
+    const int at = min(k0 + mt * 32 + lo, un.hi - 1);
+    const long long page = a.tables[sq.table + (at >> a.buf.shift)];
+    const bf16* k = reinterpret_cast<const bf16*>(a.buf.keys) +
+                    (((page * a.buf.kv_heads + h) << a.buf.shift) + (at & ((1 << a.buf.shift) - 1))) * D + hi * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kf[mt][ks] = *reinterpret_cast<const bf16x8*>(k + ks * 16);
+  }
+  // tiles [free0, free1) of 32 query rows see all of this wave's keys
+  const RowRange all = rows_seeing_all(sq, a.mask, min(k0, un.hi - 1), min(k0 + 64, un.hi));
+  const int free0 = __builtin_amdgcn_readfirstlane(max(0, (all.begin - un.r0) * a.group + 31) >> 5);
+  const int free1 = __builtin_amdgcn_readfirstlane(min(rows.n, max(0, all.end - un.r0) * a.group) >> 5);
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(kf[mt][ks]));
+
+  f32x16 sa[2], sb[2], acc[2];
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sb[mt][i] = -INFINITY, acc[mt][i] = 0.f;
+  Term ta, tb{0.f, 0.f};
+  const F f(lane);
+  // a tile that hides something: its terms here, and nothing left to add
+  auto masked = [&](int tile, f32x16 (&s)[2], Term& t) __attribute__((always_inline)) {
+    if (tile >= free0 && tile < free1) return;
+    const int r = tile * 32 + lo;
+    const Limits lim = limits_of(sq, a.mask, un.r0 + rows.token(rows.clamped(r)), r < rows.n);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      const unsigned bits = lim.bits(k0 + mt * 32) >> (hi * 4);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][i], a.scale, -t.hi));
+        acc[mt][i] = __builtin_fmaf(__uint_as_float(__float_as_uint(e) & keep_bit(bits, key_of(i))), t.f, acc[mt][i]);
+        s[mt][i] = -INFINITY;
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    t = {0.f, 0.f};
+  };
+  // products of a tile (its half of the stage in slot) with the exponentials of the one before
+  auto tile = [&](const char* slot, int half, f32x16 (&s)[2], const f32x16 (&before)[2], const Term& t) __attribute__((always_inline)) {
+    constexpr int PF = 4, STEPS = 2 * KS, EACH = 32 / STEPS;
+    bf16x8 fr[PF];
+#pragma unroll
+    for (int i = 0; i < PF; ++i) fr[i] = f.k(slot, half, i);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int mt = i & 1, ks = i >> 1;
+      if (ks == 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
+      }
+      s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[mt][ks], fr[ks % PF], s[mt], 0, 0, 0);
+      if (mt == 1 && ks + PF < KS) fr[ks % PF] = f.k(slot, half, ks + PF);
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) {
+        const int x = i * EACH + k;
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(before[x >> 4][x & 15], a.scale, -t.hi));
+        acc[x >> 4][x & 15] = __builtin_fmaf(e, t.f, acc[x >> 4][x & 15]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto stage = [&](int s, const char* slot, const char* terms, char* next, char* next_terms) __attribute__((always_inline)) {
+    XC_WAIT_VM(0);
+    tile_barrier();  // this stage is there, and the one before has been read
+    if (s + 1 < n) request(s + 1, next, next_terms);
+    const float* l = reinterpret_cast<const float*>(terms + wave * 256);
+    const float la = l[lo], lb = l[32 + lo];
+    if (s > 0) masked(2 * s - 1, sb, tb);
+    tile(slot, 0, sa, sb, tb);
+    ta = term_of(la);
+    masked(2 * s, sa, ta);
+    tile(slot, 1, sb, sa, ta);
+    tb = term_of(lb);
+  };
+  for (int s = 0; s < n; s += 2) {
+    stage(s, s0, l0, s1, l1);
+    if (s + 1 < n) stage(s + 1, s1, l1, s0, l0);
+  }
+  masked(2 * n - 1, sb, tb);
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      acc[mt][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(sb[mt][i], a.scale, -tb.hi)), tb.f, acc[mt][i]);
+  float* to = a.parts + ((long long)un.part * a.buf.kv_heads + h) * kWeightKeys + wave * 64;
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt) {
+    const float x = fold(acc[mt], lane);
+    const int i = (lane & 7) + ((lane >> 4) & 1) * 8;
+    if ((lane & 15) < 8) to[mt * 32 + key_of(i) + hi * 4] = x;
+  }
+}
+
+// float32: 4 waves of 32 keys, stages of 32 rows, v_mfma_f32_32x32x2_f32 (both k
+// indices of a product are head dims 8 t + e and 8 t + 4 + e, as in the
+// attention).  Bound by these products.
+template <int D>
+__global__ __launch_bounds__(256) void weights_f32_kernel(WeightArgs a) {
+  constexpr int CH = D / 4, SLOT = 32 * D * 4, NB = SLOT / 4096, RPB = 64 / CH;  // 16-byte chunks of a row, rows of a 1 KB block
+  __shared__ __attribute__((aligned(1024))) char s0[SLOT];
+  __shared__ __attribute__((aligned(1024))) char s1[SLOT];
+  __shared__ __attribute__((aligned(256))) char l0[4 * 256];
+  __shared__ __attribute__((aligned(256))) char l1[4 * 256];
+  int u, h;
+  if (!xcd_pair(blockIdx.x, a.n_units, a.n_long, a.buf.kv_heads, u, h)) return;
+  const WeightUnit un = a.units[u];
+  const ChunkSeq sq = a.seqs[un.seq];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hi = lane >> 5, lo = lane & 31;
+  const QueryRows rows{(un.r1 - un.r0) * a.group, a.group, a.by_group};
+  const int n = (rows.n + 31) >> 5;
+  const long long ld = a.q_ld * 4;
+  const char* q = reinterpret_cast<const char*>(a.q) + (long long)(sq.row0 + un.r0) * ld + (long long)h * a.group * D * 4;
+  const char* lse = reinterpret_cast<const char*>(a.lse + (long long)(sq.row0 + un.r0) * a.q_heads + h * a.group);
+  auto swz = [](int r, int c) __attribute__((always_inline)) {
+    return c ^ (CH >= 16 ? (r & 7) ^ ((r & 4) << 1) : r & 7);
+  };
+  auto request = [&](int s, char* slot, char* terms) __attribute__((always_inline)) {
+    const int at = s * 32;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int B = wave + 4 * i, row = B * RPB + lane / CH;
+      const int t0 = rows.token(rows.clamped(at + B * RPB)), r = rows.clamped(at + row), t = rows.token(r);
+      dma16(q + t0 * ld, (unsigned)(t - t0) * (unsigned)ld + (r - t * a.group) * (D * 4) + swz(row, lane % CH) * 16,
+            slot + B * 1024);
+    }
+    const int t0 = rows.token(rows.clamped(at)), r = rows.clamped(at + lo), t = rows.token(r);
+    dma4(lse + (long long)t0 * a.q_heads * 4, ((t - t0) * a.q_heads + r - t * a.group) * 4, terms + wave * 256);
+  };
+  request(0, s0, l0);
+  const int k0 = un.lo + wave * 32;
+  f32x4 kf[D / 8];
+  {
+    const int at = min(k0 + lo, un.hi - 1);
+    const long long page = a.tables[sq.table + (at >> a.buf.shift)];
+    const float* k = reinterpret_cast<const float*>(a.buf.keys) +
+                     (((page * a.buf.kv_heads + h) << a.buf.shift) + (at & ((1 << a.buf.shift) - 1))) * D + hi * 4;
+#pragma unroll
+    for (int t = 0; t < D / 8; ++t) kf[t] = *reinterpret_cast<const f32x4*>(k + t * 8);
+  }
+  const RowRange all = rows_seeing_all(sq, a.mask, min(k0, un.hi - 1), min(k0 + 32, un.hi));
+  const int free0 = __builtin_amdgcn_readfirstlane(max(0, (all.begin - un.r0) * a.group + 31) >> 5);
+  const int free1 = __builtin_amdgcn_readfirstlane(min(rows.n, max(0, all.end - un.r0) * a.group) >> 5);
+#pragma unroll
+  for (int t = 0; t < D / 8; ++t) asm volatile("" : "+v"(kf[t]));
+  f32x16 acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+  auto stage = [&](int st, const char* slot, const char* terms, char* next, char* next_terms) __attribute__((always_inline)) {
+    XC_WAIT_VM(0);
+    tile_barrier();  // this stage is there, and the one before has been read
+    if (st + 1 < n) request(st + 1, next, next_terms);
+    const Term t = term_of(reinterpret_cast<const float*>(terms + wave * 256)[lo]);
+    f32x16 s, o;  // two sums: no product waits for the one before it
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = o[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(slot + lo * (D * 4) + swz(lo, j * 2 + hi) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j][e], x[e], s, 0, 0, 0);
+        o = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j][e + 1], x[e + 1], o, 0, 0, 0);
+      }
+    }
+    unsigned bits = ~0u;
+    if (st < free0 || st >= free1) {
+      const int r = st * 32 + lo;
+      const Limits lim = limits_of(sq, a.mask, un.r0 + rows.token(rows.clamped(r)), r < rows.n);
+      bits = lim.bits(k0) >> (hi * 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i] + o[i], a.scale, -t.hi));
+      acc[i] = __builtin_fmaf(__uint_as_float(__float_as_uint(e) & keep_bit(bits, key_of(i))), t.f, acc[i]);
+    }
+  };
+  for (int st = 0; st < n; st += 2) {
+    stage(st, s0, l0, s1, l1);
+    if (st + 1 < n) stage(st + 1, s1, l1, s0, l0);
+  }
+  const float x = fold(acc, lane);
+  const int i = (lane & 7) + ((lane >> 4) & 1) * 8;
+  if ((lane & 15) < 8)
+    a.parts[((long long)un.part * a.buf.kv_heads + h) * kWeightKeysF32 + wave * 32 + key_of(i) + hi * 4] = x;
+}
+
+// Partial sums of a tile of keys, in a fixed order: 1024 threads, as many to a
+// key as there are, each every so many of its sums.
+template <int KEYS>
+__global__ __launch_bounds__(1024) void weights_join_kernel(WeightArgs a) {
+  constexpr int N = 1024 / KEYS;
+  __shared__ float sums[N][KEYS];
+  const WeightTile t = a.tiles[blockIdx.x];
+  const ChunkSeq q = a.seqs[t.seq];
+  const int k = threadIdx.x % KEYS, g = threadIdx.x / KEYS, parts = t.parts * a.buf.kv_heads;
+  const float* from = a.parts + (long long)t.part * a.buf.kv_heads * KEYS + k;
+  float* to = a.weights + q.number * a.ld + (t.lo - q.first + k);
+  const bool mine = g == 0 && t.lo + k < t.hi;
+  const float old = mine && a.decay != 0.f ? *to * a.decay : 0.f;
+  float sum = 0.f;
+  int i = g;
+  for (; i + 3 * N < parts; i += 4 * N) {
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = from[(long long)(i + j * N) * KEYS];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += x[j];
+  }
+  for (; i < parts; i += N) sum += from[(long long)i * KEYS];
+  sums[g][k] = sum;
+  __syncthreads();
+  if (!mine) return;
+  sum = sums[0][k];
+#pragma unroll
+  for (int j = 1; j < N; ++j) sum += sums[j][k];
+  *to = old + sum;
+}
+
+// Few rows: a workgroup has a tile of keys (or 2 or 4 of them, with 2 or 3 key
+// heads or one) and its waves share the heads; each has two K tiles in LDS, one
+// on its way.  A lane has a query row of every head, so its sums of 16 keys go on
+// over all heads; then they meet in LDS, the rows of each sequence and the
+// waves' shares.  What a row does not see is left out there, once for all heads.
+template <int D, int G>
+__device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun& run, char* ring) {
+  using F = Frags<D>;
+  constexpr int KCG = F::KCG, KS = F::KS, KEYS = few_keys(D), HT = KEYS / 32, TILE = KEYS * D * 2, LOADS = TILE / 1024, R = 32 * G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hi = lane >> 5, lo = lane & 31;
+  const int kv = a.buf.kv_heads, hw = few_head_waves(kv), h0 = wave % hw;
+  const int in_page = (1 << a.buf.shift) - 1, last = run.hi - 1;
+  const int group0 = (run.lo & ~15) + (blockIdx.x - run.group0) * (KEYS * 4 / hw), at0 = group0 + wave / hw * KEYS;
+  const ChunkSeq first = a.seqs[run.seq0], end = a.seqs[run.seq0 + run.n_seqs - 1];
+  const QueryRows rows{(end.row0 + end.rows - first.row0) * a.group, a.group, a.by_group};
+
+  // this lane's rows and what they see
+  int token[G];
+  Limits lim[G];
+  bool any = false;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int r = rows.clamped(g * 32 + lo);
+    token[g] = first.row0 + rows.token(r);
+    int s = run.seq0;
+    while (s + 1 < run.seq0 + run.n_seqs && a.seqs[s + 1].row0 <= token[g]) ++s;
+    lim[g] = limits_of(a.seqs[s], a.mask, token[g] - a.seqs[s].row0, g * 32 + lo < rows.n);
+#pragma unroll
+    for (int mt = 0; mt < HT; ++mt) any |= lim[g].bits(at0 + mt * 32) != 0;
+  }
+  const int n = at0 <= last && __builtin_amdgcn_ballot_w64(any) != 0 ? (kv - h0 + hw - 1) / hw : 0;  // heads h0, h0 + hw, ..
+
+  // the groups of 16 places, each in one page; places outside the run read the nearest of it
+  long long page_at[KEYS / 16];
+  unsigned row_at[KEYS / 8];
+  const long long head_bytes = (long long)D * 2 << a.buf.shift;
+#pragma unroll
+  for (int j = 0; j < KEYS / 16; ++j) {
+    const int g0 = min(max(at0 + j * 16, run.lo), last);
+    const long long page = a.tables[first.table + (g0 >> a.buf.shift)];
+    page_at[j] = page * kv * head_bytes;
+  }
+#pragma unroll
+  for (int rg = 0; rg < KEYS / 8; ++rg) {
+    const int at = min(max(at0 + rg * 8 + ((lane >> 3) ^ (rg & 1)), run.lo), last);
+    row_at[rg] = (unsigned)(at & in_page) * (D * 2) + k_block_col(rg, 0, lane);
+  }
+  char* kt = ring + wave * (2 * TILE);
+  auto request = [&](int i) __attribute__((always_inline)) {
+    const char* keys = reinterpret_cast<const char*>(a.buf.keys) + (h0 + i * hw) * head_bytes;
+#pragma unroll
+    for (int rg = 0; rg < KEYS / 8; ++rg)
+#pragma unroll
+      for (int cg = 0; cg < KCG; ++cg)
+        dma16(keys + page_at[rg >> 1], row_at[rg] + cg * 128, kt + (i & 1) * TILE + (rg * KCG + cg) * 1024);
+  };
+  bf16x8 q[2][G][KS];
+  float l[2][G];
+  auto queries = [&](int i, bf16x8 (&x)[G][KS], float (&y)[G]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int r = rows.clamped(g * 32 + lo), head = (h0 + i * hw) * a.group + r - rows.token(r) * a.group;
+      const bf16* p = reinterpret_cast<const bf16*>(a.q) + token[g] * a.q_ld + (long long)head * D + hi * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) x[g][ks] = *reinterpret_cast<const bf16x8*>(p + ks * 16);
+      y[g] = a.lse[(long long)token[g] * a.q_heads + head];
+    }
+  };
+  f32x16 acc[G][HT];
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int mt = 0; mt < HT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[g][mt][i] = 0.f;
+  const F f(lane);
+  // head i, while the next one's (unless it is the last) keys and queries come
+  auto head = [&](int i, auto last, bf16x8 (&x)[G][KS], float (&y)[G], bf16x8 (&nx)[G][KS], float (&ny)[G]) __attribute__((always_inline)) {
+    if constexpr (!last) {
+      request(i + 1);
+      queries(i + 1, nx, ny);
+      XC_WAIT_VM(LOADS + G * (KS + 1));
+    } else {
+      XC_WAIT_VM(0);
+    }
+    asm volatile("" ::: "memory");
+    const char* tile = kt + (i & 1) * TILE;
+    f32x16 s[G][HT];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int mt = 0; mt < HT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[g][mt][r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int mt = 0; mt < HT; ++mt) {
+        const bf16x8 k = f.k(tile, mt, ks);
+#pragma unroll
+        for (int g = 0; g < G; ++g) s[g][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, x[g][ks], s[g][mt], 0, 0, 0);
+      }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const Term t = term_of(y[g]);
+#pragma unroll
+      for (int mt = 0; mt < HT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          acc[g][mt][r] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[g][mt][r], a.scale, -t.hi)), t.f, acc[g][mt][r]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this tile has been read
+  };
+  if (n > 0) {
+    request(0);
+    queries(0, q[0], l[0]);
+  }
+  constexpr std::false_type more{};
+  constexpr std::true_type last_one{};
+  int i = 0;
+  for (; i + 2 < n; i += 2) {
+    head(i, more, q[0], l[0], q[1], l[1]);
+    head(i + 1, more, q[1], l[1], q[0], l[0]);
+  }
+  if (i + 2 == n) {
+    head(i, more, q[0], l[0], q[1], l[1]);
+    head(i + 1, last_one, q[1], l[1], q[0], l[0]);
+  } else if (i + 1 == n) {
+    head(i, last_one, q[0], l[0], q[1], l[1]);
+  }
+  // key k, row r at k * R + (r + k) % R: lanes of different rows (written) or keys (read) meet different banks
+  float* mine = reinterpret_cast<float*>(kt);
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int mt = 0; mt < HT; ++mt) {
+      const unsigned bits = lim[g].bits(at0 + mt * 32) >> (hi * 4);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = mt * 32 + key_of(i) + hi * 4;
+        mine[k * R + ((g * 32 + lo + k) & (R - 1))] = __uint_as_float(__float_as_uint(acc[g][mt][i]) & keep_bit(bits, key_of(i)));
+      }
+    }
+  __syncthreads();
+  const int group_keys = KEYS * 4 / hw;
+  for (int x = threadIdx.x; x < run.n_seqs * group_keys; x += 256) {
+    const int si = x / group_keys, gk = x - si * group_keys, at = group0 + gk, k = gk % KEYS;
+    if (at < run.lo || at > last) continue;
+    const ChunkSeq sq = a.seqs[run.seq0 + si];
+    float* to = a.weights + sq.number * a.ld + (at - sq.first);
+    const int r0 = (sq.row0 - first.row0) * a.group, r1 = r0 + sq.rows * a.group;
+    float sum = 0.f;
+    for (int w = 0; w < hw; ++w) {
+      const float* part = reinterpret_cast<const float*>(ring + (gk / KEYS * hw + w) * (2 * TILE)) + k * R;
+      for (int r = r0; r < r1; ++r) sum += part[(r + k) & (R - 1)];
+    }
+    *to = a.decay == 0.f ? sum : *to * a.decay + sum;
+  }
+}
+template <int D>
+__global__ __launch_bounds__(256, 2) void weights_few_kernel(WeightArgs a) {
+  __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * few_keys(D) * D * 2];
+  int lo = 0, hi = a.n_runs;  // the last run with group0 <= this workgroup
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.runs[mid].group0 <= (int)blockIdx.x) lo = mid;
+    else hi = mid;
+  }
+  const WeightRun run = a.runs[lo];
+  const ChunkSeq first = a.seqs[run.seq0], end = a.seqs[run.seq0 + run.n_seqs - 1];
+  if ((end.row0 + end.rows - first.row0) * a.group > 32) few_weights<D, 2>(a, run, ring);
+  else few_weights<D, 1>(a, run, ring);
+}
+
+}  // namespace
+
+// Requirements (the caller's): D in {64, 128} (float32: 32 too); a row of q is shorter than 2^28 bytes; units and runs
+// name rows, places and partial sums that there are.
+hipError_t launch_weights(int dtype, const WeightArgs& a, hipStream_t st) {
+  const int D = a.buf.D;
+  if (a.n_runs > 0) {
+    if (D == 128) weights_few_kernel<128><<<a.n_groups, 256, 0, st>>>(a);
+    else weights_few_kernel<64><<<a.n_groups, 256, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  const unsigned grid = (unsigned)xcd_grid(a.n_units, a.buf.kv_heads);
+  if (a.n_units > 0) {
+    if (dtype == 1) {
+      if (D == 128) weights_kernel<128><<<grid, 256, 0, st>>>(a);
+      else weights_kernel<64><<<grid, 256, 0, st>>>(a);
+    } else {
+      if (D == 128) weights_f32_kernel<128><<<grid, 256, 0, st>>>(a);
+      else if (D == 64) weights_f32_kernel<64><<<grid, 256, 0, st>>>(a);
+      else weights_f32_kernel<32><<<grid, 256, 0, st>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (dtype == 1) weights_join_kernel<kWeightKeys><<<a.n_tiles, 1024, 0, st>>>(a);
+  else weights_join_kernel<kWeightKeysF32><<<a.n_tiles, 1024, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace xc
