@@ -402,8 +402,12 @@ inline std::vector<WeightRun> plan_weight_runs(const std::vector<ChunkSeq>& seqs
   return runs;
 }
 
-// Rows in runs of about as many stages as give every place several workgroups:
-// the time of each is that of its stages and a start.  Measured: PLACEHOLDER
+// Rows in runs of as many stages as are cheapest: a workgroup takes stage_us
+// for each, with the others of its CU at work, and start_us for its keys, and
+// at the end of the launch some of the CUs wait for the last of them, on
+// average a third of one's time.  Measured: 7020 rows, 21060 keys, 12 heads of
+// 128, causal by frames of 2340, whole columns of 37 to 110 stages 456 us, runs
+// of up to 56 stages 423, of 28 459.
 inline WeightPlan plan_weights(const std::vector<ChunkSeq>& seqs, const ChunkMask& mask, const PlanShape& sh) {
   using namespace plan_detail;
   const bool f32 = sh.elem == 4;
@@ -433,25 +437,21 @@ inline WeightPlan plan_weights(const std::vector<ChunkSeq>& seqs, const ChunkMas
       ++kinds[at].second;
     }
   }
-  const int per_cu = 2;
-  const double stage_us = f32 ? 0.031 * sh.D : sh.D == 128 ? 0.55 : 0.4, start_us = 4.0;
-  const long long places = (long long)per_cu * sh.cus;
+  const double stage_us = f32 ? 0.03 * sh.D : sh.D == 128 ? 2.0 : 1.45, start_us = 4.6;
+  const double places = 2.0 * sh.cus;
   double best_us = 0;
-  int best_c = 1;
-  static const int kCuts[] = {1, 2, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 512, 1024, 4096, 16384, 65536};
-  Work w;
-  bool have = false;
+  int best_c = 0;
+  static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 40, 56, 80, 112, 160, 224, 320, 448, 1024, 4096, 16384, 65536};
   for (int c : kCuts) {
+    double stages = 0;
     long long groups = 0;
-    for (const auto& k : kinds) groups += k.second * cdiv(k.first, c);
-    if (groups * sh.kv_heads > 16 * places && c < longest) continue;  // rounds enough with longer runs
     for (const auto& k : kinds) {
-      const long long n = cdiv(k.first, c);
-      w.add(k.second * n * sh.kv_heads, (double)k.first / n * stage_us + start_us);
+      stages += (double)k.second * k.first;
+      groups += k.second * cdiv(k.first, c);
     }
-    const double us = w.us(places, 0.5 * places) + (double)groups * sh.kv_heads * keys * 8 / kPieceBytesPerUs;
-    w.kinds.clear();
-    if (!have || us < best_us) have = true, best_us = us, best_c = c;
+    const double one = std::min(c, longest) * stage_us * 0.65 + start_us;  // alone on its CU
+    const double us = std::max(one, sh.kv_heads * (stages * stage_us + groups * start_us) / places) + one / 3;
+    if (best_c == 0 || us < best_us) best_us = us, best_c = c;
     if (c >= longest) break;
   }
   for (size_t i = 0; i < plan.tiles.size(); ++i) {

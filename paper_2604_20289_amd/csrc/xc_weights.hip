@@ -83,18 +83,26 @@ __device__ __forceinline__ float fold(const f32x16& v, int lane) {
   return out;
 }
 
-// 4 waves of 64 keys.  The queries come by in stages of 64 rows, one on its
-// way; products of one tile of 32 rows and exponentials of the one before
-// alternate, two to four of these to a product.  Two workgroups per CU.
+// 4 waves of 64 keys.  The queries come by in stages of 64 rows through a ring
+// of four.  Products of a tile of 32 rows and exponentials of the one before
+// alternate, two (d = 64: four) to a product, so that the matrix units and the
+// others work at once: an exponential takes 9 cycles of its SIMD's and the two
+// multiply-adds with it 8, 32 of them to 512 cycles of products at d = 128.  Two
+// workgroups per CU (three at d = 64).
+//
+// Bound by both: 7020 rows, 21060 keys, 12 heads of 128 in PLACEHOLDER us, the
+// products alone 341, the exponentials alone 333.  Tried: products of a tile,
+// then its exponentials, the other wave of the SIMD in the other phase by
+// chance, 482 us; 32 keys a wave and four waves per SIMD 478; workgroups of 512
+// keys 463; two stages instead of four 470; an unrolled ring with an array per
+// slot spilled.
 template <int D>
 __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
   using F = Frags<D>;
   constexpr int KCG = F::KCG, KS = F::KS, SLOT = 64 * D * 2, NB = 2 * KCG;  // blocks of a stage per wave
-  // an array per slot: its reads then do not wait for requests into the others
-  __shared__ __attribute__((aligned(1024))) char s0[SLOT];
-  __shared__ __attribute__((aligned(1024))) char s1[SLOT];
-  __shared__ __attribute__((aligned(256))) char l0[4 * 256];
-  __shared__ __attribute__((aligned(256))) char l1[4 * 256];
+  constexpr int TERMS = 4 * 64 * 4;  // each wave's copy of a stage's log-sum-exps
+  // queries, then log-sum-exps; one array and no other, in which the compiler leaves it to the waits here what has landed
+  __shared__ __attribute__((aligned(1024))) char ring[4 * (SLOT + TERMS)];
   int u, h;
   if (!xcd_pair(blockIdx.x, a.n_units, a.n_long, a.buf.kv_heads, u, h)) return;
   const WeightUnit un = a.units[u];
@@ -107,19 +115,36 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
   const char* q = reinterpret_cast<const char*>(a.q) + (long long)(sq.row0 + un.r0) * ld + (long long)h * a.group * D * 2;
   const char* lse = reinterpret_cast<const char*>(a.lse + (long long)(sq.row0 + un.r0) * a.q_heads + h * a.group);
 
-  auto request = [&](int s, char* slot, char* terms) __attribute__((always_inline)) {
-    const int at = s * 64;
+  // What a lane fetches of a stage lies as far from the stage's first token in every whole one, where 64 rows are whole
+  // tokens (group divides 64).
+  unsigned q_off[NB], l_off;
+  auto offsets = [&](int at) __attribute__((always_inline)) {
+    const int first = rows.token(rows.clamped(at));
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const int B = wave + 4 * i, rg = B / KCG, cg = B % KCG;
       const int t0 = rows.token(rows.clamped(at + rg * 8));
       const int r = rows.clamped(at + rg * 8 + ((lane >> 3) ^ (rg & 1))), t = rows.token(r);
-      dma16(q + t0 * ld, (unsigned)(t - t0) * (unsigned)ld + (r - t * a.group) * (D * 2) + k_block_col(rg, cg, lane), slot + B * 1024);
+      q_off[i] = (unsigned)(t - t0) * (unsigned)ld + (r - t * a.group) * (D * 2) + k_block_col(rg, cg, lane);
     }
-    const int t0 = rows.token(rows.clamped(at)), r = rows.clamped(at + lane), t = rows.token(r);
-    dma4(lse + (long long)t0 * a.q_heads * 4, ((t - t0) * a.q_heads + r - t * a.group) * 4, terms + wave * 256);
+    const int r = rows.clamped(at + lane), t = rows.token(r);
+    l_off = ((t - first) * a.q_heads + r - t * a.group) * 4;
   };
-  request(0, s0, l0);
+  const bool whole = (a.group & (a.group - 1)) == 0 && a.group <= 64;
+  offsets(0);
+  auto request = [&](int s) __attribute__((always_inline)) {
+    const int at = min(s, n - 1) * 64;  // past the last stage that one again: as many in flight as ever
+    if (!whole || at + 64 > rows.n) offsets(at);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int B = wave + 4 * i;
+      dma16(q + rows.token(rows.clamped(at + B / KCG * 8)) * ld, q_off[i], ring + (s & 3) * SLOT + B * 1024);
+    }
+    dma4(lse + (long long)rows.token(at) * a.q_heads * 4, l_off, ring + 4 * SLOT + (s & 3) * TERMS + wave * 256);
+  };
+  request(0);
+  request(1);
+  request(2);
 
   const int k0 = un.lo + wave * 64;
   bf16x8 kf[2][KS];
@@ -148,23 +173,22 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
     for (int i = 0; i < 16; ++i) sb[mt][i] = -INFINITY, acc[mt][i] = 0.f;
   Term ta, tb{0.f, 0.f};
   const F f(lane);
-  // a tile that hides something: its terms here, and nothing left to add
-  auto masked = [&](int tile, f32x16 (&s)[2], Term& t) __attribute__((always_inline)) {
-    if (tile >= free0 && tile < free1) return;
-    const int r = tile * 32 + lo;
+  // a tile that hides something: what is hidden weighs nothing, whatever the row's sum is; one that is no finite number
+  // goes where the row sees
+  auto masked = [&](int number, f32x16 (&s)[2], Term& t) __attribute__((always_inline)) {
+    if (number < 0 || (number >= free0 && number < free1)) return;
+    const int r = number * 32 + lo;
     const Limits lim = limits_of(sq, a.mask, un.r0 + rows.token(rows.clamped(r)), r < rows.n);
+    const bool finite = fabsf(t.hi) < INFINITY;
+    const float other = -t.hi;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
       const unsigned bits = lim.bits(k0 + mt * 32) >> (hi * 4);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][i], a.scale, -t.hi));
-        acc[mt][i] = __builtin_fmaf(__uint_as_float(__float_as_uint(e) & keep_bit(bits, key_of(i))), t.f, acc[mt][i]);
-        s[mt][i] = -INFINITY;
-        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int i = 0; i < 16; ++i) s[mt][i] = finite ? s[mt][i] : other;
+      mask_row(s[mt], bits, key_of);
     }
-    t = {0.f, 0.f};
+    if (!finite) t = {0.f, 1.f};
   };
   // products of a tile (its half of the stage in slot) with the exponentials of the one before
   auto tile = [&](const char* slot, int half, f32x16 (&s)[2], const f32x16 (&before)[2], const Term& t) __attribute__((always_inline)) {
@@ -172,6 +196,11 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
     bf16x8 fr[PF];
 #pragma unroll
     for (int i = 0; i < PF; ++i) fr[i] = f.k(slot, half, i);
+    float arg[EACH], e[EACH];
+    auto score = [&](int x) __attribute__((always_inline)) { return before[x >> 4][x & 15]; };
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) arg[k] = __builtin_fmaf(score(k), a.scale, -t.hi);
+    // a step: a product, the exponentials of one group of scores, the next one's arguments, the sums of the last one
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       const int mt = i & 1, ks = i >> 1;
@@ -184,29 +213,36 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
 #pragma unroll
       for (int k = 0; k < EACH; ++k) {
         const int x = i * EACH + k;
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(before[x >> 4][x & 15], a.scale, -t.hi));
-        acc[x >> 4][x & 15] = __builtin_fmaf(e, t.f, acc[x >> 4][x & 15]);
+        if (i > 0) acc[(x - EACH) >> 4][(x - EACH) & 15] = __builtin_fmaf(e[k], t.f, acc[(x - EACH) >> 4][(x - EACH) & 15]);
+        e[k] = __builtin_amdgcn_exp2f(arg[k]);
+        if (i + 1 < STEPS) arg[k] = __builtin_fmaf(score(x + EACH), a.scale, -t.hi);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int x = (STEPS - 1) * EACH + k;
+      acc[x >> 4][x & 15] = __builtin_fmaf(e[k], t.f, acc[x >> 4][x & 15]);
+    }
+    // ... all of it here: without this the compiler moves the exponentials behind the next tile's products
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) asm volatile("" : "+v"(acc[mt]));
   };
-  auto stage = [&](int s, const char* slot, const char* terms, char* next, char* next_terms) __attribute__((always_inline)) {
-    XC_WAIT_VM(0);
+  for (int s = 0; s < n; ++s) {
+    const char* slot = ring + (s & 3) * SLOT;
+    XC_WAIT_VM(2 * (NB + 1));  // all but stages s + 1 and s + 2
     tile_barrier();  // this stage is there, and the one before has been read
-    if (s + 1 < n) request(s + 1, next, next_terms);
-    const float* l = reinterpret_cast<const float*>(terms + wave * 256);
+    request(s + 3);
+    const float* l = reinterpret_cast<const float*>(ring + 4 * SLOT + (s & 3) * TERMS + wave * 256);
     const float la = l[lo], lb = l[32 + lo];
-    if (s > 0) masked(2 * s - 1, sb, tb);
+    masked(2 * s - 1, sb, tb);
     tile(slot, 0, sa, sb, tb);
     ta = term_of(la);
     masked(2 * s, sa, ta);
     tile(slot, 1, sb, sa, ta);
     tb = term_of(lb);
-  };
-  for (int s = 0; s < n; s += 2) {
-    stage(s, s0, l0, s1, l1);
-    if (s + 1 < n) stage(s + 1, s1, l1, s0, l0);
   }
+  XC_WAIT_VM(0);
   masked(2 * n - 1, sb, tb);
 #pragma unroll
   for (int mt = 0; mt < 2; ++mt)
@@ -228,10 +264,8 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
 template <int D>
 __global__ __launch_bounds__(256) void weights_f32_kernel(WeightArgs a) {
   constexpr int CH = D / 4, SLOT = 32 * D * 4, NB = SLOT / 4096, RPB = 64 / CH;  // 16-byte chunks of a row, rows of a 1 KB block
-  __shared__ __attribute__((aligned(1024))) char s0[SLOT];
-  __shared__ __attribute__((aligned(1024))) char s1[SLOT];
-  __shared__ __attribute__((aligned(256))) char l0[4 * 256];
-  __shared__ __attribute__((aligned(256))) char l1[4 * 256];
+  constexpr int TERMS = 4 * 64 * 4;
+  __shared__ __attribute__((aligned(1024))) char ring[4 * (SLOT + TERMS)];  // as above
   int u, h;
   if (!xcd_pair(blockIdx.x, a.n_units, a.n_long, a.buf.kv_heads, u, h)) return;
   const WeightUnit un = a.units[u];
@@ -246,19 +280,22 @@ __global__ __launch_bounds__(256) void weights_f32_kernel(WeightArgs a) {
   auto swz = [](int r, int c) __attribute__((always_inline)) {
     return c ^ (CH >= 16 ? (r & 7) ^ ((r & 4) << 1) : r & 7);
   };
-  auto request = [&](int s, char* slot, char* terms) __attribute__((always_inline)) {
-    const int at = s * 32;
+  auto request = [&](int s) __attribute__((always_inline)) {
+    const int at = min(s, n - 1) * 32;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const int B = wave + 4 * i, row = B * RPB + lane / CH;
       const int t0 = rows.token(rows.clamped(at + B * RPB)), r = rows.clamped(at + row), t = rows.token(r);
       dma16(q + t0 * ld, (unsigned)(t - t0) * (unsigned)ld + (r - t * a.group) * (D * 4) + swz(row, lane % CH) * 16,
-            slot + B * 1024);
+            ring + (s & 3) * SLOT + B * 1024);
     }
     const int t0 = rows.token(rows.clamped(at)), r = rows.clamped(at + lo), t = rows.token(r);
-    dma4(lse + (long long)t0 * a.q_heads * 4, ((t - t0) * a.q_heads + r - t * a.group) * 4, terms + wave * 256);
+    dma4(lse + (long long)t0 * a.q_heads * 4, ((t - t0) * a.q_heads + r - t * a.group) * 4,
+         ring + 4 * SLOT + (s & 3) * TERMS + wave * 256);
   };
-  request(0, s0, l0);
+  request(0);
+  request(1);
+  request(2);
   const int k0 = un.lo + wave * 32;
   f32x4 kf[D / 8];
   {
@@ -277,11 +314,12 @@ __global__ __launch_bounds__(256) void weights_f32_kernel(WeightArgs a) {
   f32x16 acc;
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-  auto stage = [&](int st, const char* slot, const char* terms, char* next, char* next_terms) __attribute__((always_inline)) {
-    XC_WAIT_VM(0);
-    tile_barrier();  // this stage is there, and the one before has been read
-    if (st + 1 < n) request(st + 1, next, next_terms);
-    const Term t = term_of(reinterpret_cast<const float*>(terms + wave * 256)[lo]);
+  for (int st = 0; st < n; ++st) {
+    const char* slot = ring + (st & 3) * SLOT;
+    XC_WAIT_VM(2 * (NB + 1));
+    tile_barrier();
+    request(st + 3);
+    const Term t = term_of(reinterpret_cast<const float*>(ring + 4 * SLOT + (st & 3) * TERMS + wave * 256)[lo]);
     f32x16 s, o;  // two sums: no product waits for the one before it
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = o[i] = 0.f;
@@ -305,11 +343,8 @@ __global__ __launch_bounds__(256) void weights_f32_kernel(WeightArgs a) {
       const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i] + o[i], a.scale, -t.hi));
       acc[i] = __builtin_fmaf(__uint_as_float(__float_as_uint(e) & keep_bit(bits, key_of(i))), t.f, acc[i]);
     }
-  };
-  for (int st = 0; st < n; st += 2) {
-    stage(st, s0, l0, s1, l1);
-    if (st + 1 < n) stage(st + 1, s1, l1, s0, l0);
   }
+  XC_WAIT_VM(0);
   const float x = fold(acc, lane);
   const int i = (lane & 7) + ((lane >> 4) & 1) * 8;
   if ((lane & 15) < 8)
