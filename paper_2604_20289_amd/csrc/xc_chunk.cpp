@@ -287,7 +287,8 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
       a.ld = ld;
       a.kept = kept;
       a.kept_ld = kept_ld;
-      XC_HIP(launch_evict(a, p.block(0), p.esz, p.cfg.n_blocks, p.block_elems() * p.esz, most_kept, p.st));
+      XC_HIP(launch_evict(a, p.block(0), p.esz, p.cfg.n_blocks, p.block_elems() * p.esz, most_tokens, most_kept,
+                          p.st));
     });
     return XC_OK;
   });

@@ -51,8 +51,9 @@ struct EvictArgs {
 };
 
 hipError_t launch_weights(int dtype, const WeightArgs& a, hipStream_t st);
-// whole: the first block; most: of the keeps
-hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes, int most,
-                        hipStream_t st);
+// whole: the first block; of the sequences that shrink, most_tokens before and
+// `most` kept
+hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes, int most_tokens,
+                        int most, hipStream_t st);
 
 }  // namespace xc
