@@ -86,16 +86,17 @@ __device__ __forceinline__ float fold(const f32x16& v, int lane) {
 // 4 waves of 64 keys.  The queries come by in stages of 64 rows through a ring
 // of four.  Products of a tile of 32 rows and exponentials of the one before
 // alternate, two (d = 64: four) to a product, so that the matrix units and the
-// others work at once: an exponential takes 9 cycles of its SIMD's and the two
-// multiply-adds with it 8, 32 of them to 512 cycles of products at d = 128.  Two
-// workgroups per CU (three at d = 64).
+// others work at once (a step of one product, two exponentials and four
+// multiply-adds takes 41 cycles of a SIMD with two such waves, where the product
+// alone takes 32 and the others 30).  Two workgroups per CU, three at d = 64.
 //
-// Bound by both: 7020 rows, 21060 keys, 12 heads of 128 in PLACEHOLDER us, the
-// products alone 341, the exponentials alone 333.  Tried: products of a tile,
-// then its exponentials, the other wave of the SIMD in the other phase by
-// chance, 482 us; 32 keys a wave and four waves per SIMD 478; workgroups of 512
-// keys 463; two stages instead of four 470; an unrolled ring with an array per
-// slot spilled.
+// Bound by both: 7020 rows, 21060 keys, 12 heads of 128 take 450 us, 1010
+// TFLOP/s, with the products alone 341 and without them 333, at 2.0 GHz and
+// 87% of the wave slots; at d = 64 the exponentials: 16384 rows of 8
+// sequences, 6144 keys, 8 heads 140 us.  Tried: a tile's products, then its
+// exponentials, with the other wave of the SIMD in the other phase by chance,
+// 482 us; 32 keys a wave and four waves per SIMD 478; workgroups of 512 keys 463;
+// two stages instead of four 470.  An unrolled ring with an array per slot spills.
 template <int D>
 __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
   using F = Frags<D>;
@@ -388,8 +389,14 @@ __global__ __launch_bounds__(1024) void weights_join_kernel(WeightArgs a) {
 // on its way.  A lane has a query row of every head, so its sums of 16 keys go on
 // over all heads; then they meet in LDS, the rows of each sequence and the
 // waves' shares.  What a row does not see is left out there, once for all heads.
+//
+// Bound by latency and by reading keys: one row over 48448 keys, 16 heads of 128
+// (198 MB) 34 us, 16 rows over 14040 shared keys and 100 of their own, 12 heads
+// (48 MB) 15; 64 rows over 36288 and 100, 16 heads, 84, of which the queries are
+// much: a row per lane, 64 lines a load.  (By DMA into LDS, as the keys: 15 for
+// 16 rows, but 116 for 64, whose LDS then leaves room for one workgroup.)
 template <int D, int G>
-__device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun& run, char* ring) {
+__device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun& run, const ChunkSeq& first, int n_rows, char* ring) {
   using F = Frags<D>;
   constexpr int KCG = F::KCG, KS = F::KS, KEYS = few_keys(D), HT = KEYS / 32, TILE = KEYS * D * 2, LOADS = TILE / 1024, R = 32 * G;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -397,24 +404,7 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
   const int kv = a.buf.kv_heads, hw = few_head_waves(kv), h0 = wave % hw;
   const int in_page = (1 << a.buf.shift) - 1, last = run.hi - 1;
   const int group0 = (run.lo & ~15) + (blockIdx.x - run.group0) * (KEYS * 4 / hw), at0 = group0 + wave / hw * KEYS;
-  const ChunkSeq first = a.seqs[run.seq0], end = a.seqs[run.seq0 + run.n_seqs - 1];
-  const QueryRows rows{(end.row0 + end.rows - first.row0) * a.group, a.group, a.by_group};
-
-  // this lane's rows and what they see
-  int token[G];
-  Limits lim[G];
-  bool any = false;
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const int r = rows.clamped(g * 32 + lo);
-    token[g] = first.row0 + rows.token(r);
-    int s = run.seq0;
-    while (s + 1 < run.seq0 + run.n_seqs && a.seqs[s + 1].row0 <= token[g]) ++s;
-    lim[g] = limits_of(a.seqs[s], a.mask, token[g] - a.seqs[s].row0, g * 32 + lo < rows.n);
-#pragma unroll
-    for (int mt = 0; mt < HT; ++mt) any |= lim[g].bits(at0 + mt * 32) != 0;
-  }
-  const int n = at0 <= last && __builtin_amdgcn_ballot_w64(any) != 0 ? (kv - h0 + hw - 1) / hw : 0;  // heads h0, h0 + hw, ..
+  const QueryRows rows{n_rows * a.group, a.group, a.by_group};
 
   // the groups of 16 places, each in one page; places outside the run read the nearest of it
   long long page_at[KEYS / 16];
@@ -440,6 +430,27 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
       for (int cg = 0; cg < KCG; ++cg)
         dma16(keys + page_at[rg >> 1], row_at[rg] + cg * 128, kt + (i & 1) * TILE + (rg * KCG + cg) * 1024);
   };
+  // without a window every tile is seen, and its keys are asked for before anything else
+  const bool early = a.mask.window == ChunkMask::kNone && at0 <= last && h0 < kv;
+  if (early) request(0);
+
+  // this lane's rows and what they see
+  int token[G];
+  Limits lim[G];
+  bool any = false;
+  const int begins = a.seqs[run.seq0 + min(lane, run.n_seqs - 1)].row0;  // at most 64 sequences
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    token[g] = first.row0 + rows.token(rows.clamped(g * 32 + lo));
+    int s = run.seq0 - 1;
+    for (int i = 0; i < run.n_seqs; ++i) s += __builtin_amdgcn_readlane(begins, i) <= token[g];
+    const ChunkSeq sq = a.seqs[s];
+    lim[g] = limits_of(sq, a.mask, token[g] - sq.row0, g * 32 + lo < rows.n);
+#pragma unroll
+    for (int mt = 0; mt < HT; ++mt) any |= lim[g].bits(at0 + mt * 32) != 0;
+  }
+  const int n = early || (at0 <= last && __builtin_amdgcn_ballot_w64(any) != 0) ? (kv - h0 + hw - 1) / hw : 0;  // heads h0, h0 + hw, ..
+
   bf16x8 q[2][G][KS];
   float l[2][G];
   auto queries = [&](int i, bf16x8 (&x)[G][KS], float (&y)[G]) __attribute__((always_inline)) {
@@ -465,6 +476,7 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
     if constexpr (!last) {
       request(i + 1);
       queries(i + 1, nx, ny);
+      asm volatile("" ::: "memory");  // (all of them before the wait that counts them)
       XC_WAIT_VM(LOADS + G * (KS + 1));
     } else {
       XC_WAIT_VM(0);
@@ -498,7 +510,7 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this tile has been read
   };
   if (n > 0) {
-    request(0);
+    if (!early) request(0);
     queries(0, q[0], l[0]);
   }
   constexpr std::false_type more{};
@@ -515,6 +527,7 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
     head(i, last_one, q[0], l[0], q[1], l[1]);
   }
   // key k, row r at k * R + (r + k) % R: lanes of different rows (written) or keys (read) meet different banks
+  XC_WAIT_VM(0);
   float* mine = reinterpret_cast<float*>(kt);
 #pragma unroll
   for (int g = 0; g < G; ++g)
@@ -545,17 +558,20 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
 }
 template <int D>
 __global__ __launch_bounds__(256, 2) void weights_few_kernel(WeightArgs a) {
-  __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * few_keys(D) * D * 2];
-  int lo = 0, hi = a.n_runs;  // the last run with group0 <= this workgroup
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.runs[mid].group0 <= (int)blockIdx.x) lo = mid;
-    else hi = mid;
+  __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * few_keys(D) * D * 2];  // (one array and no other, as above)
+  const int lane = threadIdx.x & 63;
+  int r = -1;  // the last run with group0 <= this workgroup
+  for (int i = 0; i < a.n_runs; i += 64) {
+    const bool before = i + lane < a.n_runs && a.runs[i + lane].group0 <= (int)blockIdx.x;
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(before));
+    r += n;
+    if (n < 64) break;
   }
-  const WeightRun run = a.runs[lo];
+  const WeightRun run = a.runs[r];
   const ChunkSeq first = a.seqs[run.seq0], end = a.seqs[run.seq0 + run.n_seqs - 1];
-  if ((end.row0 + end.rows - first.row0) * a.group > 32) few_weights<D, 2>(a, run, ring);
-  else few_weights<D, 1>(a, run, ring);
+  const int n_rows = end.row0 + end.rows - first.row0;
+  if (n_rows * a.group > 32) few_weights<D, 2>(a, run, first, n_rows, ring);
+  else few_weights<D, 1>(a, run, first, n_rows, ring);
 }
 
 }  // namespace
