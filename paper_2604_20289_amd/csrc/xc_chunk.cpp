@@ -45,9 +45,11 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   // the sums of weights: where all sequences have few rows, or with partial sums
   int groups = 0;
   const std::vector<WeightRun> runs = plan_weight_runs(chunk_seqs, r.shared_end, shape, &groups);
-  const bool few = p.esz == 2 && !runs.empty();
+  std::vector<WeightFew> few;
+  std::vector<WeightInfo> infos;
   WeightPlan sums;
-  if (!few) sums = plan_weights(chunk_seqs, mask, shape);
+  if (p.esz == 2 && !runs.empty()) few = few_runs(runs, chunk_seqs, mask, group, &infos);
+  else sums = plan_weights(chunk_seqs, mask, shape);
   const size_t part_need =
       (size_t)sums.parts * p.cfg.kv_heads * (p.esz == 2 ? kWeightKeys : kWeightKeysF32) * sizeof(float);
   if ((((long long)sums.units.size() + kXcds) * p.cfg.kv_heads + kXcds * kXcds) * 256 >> 32 || (long long)groups * 256 >> 32 ||
@@ -59,7 +61,8 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const size_t o_chunks = o_seqs + align256(batch_seqs.size() * sizeof(BatchSeq));
   const size_t o_units = o_chunks + align256(chunk_seqs.size() * sizeof(ChunkSeq));
   const size_t o_runs = o_units + align256(plan.units.size() * sizeof(ChunkUnit));
-  const size_t o_sums = o_runs + align256((few ? runs.size() : 0) * sizeof(WeightRun));
+  const size_t o_infos = o_runs + align256(few.size() * sizeof(WeightFew));
+  const size_t o_sums = o_infos + align256(infos.size() * sizeof(WeightInfo));
   const size_t o_tiles = o_sums + align256(sums.units.size() * sizeof(WeightUnit));
   const size_t up = o_tiles + align256(sums.tiles.size() * sizeof(WeightTile));
   const size_t o_own = up + align256(rows * sizeof(int));
@@ -71,7 +74,8 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     put(b, o_seqs, batch_seqs);
     put(b, o_chunks, chunk_seqs);
     put(b, o_units, plan.units);
-    if (few) put(b, o_runs, runs);
+    put(b, o_runs, few);
+    put(b, o_infos, infos);
     put(b, o_sums, sums.units);
     put(b, o_tiles, sums.tiles);
     upload(b, b->dev, up);
@@ -111,9 +115,10 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   w.n_long = long_units(sums.units);
   w.n_tiles = (int)sums.tiles.size();
   w.parts = (float*)b->parts;
-  w.runs = (const WeightRun*)(b->dev + o_runs);
-  w.n_runs = few ? (int)runs.size() : 0;
-  w.n_groups = few ? groups : 0;
+  w.runs = (const WeightFew*)(b->dev + o_runs);
+  w.infos = (const WeightInfo*)(b->dev + o_infos);
+  w.n_runs = (int)few.size();
+  w.n_groups = few.empty() ? 0 : groups;
   b->place = (const int*)(b->dev + up);
   b->rows = r.rows;
   b->seqs.swap(seq_copy);

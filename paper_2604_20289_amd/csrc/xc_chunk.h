@@ -20,7 +20,8 @@ struct WeightArgs {
   const WeightTile* tiles;
   int n_units, n_long, n_tiles;
   float* parts;        // [part][key head][kWeightKeys] (float32 pools: kWeightKeysF32)
-  const WeightRun* runs;
+  const WeightFew* runs;
+  const WeightInfo* infos;
   int n_runs, n_groups;
   const void* q;       // [rows][q_ld]
   long long q_ld;

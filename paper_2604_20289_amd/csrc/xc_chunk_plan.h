@@ -402,6 +402,39 @@ inline std::vector<WeightRun> plan_weight_runs(const std::vector<ChunkSeq>& seqs
   return runs;
 }
 
+// A run as its workgroups read it: with the places of its page table, the batch
+// rows, and at infos[info] what they need of each row, then of each sequence.
+struct alignas(16) WeightFew {
+  int group0, lo, hi, table, first;
+  int row0, rows, seqs, info;
+};
+struct alignas(16) WeightInfo {
+  int a, b, c;  // a row: places [first, c) and [a, b) that it sees; a sequence: its number, its query rows [b, c) of the run
+};
+inline std::vector<WeightFew> few_runs(const std::vector<WeightRun>& runs, const std::vector<ChunkSeq>& seqs, const ChunkMask& mask,
+                                       int group, std::vector<WeightInfo>* infos) {
+  std::vector<WeightFew> out;
+  infos->clear();
+  for (const WeightRun& r : runs) {
+    const ChunkSeq& head = seqs[r.seq0];
+    WeightFew f{r.group0, r.lo, r.hi, head.table, head.first, head.row0, 0, r.n_seqs, (int)infos->size()};
+    for (int i = 0; i < r.n_seqs; ++i) {
+      const ChunkSeq& q = seqs[r.seq0 + i];
+      f.rows += q.rows;
+      for (int row = 0; row < q.rows; ++row) {
+        const Seen s = seen(q, mask, row);
+        infos->push_back({s.begin, s.end, s.sink_end});
+      }
+    }
+    for (int i = 0; i < r.n_seqs; ++i) {
+      const ChunkSeq& q = seqs[r.seq0 + i];
+      infos->push_back({q.number, (q.row0 - head.row0) * group, (q.row0 + q.rows - head.row0) * group});
+    }
+    out.push_back(f);
+  }
+  return out;
+}
+
 // Rows in runs of as many stages as are cheapest: a workgroup takes stage_us
 // for each, with the others of its CU at work, and start_us for its keys, and
 // at the end of the launch some of the CUs wait for the last of them, on

@@ -390,21 +390,55 @@ __global__ __launch_bounds__(1024) void weights_join_kernel(WeightArgs a) {
 // over all heads; then they meet in LDS, the rows of each sequence and the
 // waves' shares.  What a row does not see is left out there, once for all heads.
 //
+// All that a workgroup has to know comes in two steps (its run, then rows,
+// pages and where its sums go), so that keys, queries and the old sums are asked
+// for together: 12.5 us for 16 rows over 14040 shared keys and 100 of their own,
+// 12 heads of 128 (48 MB), where a search for the run and each row's sequence one
+// after the other take 14.4; 6.8 instead of 7.9 over 200 keys.
 // Bound by latency and by reading keys: one row over 48448 keys, 16 heads of 128
-// (198 MB) 34 us, 16 rows over 14040 shared keys and 100 of their own, 12 heads
-// (48 MB) 15; 64 rows over 36288 and 100, 16 heads, 84, of which the queries are
-// much: a row per lane, 64 lines a load.  (By DMA into LDS, as the keys: 15 for
-// 16 rows, but 116 for 64, whose LDS then leaves room for one workgroup.)
+// (198 MB) 31 us; 64 rows over 36288 and 100, 16 heads, 72, of which the queries
+// are much: a row per lane, 64 lines a load.  (By DMA into LDS, as the keys, they
+// gain nothing for 16 rows and lose a third for 64, whose LDS then leaves room for
+// one workgroup.)
 template <int D, int G>
-__device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun& run, const ChunkSeq& first, int n_rows, char* ring) {
+__device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightFew& run, char* ring) {
   using F = Frags<D>;
   constexpr int KCG = F::KCG, KS = F::KS, KEYS = few_keys(D), HT = KEYS / 32, TILE = KEYS * D * 2, LOADS = TILE / 1024, R = 32 * G;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hi = lane >> 5, lo = lane & 31;
   const int kv = a.buf.kv_heads, hw = few_head_waves(kv), h0 = wave % hw;
-  const int in_page = (1 << a.buf.shift) - 1, last = run.hi - 1;
-  const int group0 = (run.lo & ~15) + (blockIdx.x - run.group0) * (KEYS * 4 / hw), at0 = group0 + wave / hw * KEYS;
-  const QueryRows rows{n_rows * a.group, a.group, a.by_group};
+  const int in_page = (1 << a.buf.shift) - 1, last = run.hi - 1, group_keys = KEYS * 4 / hw;
+  const int group0 = (run.lo & ~15) + (blockIdx.x - run.group0) * group_keys, at0 = group0 + wave / hw * KEYS;
+  const QueryRows rows{run.rows * a.group, a.group, a.by_group};
+
+  // what this lane's rows see
+  int token[G];
+  WeightInfo row[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    token[g] = rows.token(rows.clamped(g * 32 + lo));
+    row[g] = a.infos[run.info + token[g]];
+  }
+  // The first sums that this thread is to write: where, and what is there (asked for with the first keys).
+  struct Out {
+    float* to;
+    float old;
+    int r0, r1;
+  };
+  const int n_out = run.seqs * group_keys;
+  auto out_of = [&](int x) __attribute__((always_inline)) {
+    const int si = min(x, n_out - 1) >> __builtin_ctz(group_keys), at = group0 + x - si * group_keys;
+    const WeightInfo s = a.infos[run.info + run.rows + si];
+    const bool is = x < n_out && at >= run.lo && at <= last;
+    return Out{is ? a.weights + s.a * a.ld + (at - run.first) : nullptr, 0.f, s.b, s.c};
+  };
+  auto old_of = [&](Out& o) __attribute__((always_inline)) {
+    if (a.decay != 0.f && o.to) o.old = *o.to * a.decay;
+  };
+  constexpr int AHEAD = 3 - G;
+  Out out[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) out[i] = out_of(threadIdx.x + i * 256);
 
   // the groups of 16 places, each in one page; places outside the run read the nearest of it
   long long page_at[KEYS / 16];
@@ -413,7 +447,7 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
 #pragma unroll
   for (int j = 0; j < KEYS / 16; ++j) {
     const int g0 = min(max(at0 + j * 16, run.lo), last);
-    const long long page = a.tables[first.table + (g0 >> a.buf.shift)];
+    const long long page = a.tables[run.table + (g0 >> a.buf.shift)];
     page_at[j] = page * kv * head_bytes;
   }
 #pragma unroll
@@ -430,26 +464,21 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
       for (int cg = 0; cg < KCG; ++cg)
         dma16(keys + page_at[rg >> 1], row_at[rg] + cg * 128, kt + (i & 1) * TILE + (rg * KCG + cg) * 1024);
   };
-  // without a window every tile is seen, and its keys are asked for before anything else
-  const bool early = a.mask.window == ChunkMask::kNone && at0 <= last && h0 < kv;
-  if (early) request(0);
-
-  // this lane's rows and what they see
-  int token[G];
-  Limits lim[G];
+  auto bits_of = [&](int g, int at) __attribute__((always_inline)) {
+    const unsigned b = Limits{row[g].a, row[g].b, run.first, row[g].c}.bits(at);
+    return g * 32 + lo < rows.n ? b : 0u;
+  };
+  // without a window every tile is seen
   bool any = false;
-  const int begins = a.seqs[run.seq0 + min(lane, run.n_seqs - 1)].row0;  // at most 64 sequences
+  if (a.mask.window != ChunkMask::kNone) {
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    token[g] = first.row0 + rows.token(rows.clamped(g * 32 + lo));
-    int s = run.seq0 - 1;
-    for (int i = 0; i < run.n_seqs; ++i) s += __builtin_amdgcn_readlane(begins, i) <= token[g];
-    const ChunkSeq sq = a.seqs[s];
-    lim[g] = limits_of(sq, a.mask, token[g] - sq.row0, g * 32 + lo < rows.n);
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int mt = 0; mt < HT; ++mt) any |= lim[g].bits(at0 + mt * 32) != 0;
+      for (int mt = 0; mt < HT; ++mt) any |= bits_of(g, at0 + mt * 32) != 0;
+  } else {
+    any = true;
   }
-  const int n = early || (at0 <= last && __builtin_amdgcn_ballot_w64(any) != 0) ? (kv - h0 + hw - 1) / hw : 0;  // heads h0, h0 + hw, ..
+  const int n = at0 <= last && __builtin_amdgcn_ballot_w64(any) != 0 ? (kv - h0 + hw - 1) / hw : 0;  // heads h0, h0 + hw, ..
 
   bf16x8 q[2][G][KS];
   float l[2][G];
@@ -457,10 +486,10 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const int r = rows.clamped(g * 32 + lo), head = (h0 + i * hw) * a.group + r - rows.token(r) * a.group;
-      const bf16* p = reinterpret_cast<const bf16*>(a.q) + token[g] * a.q_ld + (long long)head * D + hi * 8;
+      const bf16* p = reinterpret_cast<const bf16*>(a.q) + (run.row0 + token[g]) * a.q_ld + (long long)head * D + hi * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) x[g][ks] = *reinterpret_cast<const bf16x8*>(p + ks * 16);
-      y[g] = a.lse[(long long)token[g] * a.q_heads + head];
+      y[g] = a.lse[(long long)(run.row0 + token[g]) * a.q_heads + head];
     }
   };
   f32x16 acc[G][HT];
@@ -510,9 +539,11 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this tile has been read
   };
   if (n > 0) {
-    if (!early) request(0);
+    request(0);
     queries(0, q[0], l[0]);
   }
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) old_of(out[i]);
   constexpr std::false_type more{};
   constexpr std::true_type last_one{};
   int i = 0;
@@ -533,7 +564,7 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
   for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int mt = 0; mt < HT; ++mt) {
-      const unsigned bits = lim[g].bits(at0 + mt * 32) >> (hi * 4);
+      const unsigned bits = bits_of(g, at0 + mt * 32) >> (hi * 4);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int k = mt * 32 + key_of(i) + hi * 4;
@@ -541,37 +572,38 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightRun
       }
     }
   __syncthreads();
-  const int group_keys = KEYS * 4 / hw;
-  for (int x = threadIdx.x; x < run.n_seqs * group_keys; x += 256) {
-    const int si = x / group_keys, gk = x - si * group_keys, at = group0 + gk, k = gk % KEYS;
-    if (at < run.lo || at > last) continue;
-    const ChunkSeq sq = a.seqs[run.seq0 + si];
-    float* to = a.weights + sq.number * a.ld + (at - sq.first);
-    const int r0 = (sq.row0 - first.row0) * a.group, r1 = r0 + sq.rows * a.group;
+  auto write = [&](const Out& o, int x) __attribute__((always_inline)) {
+    if (!o.to) return;
+    const int gk = x & (group_keys - 1), k = gk % KEYS;
     float sum = 0.f;
     for (int w = 0; w < hw; ++w) {
       const float* part = reinterpret_cast<const float*>(ring + (gk / KEYS * hw + w) * (2 * TILE)) + k * R;
-      for (int r = r0; r < r1; ++r) sum += part[(r + k) & (R - 1)];
+      for (int r = o.r0; r < o.r1; ++r) sum += part[(r + k) & (R - 1)];
     }
-    *to = a.decay == 0.f ? sum : *to * a.decay + sum;
+    *o.to = o.old + sum;
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) write(out[i], threadIdx.x + i * 256);
+  for (int x = threadIdx.x + AHEAD * 256; x < n_out; x += 256) {
+    Out o = out_of(x);
+    old_of(o);
+    write(o, x);
   }
 }
 template <int D>
 __global__ __launch_bounds__(256, 2) void weights_few_kernel(WeightArgs a) {
   __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * few_keys(D) * D * 2];  // (one array and no other, as above)
-  const int lane = threadIdx.x & 63;
-  int r = -1;  // the last run with group0 <= this workgroup
-  for (int i = 0; i < a.n_runs; i += 64) {
-    const bool before = i + lane < a.n_runs && a.runs[i + lane].group0 <= (int)blockIdx.x;
-    const int n = __popcll(__builtin_amdgcn_ballot_w64(before));
-    r += n;
-    if (n < 64) break;
-  }
-  const WeightRun run = a.runs[r];
-  const ChunkSeq first = a.seqs[run.seq0], end = a.seqs[run.seq0 + run.n_seqs - 1];
-  const int n_rows = end.row0 + end.rows - first.row0;
-  if (n_rows * a.group > 32) few_weights<D, 2>(a, run, first, n_rows, ring);
-  else few_weights<D, 1>(a, run, first, n_rows, ring);
+  // its run is the last that begins at this workgroup or before: a lane each, 64 of them at a time
+  int i = 0;
+  while (i + 64 < a.n_runs && a.runs[i + 64].group0 <= (int)blockIdx.x) i += 64;
+  const WeightFew mine = a.runs[min(i + (int)(threadIdx.x & 63), a.n_runs - 1)];
+  const bool before = i + (int)(threadIdx.x & 63) < a.n_runs && mine.group0 <= (int)blockIdx.x;
+  const int at = __popcll(__builtin_amdgcn_ballot_w64(before)) - 1;
+  auto of = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, at); };
+  const WeightFew run{of(mine.group0), of(mine.lo),   of(mine.hi),   of(mine.table), of(mine.first),
+                      of(mine.row0),   of(mine.rows), of(mine.seqs), of(mine.info)};
+  if (run.rows * a.group > 32) few_weights<D, 2>(a, run, ring);
+  else few_weights<D, 1>(a, run, ring);
 }
 
 }  // namespace
