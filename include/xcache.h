@@ -539,8 +539,8 @@ xc_status xc_qk_norm_rope(xc_batch* batch, int32_t block, const void* qkv, int64
  * and values outside the sequences are not read.  NaN and infinities reach the
  * rows and heads that attend to them alone; an infinite value gives infinity or
  * NaN in its column.
- * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set or out of date),
- * XC_ERR_HIP (sticky). */
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set, set by xc_chunk_set or
+ * out of date), XC_ERR_HIP (sticky). */
 xc_status xc_branch_attention(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, void* out,
                               int64_t out_ld);
 
