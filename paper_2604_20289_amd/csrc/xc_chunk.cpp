@@ -29,6 +29,19 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     return threads >> 32 == 0;
   };
   if (!launches()) return XC_ERR_UNSUPPORTED;
+  // the sums of weights: where all sequences have few rows, or with partial sums
+  int groups = 0;
+  const std::vector<WeightRun> runs = plan_weight_runs(chunk_seqs, r.shared_end, shape, &groups);
+  std::vector<WeightFew> few;
+  std::vector<WeightInfo> infos;
+  WeightPlan sums;
+  if (p.esz == 2 && !runs.empty()) few = few_runs(runs, chunk_seqs, mask, group, &infos);
+  else sums = plan_weights(chunk_seqs, mask, shape);
+  const size_t part_need =
+      (size_t)sums.parts * p.cfg.kv_heads * (p.esz == 2 ? kWeightKeys : kWeightKeysF32) * sizeof(float);
+  if ((((long long)sums.units.size() + kXcds) * p.cfg.kv_heads + kXcds * kXcds) * 256 >> 32 || (long long)groups * 256 >> 32 ||
+      (long long)sums.tiles.size() * 1024 >> 32)
+    return XC_ERR_UNSUPPORTED;
   // pieces [slot][row][head][D], then their statistics
   auto stat_rows = [&] { return (size_t)plan.n_slots * (rows - plan.piece_row0) * p.cfg.q_heads; };
   auto stats_at = [&] { return align256(stat_rows() * p.cfg.head_dim * sizeof(float)); };
@@ -42,19 +55,6 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     const ChunkSeq& q = chunk_seqs[part.seq];
     batch_seqs.push_back({part.tok0, q.first + q.tokens - q.rows + (part.tok0 - q.row0), q.table, part.own});
   }
-  // the sums of weights: where all sequences have few rows, or with partial sums
-  int groups = 0;
-  const std::vector<WeightRun> runs = plan_weight_runs(chunk_seqs, r.shared_end, shape, &groups);
-  std::vector<WeightFew> few;
-  std::vector<WeightInfo> infos;
-  WeightPlan sums;
-  if (p.esz == 2 && !runs.empty()) few = few_runs(runs, chunk_seqs, mask, group, &infos);
-  else sums = plan_weights(chunk_seqs, mask, shape);
-  const size_t part_need =
-      (size_t)sums.parts * p.cfg.kv_heads * (p.esz == 2 ? kWeightKeys : kWeightKeysF32) * sizeof(float);
-  if ((((long long)sums.units.size() + kXcds) * p.cfg.kv_heads + kXcds * kXcds) * 256 >> 32 || (long long)groups * 256 >> 32 ||
-      (long long)sums.tiles.size() * 256 >> 32)
-    return XC_ERR_UNSUPPORTED;
   if (!enlarge(p, b->parts, b->part_bytes, part_need, part_need / 4)) return XC_ERR_OOM;
   // uploaded: tables, sequences, units; written on the device: places, own slots
   const size_t o_seqs = align256(r.tables.size() * sizeof(int));

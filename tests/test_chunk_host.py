@@ -161,6 +161,19 @@ def test_memory_that_ends_in_the_middle_of_a_call(where, dtype):
     assert ahead == 2
 
 
+@pytest.mark.parametrize("shape", [dict(q_heads=4, kv_heads=4, head_dim=128), dict(head_dim=32, dtype=XC_F32)], ids=["few", "f32"])
+def test_refused_sizes_leave_the_rows_and_their_memory(shape):
+    """More workgroups than a launch has: refused before the buffers of the rows set before are given up for larger ones."""
+    pool = Pool(n_pages=1 << 22, page_tokens=256, max_seqs=4, **shape)
+    a, b = pool.new(100), pool.new((1 << 29) + 100000)
+    assert pool.set([a], [1]) == XC_OK and chunk.info()["live_bytes"] > 0
+    before = chunk.info()["live_bytes"]
+    assert pool.set([b], [1]) == XC_ERR_UNSUPPORTED
+    assert chunk.info()["live_bytes"] == before
+    assert pool.attention() == XC_OK and pool.weights() == XC_OK
+    pool.close()
+
+
 def test_pages_that_run_out_and_launches_that_fail():
     pool = Pool(n_pages=20)
     a = pool.new(160)

@@ -11,7 +11,7 @@ import branch_reference as ref  # noqa: E402
 import chunk_reference as chunk  # noqa: E402
 from paper_2604_20289_amd import xcache  # noqa: E402
 from paper_2604_20289_amd.xcache import Batch, Pool, XCacheError  # noqa: E402
-from test_gpu_branches import BF16, F32, grow, make, pages_for, stream  # noqa: E402
+from test_gpu_branches import BF16, F32, grow, make, pages_for, stream, write  # noqa: E402
 from test_gpu_chunks import check, evict_check, p_eps  # noqa: E402
 
 
@@ -58,6 +58,52 @@ def test_many_single_tokens():
     for mask in ((1, 0, 0), (1, 64, 4)):
         batch.set_chunk(seqs, [1] * 70, *mask)
         check(pool, batch, seqs, [1] * 70, mask)
+
+
+@pytest.mark.parametrize("dtype,kv,d,n", [(BF16, 2, 128, 9), (BF16, 1, 64, 40), (F32, 2, 64, 5), (BF16, 2, 64, 300)])
+@pytest.mark.parametrize("what,bad", [("key", math.nan), ("value", math.nan), ("value", math.inf)])
+def test_numbers_that_are_not_finite_in_a_shared_history(what, bad, dtype, kv, d, n):
+    """Single tokens over one history: bad numbers among its first tokens, between them and the windows, where some windows begin
+    and others do not, and where all of them see."""
+    branches = [(i % 30, 1) for i in range(n)]
+    pool = make(dtype, pages=pages_for(2000, branches, 16), kv=kv, page=16, d=d, seqs=n + 1)
+    parent, seqs = grow(pool, 2000, 5, branches)
+    g = torch.Generator().manual_seed(6)
+    q = torch.randn(n, kv, d, generator=g).to(dtype).cuda()
+    batch, tokens, (window, sinks) = Batch(pool), 1995, (700, 40)
+    edge = tokens + 20 - window  # in the windows of branches of fewer than 20 tokens
+    history = torch.randn(2, tokens, kv, d, generator=g)
+    head, dim = kv - 1, d // 3
+    for at in ([10], [200], [edge], [tokens - 100], [39, 40, 800, edge, tokens - 3]):
+        pair = history.clone()
+        pair["kv".index(what[0]), at, head, dim] = bad
+        write(pool, parent, *pair)
+        for i, s in enumerate(seqs):
+            own = torch.randn(2, branches[i][0] + 1, kv, d, generator=g)
+            write(pool, s, *torch.cat((pair, own), 1))
+        batch.set_chunk(seqs, [1] * n, 1, window, sinks)
+        out, lse = torch.empty_like(q), torch.empty(n, kv, device="cuda")
+        w = torch.zeros(n, tokens + 40, device="cuda")
+        batch.chunk_attention(0, q, out, lse=lse)
+        batch.chunk_weights(0, q, lse, w, decay=0.0)
+        for i, s in enumerate(seqs):
+            k, v = (ref.gather(b, 0, pool.pages(s)) for b in (pool.keys, pool.values))
+            see = chunk.sees(len(k), 1, 1, window, sinks)
+            hit = bool(see[0, at].any())
+            k0, v0 = (torch.where(torch.isfinite(x), x, torch.zeros_like(x)) for x in (k, v))
+            args = q[i:i + 1].double().cpu()
+            want, tol, want_lse, lse_tol = chunk.attention(args, k0, v0, d ** -0.5, see, dtype, p_eps(dtype))
+            got, got_lse = out[i:i + 1].double().cpu(), lse[i:i + 1].double().cpu()
+            fine, sums_fine = torch.ones(want.shape, dtype=torch.bool), torch.ones(want_lse.shape, dtype=torch.bool)
+            if hit and what == "key":
+                fine[0, head], sums_fine[0, head] = False, False
+            elif hit:
+                fine[0, head, dim] = False
+                assert not torch.isfinite(got[0, head, dim])
+            assert ((got - want).abs() <= tol)[fine].all() and ((got_lse - want_lse).abs() <= lse_tol)[sums_fine].all()
+            if not hit or what == "value":
+                total, tol = chunk.weights(args, k0, d ** -0.5, see, got_lse)
+                assert ((w[i, :len(k)].double().cpu() - total).abs() <= tol + 1e-30).all()
 
 
 # ---------------------------------------------------------------- memory
