@@ -438,9 +438,12 @@ inline std::vector<WeightFew> few_runs(const std::vector<WeightRun>& runs, const
 // Rows in runs of as many stages as are cheapest: a workgroup takes stage_us
 // for each, with the others of its CU at work, and start_us for its keys, and
 // at the end of the launch some of the CUs wait for the last of them, on
-// average a third of one's time.  Measured: 7020 rows, 21060 keys, 12 heads of
-// 128, causal by frames of 2340, whole columns of 37 to 110 stages 456 us, runs
-// of up to 56 stages 423, of 28 459.
+// average a third of one's time.  So the last tiles may have shorter runs.
+// Measured: 7020 rows, 21060 keys, 12 heads of 128, causal by frames of 2340: whole
+// columns of 37 to 110 stages 456 us, runs of up to 56 stages 423, of 28 459; runs
+// of 37 439, whole columns and runs of 27 for the last third 420 (18 for it 423,
+// 13 430, 36 421).  24192 causal rows, 16 heads of 128: 1182 without and 1168
+// with; 13 causal chunks, 16 heads of 64 on 4: 154 and 151.
 inline WeightPlan plan_weights(const std::vector<ChunkSeq>& seqs, const ChunkMask& mask, const PlanShape& sh) {
   using namespace plan_detail;
   const bool f32 = sh.elem == 4;
@@ -473,23 +476,39 @@ inline WeightPlan plan_weights(const std::vector<ChunkSeq>& seqs, const ChunkMas
   const double stage_us = f32 ? 0.03 * sh.D : sh.D == 128 ? 2.0 : 1.45, start_us = 4.6;
   const double places = 2.0 * sh.cus;
   double best_us = 0;
-  int best_c = 0;
+  int best_c = 0, best_end = 0;
+  size_t best_from = 0;  // from this tile on, runs of best_end stages
   static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 40, 56, 80, 112, 160, 224, 320, 448, 1024, 4096, 16384, 65536};
+  double all = 0;
+  for (const auto& k : kinds) all += (double)k.second * k.first;
   for (int c : kCuts) {
-    double stages = 0;
     long long groups = 0;
-    for (const auto& k : kinds) {
-      stages += (double)k.second * k.first;
-      groups += k.second * cdiv(k.first, c);
+    for (const auto& k : kinds) groups += k.second * cdiv(k.first, c);
+    auto one = [&](int c) { return std::min(c, longest) * stage_us * 0.65 + start_us; };  // alone on its CU
+    auto us = [&](long long groups, int last) {
+      return std::max(one(c), sh.kv_heads * (all * stage_us + groups * start_us) / places) + one(last) / 3;
+    };
+    auto take = [&](double t, int end, size_t from) {
+      if (best_c == 0 || t < best_us) best_us = t, best_c = c, best_end = end, best_from = from;
+    };
+    take(us(groups, c), c, rows.size());
+    // the last tiles, as much work as CUs wait for, in shorter runs
+    const int end = std::max(1, std::min(c, longest) / 4);
+    double left = one(c) * 0.75 * places / (sh.kv_heads * stage_us);
+    size_t from = rows.size();
+    if (end < c && left < all / 2) {
+      while (left > 0) {
+        const int n = rows[--from].stages;
+        left -= n;
+        groups += cdiv(n, end) - cdiv(n, c);
+      }
+      take(us(groups, end), end, from);
     }
-    const double one = std::min(c, longest) * stage_us * 0.65 + start_us;  // alone on its CU
-    const double us = std::max(one, sh.kv_heads * (stages * stage_us + groups * start_us) / places) + one / 3;
-    if (best_c == 0 || us < best_us) best_us = us, best_c = c;
     if (c >= longest) break;
   }
   for (size_t i = 0; i < plan.tiles.size(); ++i) {
     WeightTile& t = plan.tiles[i];
-    const int n = (int)cdiv(rows[i].stages, best_c), tokens = rows[i].r.end - rows[i].r.begin;
+    const int n = (int)cdiv(rows[i].stages, i < best_from ? best_c : best_end), tokens = rows[i].r.end - rows[i].r.begin;
     t.part = plan.parts;
     for (int j = 0; j < n; ++j) {
       const int a = (int)((long long)tokens * j / n), b = (int)((long long)tokens * (j + 1) / n);
