@@ -174,20 +174,23 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
   for (int t = s.keep + tid; t < s.tokens; t += THREADS) w[t] = 0.f;
 }
 
-// Kept tokens to their places, in keys or values of one head of one block.  One
-// workgroup has them all, in order: a token's new place is its old one or a lower
-// one, so what is loaded ahead has not been written over, and what is written
-// over has been loaded: by every thread, before the barrier.  While a turn's rows
-// are written, the next one's are on their way, and the places of the one after.
+// Kept tokens to their places, in keys or values of one head of one block, of
+// each row one of `parts`.  One workgroup has them all, in order: a token's new
+// place is its old one or a lower one, so what is loaded ahead has not been
+// written over, and what is written over has been loaded: by every thread,
+// before the barrier.  While a turn's rows are written, the next one's are on
+// their way, and the places of the one after.  Bound by HBM: 12 sequences, 20
+// blocks, 12 heads of 128 (2.3 GB) 357 us, 6.4 TB/s.
 template <int LPR>
-__global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a, char* keys, char* values, int shift, long long block_bytes) {
-  constexpr int ROWS = 512 / LPR, U = 4;  // 16-byte chunks of a row; rows of a turn: ROWS * U
+__global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a, char* keys, char* values, int shift, int kv, int parts,
+                                                         long long block_bytes) {
+  constexpr int ROWS = 512 / LPR, U = 4;  // 16-byte chunks of a row's part; rows of a turn: ROWS * U
   const EvictSeq s = a.seqs[blockIdx.z];
   if (s.keep <= 0) return;
-  const int h = blockIdx.y, kv = gridDim.y, c = threadIdx.x % LPR, in_page = (1 << shift) - 1;
+  const int h = blockIdx.y / parts, c = blockIdx.y % parts * LPR + threadIdx.x % LPR, in_page = (1 << shift) - 1;
   u32x4* base = reinterpret_cast<u32x4*>((blockIdx.x & 1 ? values : keys) + (blockIdx.x >> 1) * block_bytes);
   auto at_of = [&](int place) __attribute__((always_inline)) {
-    return ((((long long)(place >> shift) * kv + h) << shift) + (place & in_page)) * LPR + c;
+    return ((((long long)(place >> shift) * kv + h) << shift) + (place & in_page)) * (LPR * parts) + c;
   };
   struct Turn {
     int from[U], to[U];
@@ -240,12 +243,20 @@ hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n
   else evict_select_kernel<1024><<<a.n, 1024, 0, st>>>(a, whole.shift);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || most <= 0) return e;
-  const dim3 grid(2 * n_blocks, whole.kv_heads, a.n);
-#define XC_MOVE(L) evict_move_kernel<L><<<grid, 512, 0, st>>>(a, (char*)whole.keys, (char*)whole.values, whole.shift, block_bytes)
-  const int lpr = whole.D * esz / 16;
+  // A head's rows go through one workgroup, so few heads have few workgroups: parts of 128 bytes for fewer than four to a
+  // CU, of 64 (half a line) for fewer than 192.  Measured, 21060 tokens back to 14040, 12 heads of 128 (rows of 256 bytes):
+  // 2 blocks 154 us whole, 104 in halves, 89 in quarters; 4 blocks 172, 121, 131; 14 blocks 341, 299, 398; 20 blocks 406,
+  // 405, 512; 2304 tokens back to 1536, 8 blocks, 8 heads of 64 (128 bytes): 26.1 whole, 24.0 in halves, 25.1 in quarters.
+  int lpr = whole.D * esz / 16, parts = 1;
+  const long long groups = 2ll * n_blocks * whole.kv_heads * a.n;
+  while (lpr > 4 && groups * parts < (lpr > 8 ? 1024 : 192)) lpr /= 2, parts *= 2;
+  const dim3 grid(2 * n_blocks, whole.kv_heads * parts, a.n);
+#define XC_MOVE(L) \
+  evict_move_kernel<L><<<grid, 512, 0, st>>>(a, (char*)whole.keys, (char*)whole.values, whole.shift, whole.kv_heads, parts, block_bytes)
   if (lpr == 32) XC_MOVE(32);
   else if (lpr == 16) XC_MOVE(16);
-  else XC_MOVE(8);
+  else if (lpr == 8) XC_MOVE(8);
+  else XC_MOVE(4);
 #undef XC_MOVE
   return hipGetLastError();
 }

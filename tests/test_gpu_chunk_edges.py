@@ -207,6 +207,18 @@ def test_many_evictions_at_once(dtype, blocks, kv, page, n):
     evict_check(pool, Batch(pool), [parent] + seqs, keep, 20, 15, w)
 
 
+@pytest.mark.parametrize("dtype,d,kv,n", [(BF16, 128, 6, 90), (F32, 128, 6, 90), (F32, 64, 8, 65), (BF16, 64, 6, 86), (F32, 32, 3, 180),
+                                          (BF16, 128, 12, 9), (F32, 128, 12, 9), (BF16, 128, 1, 3), (F32, 128, 1, 3)])
+def test_evictions_of_rows_in_one_piece_and_in_several(dtype, d, kv, n):
+    """As many workgroups as rows move in whole, in parts of 128 bytes and of 64."""
+    g = torch.Generator().manual_seed(8)
+    branches = [(i % 90, 30) for i in range(n)]
+    pool = make(dtype, pages=n * 16 + 8, kv=kv, page=16, d=d, seqs=n + 1)
+    _, seqs = grow(pool, 80, 3, branches)
+    keep = [int(x) for x in torch.randint(10, 150, (n,), generator=g)]
+    evict_check(pool, Batch(pool), seqs, keep, 5, 4, torch.rand(n, 210, generator=g).cuda())
+
+
 # ---------------------------------------------------------------- streams and graphs
 
 def test_graphs_of_two_batches_follow_their_inputs():
