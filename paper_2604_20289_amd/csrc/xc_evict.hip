@@ -37,14 +37,17 @@ __device__ __forceinline__ int waves_before(const int* totals, int lane, int wav
   return wave == 0 ? 0 : __builtin_amdgcn_readlane(up, wave - 1);
 }
 
-// Which tokens a sequence keeps: the m-th largest weight of those that are
-// neither among the first nor the last, by a search over the digits of its
-// order (11, 11, 10 bits, a histogram each, until all of a digit's are wanted),
-// then one pass in order that ranks
-// and lists the kept ones and moves their weights.  A workgroup a sequence: its
-// time is latency, of LDS and of barriers, 16 waves' or, for few tokens, 4's.
-// Orders stay in registers where a thread has room for its own.
-constexpr int kBins = 2048, kSelectFew = 4096;
+// Which tokens a sequence keeps: those of the m-th largest order and above,
+// where the first and the last ones' is above all others.  A search over the
+// order's digits (11, 11, 10 bits, a histogram each, until all of a digit's are
+// wanted), then one pass that ranks and lists the kept ones and moves their
+// weights.  A workgroup a sequence, each wave a run of its tokens: its time is
+// latency, of LDS and of barriers, and one CU's instructions.  Up to 24 tokens a
+// thread stay in registers, with their orders.  2304 tokens, 768 of them 0, take
+// 6.8 us, 21060 with 7020 16.4; with a pass of two barriers for every 8 tokens a
+// thread, and orders formed anew each time, 12 and 26.  256 threads are quicker
+// than 1024 up to about 1000 tokens (a call for 2000 takes 21.3 and 19.3 us).
+constexpr int kBins = 2048, kSelectFew = 1024;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int shift) {
   constexpr int WAVES = THREADS / 64, HELD = 24, ITEMS = 8, PER = kBins / THREADS;
@@ -59,42 +62,49 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
   __shared__ __attribute__((aligned(16))) int hist[kBins][4];  // a copy for every fourth lane
   __shared__ int totals[2][WAVES];
   __shared__ int found[3];
+  __shared__ int pages[HELD * THREADS / 16 + 1];
   float* w = a.weights + s.number * a.ld;
-  const int lo = a.sinks, hi = s.tokens - a.recent;
-  int want = s.keep - a.sinks - a.recent;  // of them
-  const bool any = want > 0, held = hi - lo <= HELD * THREADS;
-  unsigned prefix = 0;                     // the digits found so far
-  int below = 32;                          // the bits behind them
+  constexpr unsigned kAlways = ~0u;  // (of no weight)
+  auto order_at = [&](float x, int t) __attribute__((always_inline)) {
+    // behind the last token: 0, with the lightest, and behind all of them in every tie
+    return t < s.tokens ? (t >= a.sinks && t < s.tokens - a.recent ? order_of(x) : kAlways) : 0u;
+  };
+  int want = s.keep - a.sinks - a.recent;  // of the others
+  const bool held = s.tokens <= HELD * THREADS;
+  const int span = (s.tokens + THREADS - 1) / THREADS * 64, mine = wave * span + lane;
+  float own[HELD];
   unsigned order[HELD];
-  if (any && held) {
+  if (held) {
 #pragma unroll
-    for (int u = 0; u < HELD; ++u) {
-      const int t = lo + u * THREADS + tid;
-      if (u * THREADS < hi - lo) order[u] = order_of(w[t < hi ? t : lo]);
-    }
+    for (int u = 0; u < HELD; ++u)
+      if (u * 64 < span) own[u] = w[min(mine + u * 64, s.tokens - 1)];
+    for (int i = tid; i <= (s.first + s.tokens - 1) >> shift; i += THREADS) pages[i] = a.tables[s.from + i];
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+      if (u * 64 < span) order[u] = order_at(own[u], mine + u * 64);
   }
-  for (int pass = 0; pass < 3 && any; ++pass) {
+  unsigned prefix = 0;  // the digits found so far
+  int below = 32;       // the bits behind them
+  if (want == 0) prefix = kAlways - 1, below = 0;
+  for (int pass = 0; pass < 3 && want > 0; ++pass) {
     const int bits = pass == 2 ? 10 : 11, low = below - bits;
 #pragma unroll
     for (int i = 0; i < PER; ++i) *reinterpret_cast<i32x4*>(hist[i * THREADS + tid]) = i32x4{0, 0, 0, 0};
     __syncthreads();
-    auto count = [&](unsigned o, bool is) __attribute__((always_inline)) {
-      if (is && (pass == 0 || o >> below == prefix)) atomicAdd(&hist[o >> low & ((1 << bits) - 1)][lane & 3], 1);
+    auto count = [&](unsigned o) __attribute__((always_inline)) {
+      if (pass == 0 ? o != kAlways : o >> below == prefix) atomicAdd(&hist[o >> low & ((1 << bits) - 1)][lane & 3], 1);
     };
     if (held) {
 #pragma unroll
       for (int u = 0; u < HELD; ++u)
-        if (u * THREADS < hi - lo) count(order[u], lo + u * THREADS + tid < hi);
+        if (u * 64 < span) count(order[u]);
     } else {
-      for (int t0 = lo; t0 < hi; t0 += THREADS * ITEMS) {
+      for (int t0 = 0; t0 < s.tokens; t0 += THREADS * ITEMS) {
         float x[ITEMS];
 #pragma unroll
-        for (int u = 0; u < ITEMS; ++u) {
-          const int t = t0 + u * THREADS + tid;
-          x[u] = w[t < hi ? t : lo];
-        }
+        for (int u = 0; u < ITEMS; ++u) x[u] = w[min(t0 + u * THREADS + tid, s.tokens - 1)];
 #pragma unroll
-        for (int u = 0; u < ITEMS; ++u) count(order_of(x[u]), t0 + u * THREADS + tid < hi);
+        for (int u = 0; u < ITEMS; ++u) count(order_at(x[u], t0 + u * THREADS + tid));
       }
     }
     __syncthreads();
@@ -123,53 +133,87 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
     if (found[2] == want) break;
   }
   const int ties = want;  // of those as heavy as the lightest kept one, the first so many
-
-  int tie0 = 0, kept0 = 0;  // before the tokens at hand
-  for (int t0 = 0; t0 < s.tokens; t0 += THREADS * ITEMS) {
-    float x[ITEMS];
-    unsigned long long tie[ITEMS], sel[ITEMS];
-    const int at = t0 + wave * 64 * ITEMS + lane;
+  const unsigned long long lower = (1ull << lane) - 1;
+  // lanes whose token is as heavy as the lightest kept one, and heavier
+  struct Lanes {
+    unsigned long long tie, more;
+  };
+  auto lanes_of = [&](unsigned o) __attribute__((always_inline)) {
+    return Lanes{__builtin_amdgcn_ballot_w64(o >> below == prefix), __builtin_amdgcn_ballot_w64(o >> below > prefix)};
+  };
+  auto kept_of = [&](const Lanes& l, int rank) __attribute__((always_inline)) {
+    const bool tie = l.tie >> lane & 1, more = l.more >> lane & 1;
+    return __builtin_amdgcn_ballot_w64(more || (tie && rank + __popcll(l.tie & lower) < ties));
+  };
+  auto keep = [&](int t, int j, float x, int page) __attribute__((always_inline)) {
+    const int place = s.first + t;
+    a.src[s.at + j] = (page << shift) + (place & ((1 << shift) - 1));
+    if (kept) kept[j] = t;
+    w[j] = x;
+  };
+  // kept by the waves before this one, of ties (and all tokens) before the waves' at hand
+  auto before = [&](int tie0, int& rank, int& pos, int& all_ties, int& all_kept) __attribute__((always_inline)) {
+    const int tie = lane < WAVES ? totals[0][lane] : 0, tie_to = lanes_up_to(tie), tie_before = tie0 + tie_to - tie;
+    const int n = (lane < WAVES ? totals[1][lane] : 0) + min(max(ties - tie_before, 0), tie), to = lanes_up_to(n);
+    rank = __builtin_amdgcn_readlane(tie_before, wave);
+    pos = __builtin_amdgcn_readlane(to - n, wave);
+    all_ties = __builtin_amdgcn_readlane(tie_to, 63);
+    all_kept = __builtin_amdgcn_readlane(to, 63);
+  };
+  int rank, pos, all_ties, all_kept;
+  if (held) {
+    int n_tie = 0, n_more = 0;
 #pragma unroll
-    for (int u = 0; u < ITEMS; ++u) x[u] = at + u * 64 < s.tokens ? w[at + u * 64] : 0.f;
-    int n = 0;
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int t = at + u * 64;
-      tie[u] = __builtin_amdgcn_ballot_w64(any && t >= lo && t < hi && order_of(x[u]) >> below == prefix);
-      n += __popcll(tie[u]);
-    }
-    if (lane == 0) totals[0][wave] = n;
-    __syncthreads();
-    int all;
-    int rank = tie0 + waves_before<WAVES>(totals[0], lane, wave, all);
-    tie0 += all;
-    n = 0;
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int t = at + u * 64, mine = rank + __popcll(tie[u] & ((1ull << lane) - 1));
-      const bool is_tie = tie[u] >> lane & 1, mid = t >= lo && t < hi;
-      sel[u] = __builtin_amdgcn_ballot_w64(t < s.tokens &&
-                                           (!mid || (any && (is_tie ? mine < ties : order_of(x[u]) >> below > prefix))));
-      rank += __popcll(tie[u]);
-      n += __popcll(sel[u]);
-    }
-    if (lane == 0) totals[1][wave] = n;
-    __syncthreads();
-    int pos = kept0 + waves_before<WAVES>(totals[1], lane, wave, all);
-    kept0 += all;
-    // a kept token goes to its own place or a lower one, and all of this turn have been read
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int t = at + u * 64, j = pos + __popcll(sel[u] & ((1ull << lane) - 1));
-      if (sel[u] >> lane & 1) {
-        const int place = s.first + t;
-        a.src[s.at + j] = (a.tables[s.from + (place >> shift)] << shift) + (place & ((1 << shift) - 1));
-        if (kept) kept[j] = t;
-        w[j] = x[u];
+    for (int u = 0; u < HELD; ++u)
+      if (u * 64 < span) {
+        const Lanes l = lanes_of(order[u]);
+        n_tie += __popcll(l.tie), n_more += __popcll(l.more);
+        asm volatile("" ::"v"(own[u]));  // (there before anything is written)
       }
-      pos += __popcll(sel[u]);
-    }
+    if (lane == 0) totals[0][wave] = n_tie, totals[1][wave] = n_more;
     __syncthreads();
+    before(0, rank, pos, all_ties, all_kept);
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+      if (u * 64 < span) {
+        const Lanes l = lanes_of(order[u]);
+        const unsigned long long sel = kept_of(l, rank);
+        const int t = mine + u * 64;
+        if (sel >> lane & 1) keep(t, pos + __popcll(sel & lower), own[u], pages[(s.first + t) >> shift]);
+        rank += __popcll(l.tie);
+        pos += __popcll(sel);
+      }
+  } else {
+    int tie0 = 0, kept0 = 0;  // before the tokens at hand
+    for (int t0 = 0; t0 < s.tokens; t0 += THREADS * ITEMS) {
+      float x[ITEMS];
+      Lanes l[ITEMS];
+      const int at = t0 + wave * 64 * ITEMS + lane;
+#pragma unroll
+      for (int u = 0; u < ITEMS; ++u) x[u] = w[min(at + u * 64, s.tokens - 1)];
+      int n_tie = 0, n_more = 0;
+#pragma unroll
+      for (int u = 0; u < ITEMS; ++u) {
+        l[u] = lanes_of(order_at(x[u], at + u * 64));
+        n_tie += __popcll(l[u].tie), n_more += __popcll(l[u].more);
+        asm volatile("" ::"v"(x[u]));
+      }
+      if (lane == 0) totals[0][wave] = n_tie, totals[1][wave] = n_more;
+      __syncthreads();
+      before(tie0, rank, pos, all_ties, all_kept);
+      pos += kept0;
+      tie0 += all_ties, kept0 += all_kept;
+      // a kept token goes to its own place or a lower one, and all of this turn have been read
+#pragma unroll
+      for (int u = 0; u < ITEMS; ++u) {
+        const unsigned long long sel = kept_of(l[u], rank);
+        const int t = at + u * 64;
+        if (sel >> lane & 1) keep(t, pos + __popcll(sel & lower), x[u], a.tables[s.from + ((s.first + t) >> shift)]);
+        rank += __popcll(l[u].tie);
+        pos += __popcll(sel);
+      }
+      __syncthreads();  // (totals have been read)
+    }
   }
   for (int t = s.keep + tid; t < s.tokens; t += THREADS) w[t] = 0.f;
 }

@@ -219,6 +219,22 @@ def test_evictions_of_rows_in_one_piece_and_in_several(dtype, d, kv, n):
     evict_check(pool, Batch(pool), seqs, keep, 5, 4, torch.rand(n, 210, generator=g).cuda())
 
 
+@pytest.mark.parametrize("n", [1000, 1024, 1025, 5000, 24576, 24577, 60000])
+@pytest.mark.parametrize("sinks,recent", [(0, 0), (7, 300)])
+def test_evictions_among_few_different_weights(sinks, recent, n):
+    """Ties that begin and end in other waves' tokens, of every value that is none like the others."""
+    pool = make(BF16, pages=-(-(n + 3) // 64) + 1, kv=1, page=64, d=64, seqs=2)
+    batch, s, g = Batch(pool), pool.new(), torch.Generator().manual_seed(n)
+    pool.extend([s], [n + 3])
+    pool.trim(s, front=3)
+    values = torch.tensor([math.nan, 0.0, -0.0, 0.25, 1.0, math.inf, -math.inf, 1e-40, -2.0])
+    for keep in (n - 1, n * 5 // 7, n // 2, n // 9 + 310):
+        if keep >= pool.tokens(s):
+            continue
+        w = values[torch.randint(0, len(values), (1, pool.tokens(s)), generator=g)]
+        evict_check(pool, batch, [s], [keep], sinks, recent, w.cuda())
+
+
 # ---------------------------------------------------------------- streams and graphs
 
 def test_graphs_of_two_batches_follow_their_inputs():
