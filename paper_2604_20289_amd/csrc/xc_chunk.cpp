@@ -250,11 +250,11 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
         most_tokens = std::max(most_tokens, q.tokens);
         most_kept = std::max(most_kept, keep[i]);
         if (places + keep[i] > kMaxPlaces) return XC_ERR_UNSUPPORTED;
-        list.push_back({i, q.first, q.tokens, keep[i], (int)tables.size(), 0, (int)places});
+        list.push_back({i, q.first, q.tokens, keep[i], (int)tables.size(), 0, (int)places, 0});
         tables.insert(tables.end(), q.pages.begin(), q.pages.end());
         places += keep[i];
       } else if (kept) {
-        list.push_back({i, q.first, q.tokens, -1, 0, 0, 0});
+        list.push_back({i, q.first, q.tokens, -1, 0, 0, 0, 0});
       }
     }
     if (most_tokens > 0 && (!weights || ld < most_tokens)) return XC_ERR_INVALID_ARG;
@@ -267,7 +267,8 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
     // room for twice the tables: the new ones are no longer
     const size_t o_tables = align256(list.size() * sizeof(EvictSeq));
     const size_t up_most = o_tables + align256(2 * tables.size() * sizeof(int));
-    const size_t need = up_most + align256((size_t)places * sizeof(int));
+    const size_t o_stays = up_most + align256((size_t)places * sizeof(int));
+    const size_t need = o_stays + align256(list.size() * sizeof(int));
     tables.reserve(2 * tables.size());
     if (!staging(b, b->evict, b->evict_bytes, need, up_most)) return XC_ERR_OOM;
     std::vector<std::vector<int>> next;
@@ -276,7 +277,10 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
     committed([&] {
       for (EvictSeq& e : list) {
         e.to = (int)tables.size();
-        if (e.keep >= 0) tables.insert(tables.end(), next[e.number].begin(), next[e.number].end());
+        if (e.keep < 0) continue;
+        const std::vector<int>& now = next[e.number];
+        e.replaced = !std::equal(now.begin(), now.end(), tables.begin() + e.from);
+        tables.insert(tables.end(), now.begin(), now.end());
       }
       put(b, 0, list);
       put(b, o_tables, tables);
@@ -285,6 +289,7 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
       a.seqs = (const EvictSeq*)b->evict;
       a.tables = (const int*)(b->evict + o_tables);
       a.src = (int*)(b->evict + up_most);
+      a.stays = (int*)(b->evict + o_stays);
       a.n = (int)list.size();
       a.sinks = sinks;
       a.recent = recent;

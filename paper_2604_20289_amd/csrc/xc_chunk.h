@@ -39,11 +39,13 @@ struct EvictSeq {
   int keep;          // < tokens; -1: all of them, only listed
   int from, to;      // its old and new page table begin at tables[from], tables[to]
   int at;            // its kept tokens' places begin at src[at]
+  int replaced;      // some of its kept pages are other ones now
 };
 struct EvictArgs {
   const EvictSeq* seqs;
   const int* tables;
-  int* src;  // places (page * page tokens + row) of the kept tokens
+  int* src;    // places (page * page tokens + row) of the kept tokens
+  int* stays;  // [n] of its first tokens, all kept
   int n, sinks, recent;
   float* weights;  // [n][ld]
   long long ld;

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
   }
   __shared__ __attribute__((aligned(16))) int hist[kBins][4];  // a copy for every fourth lane
   __shared__ int totals[2][WAVES];
-  __shared__ int found[3];
+  __shared__ int found[3], stays;
   __shared__ int pages[HELD * THREADS / 16 + 1];
   float* w = a.weights + s.number * a.ld;
   constexpr unsigned kAlways = ~0u;  // (of no weight)
@@ -160,7 +160,11 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
     all_ties = __builtin_amdgcn_readlane(tie_to, 63);
     all_kept = __builtin_amdgcn_readlane(to, 63);
   };
-  int rank, pos, all_ties, all_kept;
+  int rank, pos, all_ties, all_kept, first = s.keep;  // first: of this wave's tokens, the first one not kept
+  auto not_kept = [&](unsigned long long sel, int t0) __attribute__((always_inline)) {  // of the 64 from t0 on
+    if (~sel) first = min(first, t0 + (int)__builtin_ctzll(~sel));
+  };
+  if (tid == 0) stays = s.keep;
   if (held) {
     int n_tie = 0, n_more = 0;
 #pragma unroll
@@ -180,6 +184,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
         const unsigned long long sel = kept_of(l, rank);
         const int t = mine + u * 64;
         if (sel >> lane & 1) keep(t, pos + __popcll(sel & lower), own[u], pages[(s.first + t) >> shift]);
+        not_kept(sel, wave * span + u * 64);
         rank += __popcll(l.tie);
         pos += __popcll(sel);
       }
@@ -209,13 +214,17 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
         const unsigned long long sel = kept_of(l[u], rank);
         const int t = at + u * 64;
         if (sel >> lane & 1) keep(t, pos + __popcll(sel & lower), x[u], a.tables[s.from + ((s.first + t) >> shift)]);
+        not_kept(sel, t0 + wave * 64 * ITEMS + u * 64);
         rank += __popcll(l[u].tie);
         pos += __popcll(sel);
       }
       __syncthreads();  // (totals have been read)
     }
   }
+  if (lane == 0 && first < s.keep) atomicMin(&stays, first);
   for (int t = s.keep + tid; t < s.tokens; t += THREADS) w[t] = 0.f;
+  __syncthreads();
+  if (tid == 0) a.stays[blockIdx.x] = stays;
 }
 
 // Kept tokens to their places, in keys or values of one head of one block, of
@@ -262,8 +271,10 @@ __global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a, char* keys
     for (int u = 0; u < U; ++u)
       if (t.from[u] != t.to[u]) base[at_of(t.to[u])] = t.x[u];
   };
-  // tokens in pages before the last first one's stay
-  const int sink_page = (s.first + min(a.sinks, s.keep)) >> shift << shift, j0 = max(0, sink_page - s.first);
+  // tokens before the first one given up stay, but for replaced pages: there those of pages of nothing but first tokens
+  const int sink_page = (s.first + min(a.sinks, s.keep)) >> shift << shift;
+  const int j0 = s.replaced ? max(0, sink_page - s.first) : a.stays[blockIdx.z];
+  if (j0 >= s.keep) return;
   Turn t[2];
   places(t[0], j0);
   load(t[0]);
