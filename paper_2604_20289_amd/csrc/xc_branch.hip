@@ -27,9 +27,10 @@
 // Each has a second form (CHUNK) for rows under a mask, cut by plan_chunk: of a
 // unit's tiles, those that hide something from some row are masked, a 32-bit
 // word per lane and half tile, the others run as without a mask.  24192 causal
-// rows, 16 heads of 128: 2.08 ms, 1154 TFLOP/s of what is seen; 7020 rows in three
-// frames over 21060 keys, 12 heads of 128: 747 us; 13 causal chunks, 9860 rows
-// over 4.4 to 6.1 thousand keys, 16 heads of 64 on 4: 245 us, 824 TFLOP/s.
+// rows, 16 heads of 128: 2.08 to 2.17 ms, 1105 to 1154 TFLOP/s of what is seen; 7020
+// rows in three frames over 21060 keys, 12 heads of 128: 747 to 772 us; 13 causal
+// chunks, 9860 rows over 4.4 to 6.1 thousand keys, 16 heads of 64 on 4: 248 us, 814
+// TFLOP/s.
 #include "xc_pool.h"
 
 #include "xc_internal.h"
