@@ -135,7 +135,7 @@ __device__ __forceinline__ bool clean_blocks(char* tile, int step, int lane) {
   return __builtin_amdgcn_ballot_w64(any != 0) != 0;
 }
 
-// The page table of a unit, 64 entries at a time// The page table of a unit, 64 entries at a time: entry e0 + lane.
+// The page table of a unit, 64 entries at a time: entry e0 + lane.
 struct TableWindow {
   const int* table;
   int e0, e_last, entries, shift, lane;

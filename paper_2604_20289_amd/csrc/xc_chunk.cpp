@@ -55,8 +55,7 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     const ChunkSeq& q = chunk_seqs[part.seq];
     batch_seqs.push_back({part.tok0, q.first + q.tokens - q.rows + (part.tok0 - q.row0), q.table, part.own});
   }
-  if (!enlarge(p, b->parts, b->part_bytes, part_need, part_need / 4)) return XC_ERR_OOM;
-  // uploaded: tables, sequences, units; written on the device: places, own slots
+  // uploaded: tables, sequences, units; written on the device: places, own slots, partial sums
   const size_t o_seqs = align256(r.tables.size() * sizeof(int));
   const size_t o_chunks = o_seqs + align256(batch_seqs.size() * sizeof(BatchSeq));
   const size_t o_units = o_chunks + align256(chunk_seqs.size() * sizeof(ChunkSeq));
@@ -66,7 +65,7 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const size_t o_tiles = o_sums + align256(sums.units.size() * sizeof(WeightUnit));
   const size_t up = o_tiles + align256(sums.tiles.size() * sizeof(WeightTile));
   const size_t o_own = up + align256(rows * sizeof(int));
-  const size_t need = o_own + align256(rows * sizeof(OwnSlots));
+  const size_t o_parts = o_own + align256(rows * sizeof(OwnSlots)), need = o_parts + part_need;
   std::vector<int> seq_copy(seqs, seqs + n);
   if (!staging(b, b->dev, b->dev_bytes, need, up)) return XC_ERR_OOM;
   if (rows > 0) {
@@ -114,7 +113,7 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   w.n_units = (int)sums.units.size();
   w.n_long = long_units(sums.units);
   w.n_tiles = (int)sums.tiles.size();
-  w.parts = (float*)b->parts;
+  w.parts = (float*)(b->dev + o_parts);
   w.runs = (const WeightFew*)(b->dev + o_runs);
   w.infos = (const WeightInfo*)(b->dev + o_infos);
   w.n_runs = (int)few.size();

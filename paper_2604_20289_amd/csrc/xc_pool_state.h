@@ -133,8 +133,6 @@ struct xc_batch {
   size_t dev_bytes = 0;
   char* pieces = nullptr;
   size_t piece_bytes = 0;
-  char* parts = nullptr;  // partial sums of weights
-  size_t part_bytes = 0;
   char* evict = nullptr;  // an eviction's tables and choices
   size_t evict_bytes = 0;
   char* pinned = nullptr;
