@@ -595,7 +595,11 @@ __global__ __launch_bounds__(256, 2) void weights_few_kernel(WeightArgs a) {
   __shared__ __attribute__((aligned(1024))) char ring[4 * 2 * few_keys(D) * D * 2];  // (one array and no other, as above)
   // its run is the last that begins at this workgroup or before: a lane each, 64 of them at a time
   int i = 0;
-  while (i + 64 < a.n_runs && a.runs[i + 64].group0 <= (int)blockIdx.x) i += 64;
+  for (int n = (a.n_runs + 63) / 64; n > 1;) {
+    const int half = n / 2;
+    if (a.runs[i + half * 64].group0 <= (int)blockIdx.x) i += half * 64, n -= half;
+    else n = half;
+  }
   const WeightFew mine = a.runs[min(i + (int)(threadIdx.x & 63), a.n_runs - 1)];
   const bool before = i + (int)(threadIdx.x & 63) < a.n_runs && mine.group0 <= (int)blockIdx.x;
   const int at = __popcll(__builtin_amdgcn_ballot_w64(before)) - 1;

@@ -49,15 +49,16 @@ def test_many_rows_of_any_number_of_heads(kv, group, d, dtype, rows):
         check(pool, batch, seqs, new, mask)
 
 
-def test_many_single_tokens():
-    """Seventy sequences of one row over a history that they share, each with tokens of its own."""
-    branches = [(i % 23, 1) for i in range(70)]
-    pool = make(BF16, pages=pages_for(500, branches, 16), kv=2, page=16, d=64, seqs=71)
+@pytest.mark.parametrize("n,d", [(65, 128), (70, 64), (129, 64), (300, 128), (700, 64)])
+def test_many_single_tokens(n, d):
+    """Sequences of one row over a history that they share, each with tokens of its own."""
+    branches = [(i % 23, 1) for i in range(n)]
+    pool = make(BF16, pages=pages_for(500, branches, 16), kv=2, page=16, d=d, seqs=n + 1)
     _, seqs = grow(pool, 500, 3, branches)
     batch = Batch(pool)
     for mask in ((1, 0, 0), (1, 64, 4)):
-        batch.set_chunk(seqs, [1] * 70, *mask)
-        check(pool, batch, seqs, [1] * 70, mask)
+        batch.set_chunk(seqs, [1] * n, *mask)
+        check(pool, batch, seqs, [1] * n, mask)
 
 
 @pytest.mark.parametrize("dtype,kv,d,n", [(BF16, 2, 128, 9), (BF16, 1, 64, 40), (F32, 2, 64, 5), (BF16, 2, 64, 300)])
