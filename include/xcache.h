@@ -602,6 +602,8 @@ xc_status xc_chunk_attention(xc_batch* batch, int32_t block, const void* q, int6
  * rows and columns of weights are left as they are.
  *   q, scale : as in xc_chunk_attention, lse: what it gave.
  *   decay    : 1 adds up, 0 begins anew (weights is not read then); >= 0.
+ *              Where it is not 0, the columns of tokens that are new since the
+ *              last call are the caller's to clear (xc_chunk_evict leaves 0).
  *   weights  : device float32 [n of xc_chunk_set][ld], ld at least the tokens of
  *              the longest sequence; does not overlap q, lse or the page
  *              buffers.
