@@ -53,6 +53,12 @@ struct EvictArgs {
   long long kept_ld;
 };
 
+// What fits into a kernel's arguments.
+struct LittleUpload {
+  static constexpr size_t kMost = 3584;
+  alignas(16) char bytes[kMost];
+};
+hipError_t launch_upload(const LittleUpload& from, void* to, int bytes, hipStream_t st);
 hipError_t launch_weights(int dtype, const WeightArgs& a, hipStream_t st);
 // whole: the first block; of the sequences that shrink, most_tokens before and
 // `most` kept
