@@ -8,31 +8,6 @@ using namespace xc;
 
 namespace {
 
-// What an eviction sends to the device, `most` bytes of it at most: with a launch where that is little, else through the
-// batch's staging memory.  2304 tokens back to 1536, 8 blocks, 8 heads of 64: 17.4 us a call with a launch, 20.0 with a
-// copy; 12 sequences, 20 blocks, 12 heads of 128 391 and 394.  (xc_chunk_set takes as long either way.)
-class Sent {
- public:
-  Sent(xc_batch* b, size_t most) : b_(b), most_(most), little_(most <= LittleUpload::kMost) {}
-  bool room(char*& dev, size_t& have, size_t need) {
-    return little_ ? enlarge(*b_->p, dev, have, need, need / 2) : staging(b_, dev, have, need, most_);
-  }
-  template <typename T>
-  void put(size_t at, const std::vector<T>& v) {
-    if (!v.empty()) std::memcpy((little_ ? words_.bytes : b_->pinned) + at, v.data(), v.size() * sizeof(T));
-  }
-  void send(char* dev, size_t bytes) {
-    if (little_) XC_HIP(launch_upload(words_, dev, (int)bytes, b_->p->st));
-    else upload(b_, dev, bytes);
-  }
-
- private:
-  xc_batch* b_;
-  size_t most_;
-  bool little_;
-  LittleUpload words_{};
-};
-
 xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* new_tokens, const ChunkMask& mask) {
   Pool& p = *b->p;
   BatchRows r;
@@ -294,8 +269,13 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
     const size_t o_stays = up_most + align256((size_t)places * sizeof(int));
     const size_t need = o_stays + align256(list.size() * sizeof(int));
     tables.reserve(2 * tables.size());
-    Sent sent(b, up_most);
-    if (!sent.room(b->evict, b->evict_bytes, need)) return XC_ERR_OOM;
+    // A few tables go with the launch: nothing to wait for, and no copy.  2304 tokens back to 1536, 8 blocks, 8 heads of 64:
+    // 14.5 us a call so, 17.4 with a launch for them alone, 19.8 with a copy; 12 sequences, 20 blocks, 12 heads of 128: 390,
+    // 392 and 395.
+    Little words{};
+    const bool little = up_most <= Little::kMost;
+    if (!(little ? enlarge(p, b->evict, b->evict_bytes, need, need / 2) : staging(b, b->evict, b->evict_bytes, need, up_most)))
+      return XC_ERR_OOM;
     std::vector<std::vector<int>> next;
     const PageStatus s = p.book.evict(n, seqs, keep, sinks, &next);
     if (s != PageStatus::ok) return status_of(s);
@@ -307,12 +287,13 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
         e.replaced = !std::equal(now.begin(), now.end(), tables.begin() + e.from);
         tables.insert(tables.end(), now.begin(), now.end());
       }
-      sent.put(0, list);
-      sent.put(o_tables, tables);
-      sent.send(b->evict, o_tables + tables.size() * sizeof(int));
+      char* to = little ? words.bytes : b->pinned;
+      std::memcpy(to, list.data(), list.size() * sizeof(EvictSeq));
+      if (!tables.empty()) std::memcpy(to + o_tables, tables.data(), tables.size() * sizeof(int));
+      if (!little) upload(b, b->evict, up_most);
       EvictArgs a{};
-      a.seqs = (const EvictSeq*)b->evict;
-      a.tables = (const int*)(b->evict + o_tables);
+      a.seqs = (EvictSeq*)b->evict;
+      a.tables = (int*)(b->evict + o_tables);
       a.src = (int*)(b->evict + up_most);
       a.stays = (int*)(b->evict + o_stays);
       a.n = (int)list.size();
@@ -322,8 +303,8 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
       a.ld = ld;
       a.kept = kept;
       a.kept_ld = kept_ld;
-      XC_HIP(launch_evict(a, p.block(0), p.esz, p.cfg.n_blocks, p.block_elems() * p.esz, most_tokens, most_kept,
-                          p.st));
+      XC_HIP(launch_evict(a, little ? &words : nullptr, p.block(0), p.esz, p.cfg.n_blocks, p.block_elems() * p.esz,
+                          most_tokens, most_kept, p.st));
     });
     return XC_OK;
   });

@@ -42,8 +42,8 @@ struct EvictSeq {
   int replaced;      // some of its kept pages are other ones now
 };
 struct EvictArgs {
-  const EvictSeq* seqs;
-  const int* tables;
+  EvictSeq* seqs;
+  int* tables;
   int* src;    // places (page * page tokens + row) of the kept tokens
   int* stays;  // [n] of its first tokens, all kept
   int n, sinks, recent;
@@ -53,16 +53,15 @@ struct EvictArgs {
   long long kept_ld;
 };
 
+hipError_t launch_weights(int dtype, const WeightArgs& a, hipStream_t st);
 // What fits into a kernel's arguments.
-struct LittleUpload {
+struct Little {
   static constexpr size_t kMost = 3584;
   alignas(16) char bytes[kMost];
 };
-hipError_t launch_upload(const LittleUpload& from, void* to, int bytes, hipStream_t st);
-hipError_t launch_weights(int dtype, const WeightArgs& a, hipStream_t st);
 // whole: the first block; of the sequences that shrink, most_tokens before and
-// `most` kept
-hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes, int most_tokens,
-                        int most, hipStream_t st);
+// `most` kept; little: what seqs and, as far behind them, tables are to hold (null: they do)
+hipError_t launch_evict(const EvictArgs& a, const Little* little, const PageBuf& whole, int esz, int n_blocks,
+                        long long block_bytes, int most_tokens, int most, hipStream_t st);
 
 }  // namespace xc

@@ -6,6 +6,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace xc {
 
 namespace {
@@ -48,17 +50,25 @@ __device__ __forceinline__ int waves_before(const int* totals, int lane, int wav
 // thread, and orders formed anew each time, 12 and 26.  256 threads are quicker
 // than 1024 up to about 1000 tokens (a call for 2000 takes 21.3 and 19.3 us).
 constexpr int kBins = 2048, kSelectFew = 1024;
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int shift) {
+struct Nothing {};
+template <int THREADS, typename Sent>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int shift, Sent sent) {
   constexpr int WAVES = THREADS / 64, HELD = 24, ITEMS = 8, PER = kBins / THREADS;
   typedef int i32x4 __attribute__((ext_vector_type(4)));
-  const EvictSeq s = a.seqs[blockIdx.x];
+  // what came with the launch is passed on to the rows' kernel
+  constexpr bool LITTLE = std::is_same<Sent, Little>::value;
+  const char* words = LITTLE ? reinterpret_cast<const char*>(&sent) : reinterpret_cast<const char*>(a.seqs);
+  const EvictSeq s = reinterpret_cast<const EvictSeq*>(words)[blockIdx.x];
+  const int* tables = reinterpret_cast<const int*>(words + (reinterpret_cast<const char*>(a.tables) - reinterpret_cast<const char*>(a.seqs)));
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int* kept = a.kept ? a.kept + s.number * a.kept_ld : nullptr;
+  if (LITTLE && tid == 0) a.seqs[blockIdx.x] = s;
   if (s.keep < 0) {
     for (int t = tid; t < s.tokens; t += THREADS) kept[t] = t;
     return;
   }
+  if (LITTLE && s.keep > 0)
+    for (int i = tid; i <= (s.first + s.keep - 1) >> shift; i += THREADS) a.tables[s.to + i] = tables[s.to + i];
   __shared__ __attribute__((aligned(16))) int hist[kBins][4];  // a copy for every fourth lane
   __shared__ int totals[2][WAVES];
   __shared__ int found[3], stays;
@@ -78,7 +88,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
       if (u * 64 < span) own[u] = w[min(mine + u * 64, s.tokens - 1)];
-    for (int i = tid; i <= (s.first + s.tokens - 1) >> shift; i += THREADS) pages[i] = a.tables[s.from + i];
+    for (int i = tid; i <= (s.first + s.tokens - 1) >> shift; i += THREADS) pages[i] = tables[s.from + i];
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
       if (u * 64 < span) order[u] = order_at(own[u], mine + u * 64);
@@ -213,7 +223,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a, int 
       for (int u = 0; u < ITEMS; ++u) {
         const unsigned long long sel = kept_of(l[u], rank);
         const int t = at + u * 64;
-        if (sel >> lane & 1) keep(t, pos + __popcll(sel & lower), x[u], a.tables[s.from + ((s.first + t) >> shift)]);
+        if (sel >> lane & 1) keep(t, pos + __popcll(sel & lower), x[u], tables[s.from + ((s.first + t) >> shift)]);
         not_kept(sel, t0 + wave * 64 * ITEMS + u * 64);
         rank += __popcll(l[u].tie);
         pos += __popcll(sel);
@@ -292,10 +302,15 @@ __global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a, char* keys
 
 }  // namespace
 
-hipError_t launch_evict(const EvictArgs& a, const PageBuf& whole, int esz, int n_blocks, long long block_bytes, int most_tokens,
-                        int most, hipStream_t st) {
-  if (most_tokens <= kSelectFew) evict_select_kernel<256><<<a.n, 256, 0, st>>>(a, whole.shift);
-  else evict_select_kernel<1024><<<a.n, 1024, 0, st>>>(a, whole.shift);
+hipError_t launch_evict(const EvictArgs& a, const Little* little, const PageBuf& whole, int esz, int n_blocks,
+                        long long block_bytes, int most_tokens, int most, hipStream_t st) {
+  if (most_tokens <= kSelectFew) {
+    if (little) evict_select_kernel<256><<<a.n, 256, 0, st>>>(a, whole.shift, *little);
+    else evict_select_kernel<256><<<a.n, 256, 0, st>>>(a, whole.shift, Nothing{});
+  } else {
+    if (little) evict_select_kernel<1024><<<a.n, 1024, 0, st>>>(a, whole.shift, *little);
+    else evict_select_kernel<1024><<<a.n, 1024, 0, st>>>(a, whole.shift, Nothing{});
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || most <= 0) return e;
   // A head's rows go through one workgroup, so few heads have few workgroups: parts of 128 bytes for fewer than four to a

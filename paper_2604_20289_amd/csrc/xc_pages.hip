@@ -4,7 +4,6 @@
 //
 // All are bound by HBM (or, with few rows, by latency): every one moves
 // 16 bytes per lane and load, with several loads in flight per wave.
-#include "xc_chunk.h"
 #include "xc_pool.h"
 
 #include "xc_internal.h"
@@ -130,12 +129,6 @@ __global__ __launch_bounds__(256) void import_kernel(ImportArgs a, const T* __re
     const int t = i / per_row, c = (i - t * per_row) * V;
     *reinterpret_cast<vec*>(pv + dst(t) + c) = *reinterpret_cast<const vec*>(&tile[t * pitch + c]);
   }
-}
-
-// A few tables, sent with the launch: no staging memory to wait for, and no copy.
-__global__ __launch_bounds__(256) void upload_kernel(LittleUpload from, u32x4* to, int n) {
-  static_assert(LittleUpload::kMost <= 256 * 16);
-  if ((int)threadIdx.x < n) to[threadIdx.x] = reinterpret_cast<const u32x4*>(from.bytes)[threadIdx.x];
 }
 
 __global__ __launch_bounds__(256) void batch_rows_kernel(const int* __restrict__ tables,
@@ -304,11 +297,6 @@ hipError_t launch_import(const ImportArgs& a, const HandleWindow& w, int slot, i
 hipError_t launch_batch_rows(const int* tables, const BatchSeq* seqs, int n, int rows, int shift, int* place,
                              OwnSlots* own, hipStream_t st) {
   batch_rows_kernel<<<(rows + 255) / 256, 256, 0, st>>>(tables, seqs, n, rows, shift, place, own);
-  return hipGetLastError();
-}
-
-hipError_t launch_upload(const LittleUpload& from, void* to, int bytes, hipStream_t st) {
-  upload_kernel<<<1, 256, 0, st>>>(from, (u32x4*)to, (bytes + 15) / 16);
   return hipGetLastError();
 }
 

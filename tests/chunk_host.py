@@ -12,11 +12,6 @@ from paper_2604_20289_amd import build, xcache
 SHIM = host.SHIM + r"""
 #include "xc_chunk.h"
 namespace xc {
-hipError_t launch_upload(const LittleUpload&, void* to, int bytes, hipStream_t) {
-  if (counts_down(launch_fails)) return hipErrorLaunchFailure;
-  if (bytes > (int)LittleUpload::kMost) return hipErrorInvalidValue;
-  return ++launched, use(to), hipSuccess;
-}
 hipError_t launch_weights(int, const WeightArgs& a, hipStream_t) {
   const hipError_t e = launch(5);
   use(a.tables);
@@ -24,7 +19,8 @@ hipError_t launch_weights(int, const WeightArgs& a, hipStream_t) {
   return e;
 }
 static int evicted_most[2];
-hipError_t launch_evict(const EvictArgs& a, const PageBuf&, int, int, long long, int most_tokens, int most, hipStream_t) {
+hipError_t launch_evict(const EvictArgs& a, const Little*, const PageBuf&, int, int, long long, int most_tokens, int most,
+                        hipStream_t) {
   const hipError_t e = launch(6);
   use(a.seqs);
   use(a.src);
