@@ -392,11 +392,15 @@ __global__ __launch_bounds__(1024) void weights_join_kernel(WeightArgs a) {
 //
 // All that a workgroup has to know comes in two steps (its run, then rows,
 // pages and where its sums go), so that keys, queries and the old sums are asked
-// for together: 12.5 us for 16 rows over 14040 shared keys and 100 of their own,
+// for together: 12.6 us for 16 rows over 14040 shared keys and 100 of their own,
 // 12 heads of 128 (48 MB), where a search for the run and each row's sequence one
 // after the other take 14.4; 6.8 instead of 7.9 over 200 keys.
+// The rows of a sequence are summed by one lane of each key, by 2 to 8 where there
+// are few outputs of many rows (64 rows of one sequence over 4000 keys: 21.8 us
+// with one, 11.7), and the old sums of further outputs are asked for four at a
+// time (64 sequences over 20000 keys, 8 heads of 64: 29.1 us one by one, 27.0).
 // Bound by latency and by reading keys: one row over 48448 keys, 16 heads of 128
-// (198 MB) 31 us; 64 rows over 36288 and 100, 16 heads, 72, of which the queries
+// (198 MB) 31 us; 64 rows over 36288 and 100, 16 heads, 71, of which the queries
 // are much: a row per lane, 64 lines a load.  (By DMA into LDS, as the keys, they
 // gain nothing for 16 rows and lose a third for 64, whose LDS then leaves room for
 // one workgroup.)
@@ -423,22 +427,27 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightFew
   struct Out {
     float* to;
     float old;
-    int r0, r1;
+    int rows;  // of the first row and past the last, 8 bits each
   };
+  // Where they are few and of many rows, 2, 4 or 8 neighbouring lanes have one, each every so many of its rows.
   const int n_out = run.seqs * group_keys;
+  const int lanes_log2 = rows.n < 8 * run.seqs ? 0 : n_out <= 32 ? 3 : n_out <= 64 ? 2 : n_out <= 128 ? 1 : 0;
   auto out_of = [&](int x) __attribute__((always_inline)) {
-    const int si = min(x, n_out - 1) >> __builtin_ctz(group_keys), at = group0 + x - si * group_keys;
+    const int o = x >> lanes_log2, si = min(o, n_out - 1) >> __builtin_ctz(group_keys), at = group0 + o - si * group_keys;
     const WeightInfo s = a.infos[run.info + run.rows + si];
-    const bool is = x < n_out && at >= run.lo && at <= last;
-    return Out{is ? a.weights + s.a * a.ld + (at - run.first) : nullptr, 0.f, s.b, s.c};
+    const bool is = o < n_out && at >= run.lo && at <= last;
+    return Out{is ? a.weights + s.a * a.ld + (at - run.first) : nullptr, 0.f, s.b | s.c << 8};
   };
   auto old_of = [&](Out& o) __attribute__((always_inline)) {
     if (a.decay != 0.f && o.to) o.old = *o.to * a.decay;
   };
   constexpr int AHEAD = 3 - G;
+  constexpr bool LATE = G * HT > 2;  // (no registers for them)
   Out out[AHEAD];
+  if (!LATE) {
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) out[i] = out_of(threadIdx.x + i * 256);
+    for (int i = 0; i < AHEAD; ++i) out[i] = out_of(threadIdx.x + i * 256);
+  }
 
   // the groups of 16 places, each in one page; places outside the run read the nearest of it
   long long page_at[KEYS / 16];
@@ -542,8 +551,10 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightFew
     request(0);
     queries(0, q[0], l[0]);
   }
+  if (!LATE) {
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) old_of(out[i]);
+    for (int i = 0; i < AHEAD; ++i) old_of(out[i]);
+  }
   constexpr std::false_type more{};
   constexpr std::true_type last_one{};
   int i = 0;
@@ -572,22 +583,47 @@ __device__ __forceinline__ void few_weights(const WeightArgs& a, const WeightFew
       }
     }
   __syncthreads();
-  auto write = [&](const Out& o, int x) __attribute__((always_inline)) {
-    if (!o.to) return;
-    const int gk = x & (group_keys - 1), k = gk % KEYS;
+  if (LATE) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) out[i] = out_of(threadIdx.x + i * 256), old_of(out[i]);
+  }
+  // rows from, from + step, .. of an output's, all waves' shares
+  auto sum_of = [&](const Out& o, int gk, int from, int step) __attribute__((always_inline)) {
+    const int k = gk % KEYS;
     float sum = 0.f;
     for (int w = 0; w < hw; ++w) {
       const float* part = reinterpret_cast<const float*>(ring + (gk / KEYS * hw + w) * (2 * TILE)) + k * R;
-      for (int r = o.r0; r < o.r1; ++r) sum += part[(r + k) & (R - 1)];
+      for (int r = (o.rows & 255) + from; r < o.rows >> 8; r += step) sum += part[(r + k) & (R - 1)];
     }
-    *o.to = o.old + sum;
+    return sum;
+  };
+  if (lanes_log2 > 0) {
+    const int lanes = 1 << lanes_log2, from = threadIdx.x & (lanes - 1);
+    float sum = sum_of(out[0], threadIdx.x >> lanes_log2 & (group_keys - 1), from, lanes);
+    auto add = [&](auto ctrl) __attribute__((always_inline)) {
+      sum += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, sum), decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    add(std::integral_constant<int, 0xB1>{});                  // lane ^ 1
+    if (lanes > 2) add(std::integral_constant<int, 0x4E>{});   // lane ^ 2
+    if (lanes > 4) add(std::integral_constant<int, 0x141>{});  // the two quads of 8 lanes
+    if (out[0].to && from == 0) *out[0].to = out[0].old + sum;
+    return;
+  }
+  auto write = [&](const Out& o, int x) __attribute__((always_inline)) {
+    if (o.to) *o.to = o.old + sum_of(o, x & (group_keys - 1), 0, 1);
   };
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) write(out[i], threadIdx.x + i * 256);
-  for (int x = threadIdx.x + AHEAD * 256; x < n_out; x += 256) {
-    Out o = out_of(x);
-    old_of(o);
-    write(o, x);
+  // the others, so many at a time that their loads go together
+  constexpr int BATCH = 4;
+  for (int x = threadIdx.x + AHEAD * 256; x < n_out; x += BATCH * 256) {
+    Out o[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) o[i] = out_of(x + i * 256);
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) old_of(o[i]);
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) write(o[i], x + i * 256);
   }
 }
 template <int D>

@@ -49,6 +49,18 @@ def test_many_rows_of_any_number_of_heads(kv, group, d, dtype, rows):
         check(pool, batch, seqs, new, mask)
 
 
+@pytest.mark.parametrize("kv,d", [(12, 128), (5, 128), (3, 128), (1, 128), (4, 64), (2, 64), (1, 64)])
+def test_few_sequences_of_several_rows(kv, d):
+    """One to three sequences whose rows fill a workgroup: their keys' sums are dealt to as many lanes as there are."""
+    for branches in ([(0, 8)], [(3, 31)], [(0, 64)], [(0, 16), (9, 40)], [(0, 10), (0, 3), (20, 25)]):
+        pool = make(BF16, pages=pages_for(300, branches, 16), kv=kv, page=16, d=d, seqs=len(branches) + 1)
+        _, seqs = grow(pool, 300, 7, branches)
+        batch, new = Batch(pool), [n for _, n in branches]
+        for mask in ((1, 0, 0), (8, 50, 3)):
+            batch.set_chunk(seqs, new, *mask)
+            check(pool, batch, seqs, new, mask)
+
+
 @pytest.mark.parametrize("n,d", [(65, 128), (70, 64), (129, 64), (300, 128), (700, 64)])
 def test_many_single_tokens(n, d):
     """Sequences of one row over a history that they share, each with tokens of its own."""
