@@ -18,13 +18,10 @@ hipError_t launch_weights(int, const WeightArgs& a, hipStream_t) {
   if (a.n_units) use(a.parts);
   return e;
 }
-static int evicted_most[2];
-hipError_t launch_evict(const EvictArgs& a, const Little*, const PageBuf&, int, int, long long, int most_tokens, int most,
-                        hipStream_t) {
+hipError_t launch_evict(const EvictArgs& a, const Little*, const PageBuf&, int, int, long long, int, int, hipStream_t) {
   const hipError_t e = launch(6);
   use(a.seqs);
   use(a.src);
-  evicted_most[0] = most_tokens, evicted_most[1] = most;
   return e;
 }
 }  // namespace xc

@@ -232,6 +232,21 @@ def test_evictions_of_rows_in_one_piece_and_in_several(dtype, d, kv, n):
     evict_check(pool, Batch(pool), seqs, keep, 5, 4, torch.rand(n, 210, generator=g).cuda())
 
 
+@pytest.mark.parametrize("pages", [1, 2, 63, 64, 65, 415, 416, 417, 900])
+@pytest.mark.parametrize("shared", [False, True])
+def test_evictions_of_tables_of_every_size(shared, pages):
+    """One sequence's tables: of which so many fit into a kernel's arguments."""
+    pool = make(BF16, pages=2 * pages + 2, kv=1, page=16, d=64, seqs=3)
+    batch, s, g = Batch(pool), pool.new(), torch.Generator().manual_seed(pages)
+    pool.extend([s], [16 * pages])
+    if shared:
+        other, = pool.fork(s, 1)
+        before = ref.gather(pool.keys, 0, pool.pages(other))
+    evict_check(pool, batch, [s], [16 * pages - 3], 2, 5, torch.rand(1, 16 * pages, generator=g).cuda())
+    if shared:
+        assert torch.equal(ref.gather(pool.keys, 0, pool.pages(other)), before)
+
+
 @pytest.mark.parametrize("n", [1000, 1024, 1025, 5000, 24576, 24577, 60000])
 @pytest.mark.parametrize("sinks,recent", [(0, 0), (7, 300)])
 def test_evictions_among_few_different_weights(sinks, recent, n):
