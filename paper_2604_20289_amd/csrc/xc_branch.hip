@@ -189,6 +189,12 @@ __device__ __forceinline__ void spoil_rows(int u, int h, int keys, int r0, int r
   }
 }
 
+// ... written by whichever waves: their stores are done before a NaN goes over them.
+__device__ __forceinline__ void stores_done() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
 __device__ __forceinline__ float log_sum(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
 
 // The address of a unit's query row r, head dims hi * 8 on.
@@ -830,8 +836,10 @@ __device__ __forceinline__ void few_body(const AttnArgs& a, const U& un, int u, 
     }
   }
   if constexpr (CHUNK) {
-    if (spoils[0] | spoils[1] | spoils[2] | spoils[3])
+    if (__builtin_amdgcn_readfirstlane(spoils[0] | spoils[1] | spoils[2] | spoils[3]) != 0) {
+      stores_done();
       spoil_rows<bf16>(u, h, S::KEYS, wave * (G * 8), min((wave + 1) * (G * 8), rows));
+    }
   }
 }
 template <int D, bool CHUNK>
@@ -1032,7 +1040,10 @@ __global__ __launch_bounds__(256, 1) void branch_f32_kernel(AttnArgs a) {
     }
   }
   if constexpr (CHUNK) {
-    if (spoils[0] | spoils[1] | spoils[2] | spoils[3]) spoil_rows<float>(u, h, 32, wave * 8, min(wave * 8 + 8, rows));
+    if (__builtin_amdgcn_readfirstlane(spoils[0] | spoils[1] | spoils[2] | spoils[3]) != 0) {
+      stores_done();
+      spoil_rows<float>(u, h, 32, wave * 8, min(wave * 8 + 8, rows));
+    }
   }
 }
 
