@@ -31,7 +31,9 @@ struct Term {
 __device__ __forceinline__ Term term_of(float lse) {
   constexpr float kLog2e = 1.44269502162933349609375f, kRest = 1.925963033500e-8f;
   const float hi = lse * kLog2e, lo = __builtin_fmaf(lse, kLog2e, -hi) + lse * kRest;
-  return {hi, lo == lo ? __builtin_amdgcn_exp2f(-lo) : 1.f};  // (infinite or NaN: hi says it)
+  // Infinite or NaN: hi says it.  From some 10^9 on lo itself is past 128: bounded, so that f is a number and nothing times f
+  // nothing.
+  return {hi, lo == lo ? __builtin_amdgcn_exp2f(__builtin_amdgcn_fmed3f(-lo, -126.f, 126.f)) : 1.f};
 }
 
 // (nothing, where it is no row)
