@@ -346,6 +346,13 @@ constexpr RowRange rows_seeing_all(const ChunkSeq& q, const ChunkMask& m, int k0
   return r;
 }
 
+// Of a workgroup's rows [r0, r1), `group` query rows each in tiles of 32: the tiles that lie in rows `all`.  (Within its rows
+// first: 2^24 of 256 query rows would not fit into 32 bits.)
+constexpr RowRange tiles_within(const RowRange& all, int r0, int r1, int group) {
+  const int begin = all.begin < r0 ? r0 : all.begin < r1 ? all.begin : r1, end = all.end < r0 ? r0 : all.end < r1 ? all.end : r1;
+  return {((begin - r0) * group + 31) >> 5, ((end - r0) * group) >> 5};
+}
+
 // Keys of a workgroup, query rows of a stage of its queries.
 constexpr int kWeightKeys = 256, kWeightKeysF32 = 128, kWeightRows = 64, kWeightRowsF32 = 32;
 // A workgroup's share: what rows [r0, r1) of a sequence give to the keys at

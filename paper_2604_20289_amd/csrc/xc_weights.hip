@@ -162,8 +162,8 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(WeightArgs a) {
   }
   // tiles [free0, free1) of 32 query rows see all of this wave's keys
   const RowRange all = rows_seeing_all(sq, a.mask, min(k0, un.hi - 1), min(k0 + 64, un.hi));
-  const int free0 = __builtin_amdgcn_readfirstlane(max(0, (all.begin - un.r0) * a.group + 31) >> 5);
-  const int free1 = __builtin_amdgcn_readfirstlane(min(rows.n, max(0, all.end - un.r0) * a.group) >> 5);
+  const RowRange free = tiles_within(all, un.r0, un.r1, a.group);
+  const int free0 = __builtin_amdgcn_readfirstlane(free.begin), free1 = __builtin_amdgcn_readfirstlane(free.end);
 #pragma unroll
   for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -310,8 +310,8 @@ __global__ __launch_bounds__(256) void weights_f32_kernel(WeightArgs a) {
     for (int t = 0; t < D / 8; ++t) kf[t] = *reinterpret_cast<const f32x4*>(k + t * 8);
   }
   const RowRange all = rows_seeing_all(sq, a.mask, min(k0, un.hi - 1), min(k0 + 32, un.hi));
-  const int free0 = __builtin_amdgcn_readfirstlane(max(0, (all.begin - un.r0) * a.group + 31) >> 5);
-  const int free1 = __builtin_amdgcn_readfirstlane(min(rows.n, max(0, all.end - un.r0) * a.group) >> 5);
+  const RowRange free = tiles_within(all, un.r0, un.r1, a.group);
+  const int free0 = __builtin_amdgcn_readfirstlane(free.begin), free1 = __builtin_amdgcn_readfirstlane(free.end);
 #pragma unroll
   for (int t = 0; t < D / 8; ++t) asm volatile("" : "+v"(kf[t]));
   f32x16 acc;

@@ -1,0 +1,51 @@
+"""Chunks under a mask at the largest sizes that include/xcache.h allows, on the CPU: what no test on a GPU has memory for."""
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2604_20289_amd import build
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="no host compiler")
+
+TILES = r"""
+#include "xc_chunk_plan.h"
+#include <cstdio>
+using namespace xc;
+
+// a tile lies in rows `all` iff each of its 32 query rows is one of theirs
+static bool truth(const RowRange& all, int r0, long long n, int group, long long tile) {
+  if ((tile + 1) * 32 > n) return false;
+  for (long long i = tile * 32; i < tile * 32 + 32; ++i)
+    if (r0 + i / group < all.begin || r0 + i / group >= all.end) return false;
+  return true;
+}
+int main() {
+  const int most = 1 << 24;
+  for (int group : {1, 3, 29, 64, 100, 128, 255, 256})
+    for (int r0 : {0, 1, 777, (1 << 23) - 100, most - 4096 / group - 5})
+      for (int rows : {1, 2, 31, 4096 / group + 1})
+        for (int begin : {0, r0 - 1, r0, r0 + 1, r0 + rows / 2, r0 + rows, r0 + rows + 1, 1 << 23, (1 << 23) + 1, most - 1, most})
+          for (int end : {0, r0, r0 + 1, r0 + rows / 2, r0 + rows, r0 + rows + 9, (1 << 23) + 1, most}) {
+            if (begin < 0 || begin > end || end > most) continue;
+            const RowRange all{begin, end}, got = tiles_within(all, r0, r0 + rows, group);
+            const long long n = (long long)rows * group;
+            for (long long t = 0; t * 32 < n; ++t)
+              if ((t >= got.begin && t < got.end) != truth(all, r0, n, group, t))
+                return printf("group %d, rows %d + %d, all %d to %d: tile %lld\n", group, r0, rows, begin, end, t), 1;
+          }
+  return 0;
+}
+"""
+
+
+def run(tmp_path, source):
+    src, exe = tmp_path / "check.cpp", tmp_path / "check"
+    src.write_text(source)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-D_GLIBCXX_ASSERTIONS", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout
+
+
+def test_tiles_of_rows_that_see_all_of_some_keys(tmp_path):
+    run(tmp_path, TILES)
