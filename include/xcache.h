@@ -630,8 +630,10 @@ xc_status xc_chunk_weights(xc_batch* batch, int32_t block, const void* q, int64_
  * tokens, which do not move; pages left over are released.  The batch lends
  * its staging memory alone (it need not be set, and its rows play no part);
  * batches of sequences that shrank are set anew before their next call.
- * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED (more than 65535 sequences),
- * XC_ERR_OOM (all or nothing), XC_ERR_STATE, XC_ERR_HIP (sticky). */
+ * Errors: XC_ERR_INVALID_ARG, XC_ERR_UNSUPPORTED (more than 65535 sequences;
+ * those that shrink have 2^30 pages together or keep more than 2^30 tokens,
+ * shared ones counted for each), XC_ERR_OOM (all or nothing), XC_ERR_STATE,
+ * XC_ERR_HIP (sticky). */
 xc_status xc_chunk_evict(xc_batch* batch, int32_t n, const int32_t* seqs, const int32_t* keep, int32_t sinks,
                          int32_t recent, float* weights, int64_t ld, int32_t* kept, int64_t kept_ld);
 

@@ -237,7 +237,10 @@ xc_status xc_chunk_evict(xc_batch* b, int32_t n, const int32_t* seqs, const int3
     std::vector<EvictSeq> list;
     std::vector<int> tables;
     int most_tokens = 0, most_listed = 0, most_kept = 0;
-    long long places = 0;
+    long long places = 0, pages = 0;
+    // the kernels number the pages before and after, which are no more, in 32 bits
+    for (int i = 0; i < n; ++i) pages += keep[i] < p.book.seq(seqs[i]).tokens ? p.book.seq(seqs[i]).pages.size() : 0;
+    if (pages >= kMaxPlaces) return XC_ERR_UNSUPPORTED;
     for (int i = 0; i < n; ++i) {
       const PageSeq& q = p.book.seq(seqs[i]);
       if (keep[i] < 0) return XC_ERR_INVALID_ARG;

@@ -1,10 +1,13 @@
 """Chunks under a mask at the largest sizes that include/xcache.h allows, on the CPU: what no test on a GPU has memory for."""
+import ctypes
 import shutil
 import subprocess
 
 import pytest
 
+import chunk_host as chunk
 from paper_2604_20289_amd import build
+from paper_2604_20289_amd.xcache import XC_ERR_UNSUPPORTED, XC_OK
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="no host compiler")
 
@@ -49,3 +52,27 @@ def run(tmp_path, source):
 
 def test_tiles_of_rows_that_see_all_of_some_keys(tmp_path):
     run(tmp_path, TILES)
+
+
+def test_an_eviction_numbers_its_pages_in_32_bits():
+    """16 forks of the longest sequence there is list 2^30 pages, and as many again may be those after: refused, with the tables as
+    they were.  (Their page tables take 4 GB here.)"""
+    pool = chunk.Pool(n_pages=1 << 26, max_seqs=20)
+    a = pool.new(1 << 30)
+    seqs = [a] + pool.fork(a, 15)
+    launches = chunk.info()["launches"]
+    assert pool.evict(seqs, [1] * 16, ld=1 << 30, kept=None) == XC_ERR_UNSUPPORTED
+    assert chunk.info()["launches"] == launches
+    live = ctypes.c_int32()
+    assert chunk.lib().xc_pool_info(pool.p, ctypes.byref(live), None, None) == XC_OK and live.value == 1 << 26
+    assert all(pool.table(s, 0)[1] == 1 << 30 for s in seqs)
+    pool.close()
+
+
+def test_an_eviction_numbers_its_kept_tokens_in_32_bits():
+    pool = chunk.Pool(n_pages=1 << 22, page_tokens=256, max_seqs=4)
+    a = pool.new(1 << 30)
+    seqs = [a] + pool.fork(a, 1)
+    assert pool.evict(seqs, [(1 << 29) + 1, 1 << 29], ld=1 << 30, kept=None) == XC_ERR_UNSUPPORTED
+    assert [pool.table(s, 0)[1] for s in seqs] == [1 << 30] * 2
+    pool.close()
