@@ -577,9 +577,11 @@ typedef struct xc_chunk_mask {
 /* As xc_batch_set, for rows under a mask (NULL: none): the batch then serves
  * xc_qk_norm_rope, xc_chunk_attention and xc_chunk_weights
  * (xc_branch_attention has no mask and returns XC_ERR_STATE), until it is set
- * again or goes out of date.
- * Errors: those of xc_batch_set; XC_ERR_INVALID_ARG also for a negative field
- * of the mask. */
+ * again or goes out of date.  Asks for the memory of xc_chunk_weights too; where
+ * there is none for it, that call alone is left without.
+ * Errors: those of xc_batch_set, XC_ERR_UNSUPPORTED also where
+ * xc_chunk_weights would take more than a launch; XC_ERR_INVALID_ARG also for a
+ * negative field of the mask. */
 xc_status xc_chunk_set(xc_batch* batch, int32_t n, const int32_t* seqs, const int32_t* new_tokens,
                        const xc_chunk_mask* mask);
 
@@ -609,7 +611,8 @@ xc_status xc_chunk_attention(xc_batch* batch, int32_t block, const void* q, int6
  *              buffers.
  * The same call gives the same bits.  Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE
  * (as xc_chunk_attention), XC_ERR_UNSUPPORTED (rows of q of 256 MiB or more
- * apart), XC_ERR_HIP (sticky). */
+ * apart), XC_ERR_OOM (no memory for partial sums, when the batch was set and
+ * again now; in a capture it is not asked for again), XC_ERR_HIP (sticky). */
 xc_status xc_chunk_weights(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, const float* lse,
                            float decay, float* weights, int64_t ld);
 

@@ -8,6 +8,13 @@ using namespace xc;
 
 namespace {
 
+// The batch's partial sums of weights; false: no memory for them.
+bool room_for_parts(xc_batch* b) {
+  Pool& p = *b->p;
+  return enlarge(p, b->parts, b->parts_bytes, b->parts_need, b->parts_need / 4) ||
+         enlarge(p, b->parts, b->parts_bytes, b->parts_need, 0);
+}
+
 xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* new_tokens, const ChunkMask& mask) {
   Pool& p = *b->p;
   BatchRows r;
@@ -37,8 +44,6 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   WeightPlan sums;
   if (p.esz == 2 && !runs.empty()) few = few_runs(runs, chunk_seqs, mask, group, &infos);
   else sums = plan_weights(chunk_seqs, mask, shape);
-  const size_t part_need =
-      (size_t)sums.parts * p.cfg.kv_heads * (p.esz == 2 ? kWeightKeys : kWeightKeysF32) * sizeof(float);
   if ((((long long)sums.units.size() + kXcds) * p.cfg.kv_heads + kXcds * kXcds) * 256 >> 32 || (long long)groups * 256 >> 32 ||
       (long long)sums.tiles.size() * 1024 >> 32)
     return XC_ERR_UNSUPPORTED;
@@ -55,7 +60,7 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
     const ChunkSeq& q = chunk_seqs[part.seq];
     batch_seqs.push_back({part.tok0, q.first + q.tokens - q.rows + (part.tok0 - q.row0), q.table, part.own});
   }
-  // uploaded: tables, sequences, units; written on the device: places, own slots, partial sums
+  // uploaded: tables, sequences, units; written on the device: places, own slots
   const size_t o_seqs = align256(r.tables.size() * sizeof(int));
   const size_t o_chunks = o_seqs + align256(batch_seqs.size() * sizeof(BatchSeq));
   const size_t o_units = o_chunks + align256(chunk_seqs.size() * sizeof(ChunkSeq));
@@ -65,9 +70,13 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   const size_t o_tiles = o_sums + align256(sums.units.size() * sizeof(WeightUnit));
   const size_t up = o_tiles + align256(sums.tiles.size() * sizeof(WeightTile));
   const size_t o_own = up + align256(rows * sizeof(int));
-  const size_t o_parts = o_own + align256(rows * sizeof(OwnSlots)), need = o_parts + part_need;
+  const size_t need = o_own + align256(rows * sizeof(OwnSlots));
   std::vector<int> seq_copy(seqs, seqs + n);
-  if (!staging(b, b->dev, b->dev_bytes, need, up)) return XC_ERR_OOM;
+  // (a quarter more than needed, as of pieces and sums)
+  if (!enlarge(p, b->dev, b->dev_bytes, need, need / 4) || !staging(b, b->dev, b->dev_bytes, need, up)) return XC_ERR_OOM;
+  // Asked for here, since xc_chunk_weights may be captured; the attention does without.
+  b->parts_need = (size_t)sums.parts * p.cfg.kv_heads * (p.esz == 2 ? kWeightKeys : kWeightKeysF32) * sizeof(float);
+  (void)room_for_parts(b);
   if (rows > 0) {
     put(b, 0, r.tables);
     put(b, o_seqs, batch_seqs);
@@ -113,7 +122,6 @@ xc_status set_chunk(xc_batch* b, int32_t n, const int32_t* seqs, const int32_t* 
   w.n_units = (int)sums.units.size();
   w.n_long = long_units(sums.units);
   w.n_tiles = (int)sums.tiles.size();
-  w.parts = (float*)(b->dev + o_parts);
   w.runs = (const WeightFew*)(b->dev + o_runs);
   w.infos = (const WeightInfo*)(b->dev + o_infos);
   w.n_runs = (int)few.size();
@@ -210,7 +218,13 @@ xc_status xc_chunk_weights(xc_batch* b, int32_t block, const void* q, int64_t q_
     const Rows in = rows_at(q, b->rows, q_ld, width, p.esz), sums = rows_at(lse, b->rows, c.q_heads, c.q_heads, 4),
                to = rows_at(weights, (long long)b->seqs.size(), ld, most, 4);
     if (overlap(in, to) || overlap(sums, to) || p.holds(weights, to.extent)) return XC_ERR_INVALID_ARG;
+    if (b->parts_bytes < b->parts_need) {
+      if (capturing(p.st)) return XC_ERR_OOM;
+      const OutsideCapture outside;
+      if (!room_for_parts(b)) return XC_ERR_OOM;
+    }
     WeightArgs a = b->weights;
+    a.parts = (float*)b->parts;
     a.buf = p.block(block);
     a.q = q;
     a.q_ld = q_ld;

@@ -283,9 +283,10 @@ xc_status xc_batch_destroy(xc_batch* b) {
   try {
     const DeviceScope scope(b->p->device);
     const OutsideCapture outside;
-    if (b->dev || b->pieces || b->evict || b->pinned) (void)hipStreamSynchronize(b->p->st);
+    if (b->dev || b->pieces || b->parts || b->evict || b->pinned) (void)hipStreamSynchronize(b->p->st);
     if (b->dev) (void)hipFree(b->dev);
     if (b->pieces) (void)hipFree(b->pieces);
+    if (b->parts) (void)hipFree(b->parts);
     if (b->evict) (void)hipFree(b->evict);
     if (b->pinned) (void)hipHostFree(b->pinned);
     if (b->uploaded) (void)hipEventDestroy(b->uploaded);

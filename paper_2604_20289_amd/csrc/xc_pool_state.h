@@ -133,6 +133,8 @@ struct xc_batch {
   size_t dev_bytes = 0;
   char* pieces = nullptr;
   size_t piece_bytes = 0;
+  char* parts = nullptr;  // partial sums of weights; parts_need: of the rows that are set
+  size_t parts_bytes = 0, parts_need = 0;
   char* evict = nullptr;  // an eviction's tables and choices
   size_t evict_bytes = 0;
   char* pinned = nullptr;

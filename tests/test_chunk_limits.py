@@ -6,8 +6,9 @@ import subprocess
 import pytest
 
 import chunk_host as chunk
+import pool_host as host
 from paper_2604_20289_amd import build
-from paper_2604_20289_amd.xcache import XC_ERR_UNSUPPORTED, XC_OK
+from paper_2604_20289_amd.xcache import XC_BF16, XC_ERR_OOM, XC_ERR_UNSUPPORTED, XC_F32, XC_OK
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="no host compiler")
 
@@ -75,4 +76,47 @@ def test_an_eviction_numbers_its_kept_tokens_in_32_bits():
     seqs = [a] + pool.fork(a, 1)
     assert pool.evict(seqs, [(1 << 29) + 1, 1 << 29], ld=1 << 30, kept=None) == XC_ERR_UNSUPPORTED
     assert [pool.table(s, 0)[1] for s in seqs] == [1 << 30] * 2
+    pool.close()
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_attention_needs_no_memory_for_weights(new):
+    """Where there is room for all but the partial sums, the rows are set and attended; the weights come once there is room."""
+    shape = dict(n_pages=3000, q_heads=8, kv_heads=8, dtype=XC_F32 if new == 1 else XC_BF16)
+
+    def rows():
+        pool = chunk.Pool(**shape)
+        kids = pool.fork(pool.new(5000), 20)
+        assert chunk.lib().xc_seq_extend(pool.p, 20, host.ints(*kids), host.ints(*[new] * 20)) == XC_OK
+        return pool, kids
+
+    pool, kids = rows()
+    before = chunk.info()["live_bytes"]
+    assert pool.set(kids, [new] * 20) == XC_OK
+    all_of_it = chunk.info()["live_bytes"] - before
+    pool.close()
+    keys = 128 if new == 1 else 256
+    sums = 20 * -(-(5000 + new) // keys) * 8 * keys * 4  # a partial sum per key and head
+    pool, kids = rows()
+    for room, fits in ((all_of_it - sums // 4 - 1, False), (all_of_it - sums // 4, True)):
+        chunk.lib().fake_memory(before + room)
+        assert pool.set(kids, [new] * 20) == XC_OK
+        assert pool.attention() == XC_OK
+        assert pool.weights() == (XC_OK if fits else XC_ERR_OOM) and pool.attention() == XC_OK
+    pool.close()
+    # asked for again, but not in a capture
+    pool, kids = rows()
+    chunk.lib().fake_memory(before + all_of_it - sums // 4 - 1)
+    assert pool.set(kids, [new] * 20) == XC_OK
+    chunk.lib().fake_memory(1 << 60)
+    chunk.lib().fake_set(0, 1)
+    assert pool.weights() == XC_ERR_OOM and pool.attention() == XC_OK
+    chunk.lib().fake_set(0, 0)
+    chunk.lib().fake_elsewhere(1)
+    assert pool.weights() == XC_OK
+    chunk.lib().fake_elsewhere(0)
+    chunk.lib().fake_set(0, 1)
+    assert pool.weights() == XC_OK and pool.attention() == XC_OK
+    chunk.lib().fake_set(0, 0)
+    assert chunk.info()["broken_captures"] == 0
     pool.close()
