@@ -538,7 +538,9 @@ xc_status xc_qk_norm_rope(xc_batch* batch, int32_t block, const void* qkv, int64
  * head_dim 64 sum the rounded ones).  The same call gives the same bits.  Keys
  * and values outside the sequences are not read.  NaN and infinities reach the
  * rows and heads that attend to them alone; an infinite value gives infinity or
- * NaN in its column.
+ * NaN in its column.  A row's largest score is below 2^30 in magnitude, or
+ * infinite: past that its float32 rounding no longer fits into an exponential,
+ * and the row may become NaN.
  * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set, set by xc_chunk_set or
  * out of date), XC_ERR_HIP (sticky). */
 xc_status xc_branch_attention(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, void* out,

@@ -43,3 +43,33 @@ def test_one_row_of_enormous_scores(size, dtype, d, rows):
     got = w[0].double().cpu()
     rest = torch.arange(rows) != t
     assert ((got - total).abs() <= tol + 1e-30)[rest].all()
+
+
+@pytest.mark.parametrize("dtype,d,rows,kv", [(BF16, 64, 40, 2), (BF16, 128, 40, 2), (BF16, 64, 300, 256), (BF16, 128, 300, 256),
+                                             (F32, 32, 40, 2), (F32, 64, 70, 2), (F32, 128, 300, 2)])
+@pytest.mark.parametrize("size", [3e8, -3e8, 1.06e9, -1.06e9])
+def test_scores_of_up_to_2_to_the_30(size, dtype, d, rows, kv):
+    """As above: the row's result is the value of the token with all of its weight, through a probability and a result that are
+    rounded once each; its log-sum-exp is the score, through a dozen roundings of 2^-24."""
+    pool = make(dtype, pages=-(-rows // 16) + 1, kv=kv, page=16, d=d, seqs=2)
+    s = pool.new()
+    pool.extend([s], [rows])
+    g = torch.Generator().manual_seed(9)
+    k, v = torch.randn(2, rows, kv, d, generator=g)
+    q = torch.randn(rows, kv, d, generator=g)
+    q[..., 0] = k[..., 0] = 0
+    row, t = (0, 0) if size < 0 else (rows // 2, rows // 4)
+    root = 2.0 ** 15 if abs(size) > 1e9 else 2.0 ** 14
+    q[row, :, 0], k[t, :, 0] = root, size / root
+    write(pool, s, k, v)
+    q = q.to(dtype).cuda()
+    batch = Batch(pool)
+    batch.set_chunk([s], [rows])
+    out, lse = torch.empty_like(q), torch.empty(rows, kv, device="cuda")
+    batch.chunk_attention(0, q, out, lse=lse, scale=1.0)
+    k, v = (ref.gather(b, 0, pool.pages(s)) for b in (pool.keys, pool.values))
+    score = (q[row].double().cpu() * k[t]).sum(-1)
+    assert (score.abs() < 2.0 ** 30).all()
+    assert ((out[row].double().cpu() - v[t]).abs() <= (2 * torch.finfo(dtype).eps / 2 + 2.0 ** -20) * v[t].abs()).all()
+    assert ((lse[row].double().cpu() - score).abs() <= 12 * 2.0 ** -24 * score.abs()).all()
+    assert torch.isfinite(out.double()).all() and torch.isfinite(lse).all()
