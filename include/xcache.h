@@ -538,9 +538,9 @@ xc_status xc_qk_norm_rope(xc_batch* batch, int32_t block, const void* qkv, int64
  * head_dim 64 sum the rounded ones).  The same call gives the same bits.  Keys
  * and values outside the sequences are not read.  NaN and infinities reach the
  * rows and heads that attend to them alone; an infinite value gives infinity or
- * NaN in its column.  A row's largest score is below 2^30 in magnitude, or
- * infinite: past that its float32 rounding no longer fits into an exponential,
- * and the row may become NaN.
+ * NaN in its column.  A row's largest score is to be below 2^30 in magnitude:
+ * past that what its float32 rounding leaves no longer fits into an
+ * exponential, and the row may become NaN.
  * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set, set by xc_chunk_set or
  * out of date), XC_ERR_HIP (sticky). */
 xc_status xc_branch_attention(xc_batch* batch, int32_t block, const void* q, int64_t q_ld, float scale, void* out,
@@ -592,6 +592,7 @@ xc_status xc_chunk_set(xc_batch* batch, int32_t n, const int32_t* seqs, const in
  *   lse : device float32 [rows][q_heads], the natural logarithm of the row's
  *         sum of exp(scale q k^T); NULL: not wanted.  Does not overlap q, out
  *         or the page buffers.
+ * Sums and log-sum-exps take the probabilities before they are rounded to bf16.
  * Keys and values that a row does not see do not reach it, whatever they hold;
  * NaN and infinities that it sees do, as there.
  * Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE (not set by xc_chunk_set, or out of
@@ -611,6 +612,9 @@ xc_status xc_chunk_attention(xc_batch* batch, int32_t block, const void* q, int6
  *   weights  : device float32 [n of xc_chunk_set][ld], ld at least the tokens of
  *              the longest sequence; does not overlap q, lse or the page
  *              buffers.
+ * In bf16 pools, where every sequence has at most 64 rows times query heads per
+ * key head, the keys that all of them share are read once for as many rows as
+ * that; one longer sequence, or float32, and they are read for each.
  * The same call gives the same bits.  Errors: XC_ERR_INVALID_ARG, XC_ERR_STATE
  * (as xc_chunk_attention), XC_ERR_UNSUPPORTED (rows of q of 256 MiB or more
  * apart), XC_ERR_OOM (no memory for partial sums, when the batch was set and

@@ -158,8 +158,9 @@ struct TableWindow {
   }
 };
 
-// Rows [r0, r1) of a unit, written before: NaN where they see a value that is
-// not finite in a tile that not all rows see.  A wave, a lane per column or two.
+// Rows [r0, r1) of a unit, written before (by other waves: before stores_done): NaN
+// where they see a value that is not finite in a tile that not all rows see.  A
+// wave, a lane per column or two.
 // (Its arguments are loaded here: held in registers from the start they would crowd out the loop's.)
 template <typename T>
 __device__ __forceinline__ void spoil_rows(int u, int h, int keys, int r0, int r1) {

@@ -370,7 +370,7 @@ struct WeightPlan {
   int parts = 0;
 };
 
-// Few rows: the keys of a run of places and the query rows of sequences
+// Few rows (bf16; a float32 batch has units): the keys of a run of places and the query rows of sequences
 // seq0 .. seq0 + n_seqs - 1, at most kWeightFew of them, which all have these
 // places.  Its workgroups begin at number `group0`.
 constexpr int kWeightFew = 64;

@@ -7,10 +7,11 @@
 // fixed order.  exp2(x - hi) f, with lse log2(e) = hi + lo rounded apart and f =
 // 2^-lo, keeps what the product with log2(e) would lose of a large lse.
 //
-// Two kinds of workgroup.  Many rows: weights_kernel (float32:
+// Two kinds of workgroup.  Many rows: weights_kernel (float32, of few rows too:
 // weights_f32_kernel), 256 (128) keys of one head against a run of rows, whose
-// partial sums weights_join_kernel adds up.  Few rows: weights_few_kernel, all
-// heads of a few keys, read once for all sequences that have them.
+// partial sums weights_join_kernel adds up.  bf16 batches of sequences that all
+// have few rows: weights_few_kernel, all heads of a few keys, read once for all
+// sequences that have them.
 #include "xc_chunk.h"
 
 #include "xc_internal.h"
